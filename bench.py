@@ -63,11 +63,11 @@ PAPER_CONTEXT = {
 
 
 def source_digest():
-    """sha256 (first 16 hex digits) over the library's sources: ties a counter measurement to the code."""
+    """sha256 (first 16 hex digits) over the CTC path's sources: ties a counter measurement to the code."""
     import hashlib
     h = hashlib.sha256()
     csrc = os.path.join(ROOT, "paper_1512_02595_amd", "csrc")
-    for name in sorted(os.listdir(csrc)):
+    for name in sorted(n for n in os.listdir(csrc) if not n.startswith("layer_")):
         with open(os.path.join(csrc, name), "rb") as f:
             h.update(name.encode() + b"\0" + f.read())
     return h.hexdigest()[:16]

@@ -1,0 +1,651 @@
+// Kernels of the output layer held in 8 bits (ctc_layer.h).
+
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "layer_internal.h"
+
+namespace layer {
+namespace {
+
+constexpr int kWave = 64;
+
+// ---- elements ---------------------------------------------------------------------------------------------------
+
+struct bf16_t { uint16_t bits; };
+
+__device__ __forceinline__ float widen(float v) { return v; }
+__device__ __forceinline__ float widen(bf16_t v) { return __uint_as_float(static_cast<uint32_t>(v.bits) << 16); }
+
+// To the nearest, ties to even; a NaN stays one.
+template <typename T> __device__ __forceinline__ T narrow(float v);
+template <> __device__ __forceinline__ float narrow<float>(float v) { return v; }
+template <> __device__ __forceinline__ bf16_t narrow<bf16_t>(float v)
+{
+    return {__builtin_bit_cast(uint16_t, static_cast<__bf16>(v))};
+}
+
+// 16 bytes of a row: 4 floats or 8 bf16.  Rows of odd widths begin anywhere, so these are loads and stores that ask for the
+// alignment of an element only, which the hardware takes.
+template <typename T> struct Vector {
+    static constexpr int kElements = 16 / sizeof(T);
+    T v[kElements];
+};
+template <typename T> __device__ __forceinline__ Vector<T> load_whole(const T* p)
+{
+    Vector<T> r;
+    __builtin_memcpy(&r, p, 16);
+    return r;
+}
+// Elements [col, col + kElements) of a row of H; behind the row's end zeros.
+template <typename T> __device__ __forceinline__ Vector<T> load_vector(const T* row, int col, int H)
+{
+    constexpr int kE = Vector<T>::kElements;
+    if (col + kE <= H) return load_whole(row + col);
+    Vector<T> r;
+#pragma unroll
+    for (int i = 0; i < kE; ++i) r.v[i] = col + i < H ? row[col + i] : narrow<T>(0.0f);
+    return r;
+}
+template <typename T> __device__ __forceinline__ void store_vector(T* row, int col, int H, const Vector<T>& r)
+{
+    constexpr int kE = Vector<T>::kElements;
+    if (col + kE <= H) {
+        __builtin_memcpy(row + col, &r, 16);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < kE; ++i)
+        if (col + i < H) row[col + i] = r.v[i];
+}
+
+// ---- lists of rows ----------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ int listed(const int32_t* frames, int rows)
+{
+    if (!frames) return rows;
+    const int n = frames[0];
+    return n < 0 ? 0 : n > rows ? rows : n;
+}
+// Row of the i-th entry, i < listed(); -1: an entry to skip.
+__device__ __forceinline__ int row_of(const int32_t* frames, int rows, int i)
+{
+    if (!frames) return i;
+    const int r = frames[1 + static_cast<int64_t>(i)];
+    return r < 0 || r >= rows ? -1 : r;
+}
+
+// ---- sums and maxima over lanes ---------------------------------------------------------------------------------
+
+__device__ __forceinline__ uint32_t wave_max(uint32_t v)
+{
+#pragma unroll
+    for (int d = 32; d; d >>= 1) {
+        const uint32_t o = __shfl_xor(v, d, kWave);
+        v = v > o ? v : o;
+    }
+    return v;
+}
+template <typename V> __device__ __forceinline__ V wave_sum(V v)
+{
+#pragma unroll
+    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d, kWave);
+    return v;
+}
+
+// ---- frames of a minibatch --------------------------------------------------------------------------------------
+
+// Rows in ascending order: frame t's begin behind sum_b min(length_b, t) others, so a wavefront to a frame needs nobody.
+__global__ __launch_bounds__(256) void ctc_pack_frames_kernel(const int32_t* __restrict__ lengths, int T, int B,
+                                                              int32_t* __restrict__ frames)
+{
+    const int lane = threadIdx.x % kWave, t = blockIdx.x * 4 + threadIdx.x / kWave;
+    if (t >= T) return;
+    int before = 0, all = 0;
+    for (int b = lane; b < B; b += kWave) {
+        int n = lengths[b];
+        n = n < 0 ? 0 : n > T ? T : n;
+        before += n < t ? n : t;
+        all += n;
+    }
+    before = wave_sum(before);
+    if (t == 0) {
+        all = wave_sum(all);
+        if (lane == 0) frames[0] = all;
+    }
+    int at = before;
+    for (int b0 = 0; b0 < B; b0 += kWave) {
+        const int b = b0 + lane;
+        const bool in = b < B && lengths[b] > t;
+        const uint64_t who = __ballot(in);
+        if (in) frames[1 + static_cast<int64_t>(at) + __popcll(who & ((1ull << lane) - 1))] = t * B + b;
+        at += __popcll(who);
+    }
+}
+
+// ---- rows to 8 bits ---------------------------------------------------------------------------------------------
+
+constexpr uint32_t kInfinity = 0x7f800000u;
+
+// The whole number nearest to 127 |u| / m, ties to even, exactly: `inverse` is 127 / m to within half a step, so the
+// product is off by less than 2^-16 (127 * 2^-23); where it comes that near to the middle between two whole numbers, 254 |u|
+// is compared with (2 j + 1) m, both of which fp64 holds (32 bits).
+__device__ __forceinline__ int level(float u, float m, float inverse)
+{
+    const float a = fabsf(u), t = a * inverse;
+    int k = static_cast<int>(rintf(t));
+    if (fabsf(t - static_cast<float>(k)) > 0.5f - 0x1p-15f) {
+        const int j = static_cast<int>(t);
+        const double twice = 254.0 * static_cast<double>(a), middle = static_cast<double>(2 * j + 1) * static_cast<double>(m);
+        k = twice > middle || (twice == middle && (j & 1)) ? j + 1 : j;
+    }
+    return u < 0.0f ? -k : k;
+}
+
+struct NormArgs {
+    const void* x;
+    const void* residual;
+    const float* weight;
+    float eps;
+    const int32_t* frames;
+    int rows, H, pitch;
+    void* sum;
+    int8_t* q;
+    float* scales;
+};
+
+// One row to a wavefront, or to the four of a workgroup; a row's elements stay in registers (E to a thread) from its one
+// reading to its writing, its maximum and its sum of squares are formed across lanes.  Bound by the bytes.
+template <typename T, int WAVES, int E, bool NORM>
+__global__ __launch_bounds__(256) void ctc_rows_to_8_bits_kernel(NormArgs p)
+{
+    constexpr int kE = Vector<T>::kElements, kVectors = E / kE;
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int i = blockIdx.x * (4 / WAVES) + wave / WAVES;
+    if (i >= listed(p.frames, p.rows)) return;
+    const int r = row_of(p.frames, p.rows, i);
+    if (r < 0) return;
+    const int thread = (wave % WAVES) * kWave + lane;
+    const T* x = static_cast<const T*>(p.x) + static_cast<int64_t>(r) * p.H;
+    const T* residual = NORM && p.residual ? static_cast<const T*>(p.residual) + static_cast<int64_t>(r) * p.H : nullptr;
+    float u[E];
+    double squares = 0.0;
+    uint32_t most = 0;
+#pragma unroll
+    for (int v = 0; v < kVectors; ++v) {
+        const int col = (v * WAVES * kWave + thread) * kE;
+        Vector<T> z = load_vector(x, col, p.H);
+        if constexpr (NORM) {
+            if (residual) {
+                const Vector<T> y = load_vector(residual, col, p.H);
+#pragma unroll
+                for (int k = 0; k < kE; ++k) z.v[k] = narrow<T>(widen(z.v[k]) + widen(y.v[k]));
+            }
+            if (p.sum) store_vector(static_cast<T*>(p.sum) + static_cast<int64_t>(r) * p.H, col, p.H, z);
+        }
+        Vector<float> w[kE / 4];
+        if constexpr (NORM) {
+            if (p.weight) {
+#pragma unroll
+                for (int k = 0; k < kE / 4; ++k) w[k] = load_vector(p.weight, col + 4 * k, p.H);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kE; ++k) {
+            const float f = widen(z.v[k]);
+            if constexpr (NORM) squares += static_cast<double>(f) * static_cast<double>(f);
+            const float g = NORM && p.weight ? f * w[k / 4].v[k % 4] : f;
+            const uint32_t a = __float_as_uint(g) & 0x7fffffffu;
+            most = most > a ? most : a;
+            u[v * kE + k] = g;
+        }
+    }
+    most = wave_max(most);
+    if constexpr (NORM) squares = wave_sum(squares);
+    if constexpr (WAVES > 1) {
+        __shared__ uint32_t s_most[4];
+        __shared__ double s_squares[4];
+        if (lane == 0) {
+            s_most[wave] = most;
+            s_squares[wave] = squares;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < 4; ++w) most = most > s_most[w] ? most : s_most[w];
+        squares = s_squares[0] + s_squares[1] + s_squares[2] + s_squares[3];
+    }
+    // A row that is not finite: zeros, and a scale that says so.  Rows of tiny values are lifted, which is exact.
+    const bool finite = most < kInfinity;
+    const float lift = most < 0x20000000u ? 0x1p80f : 1.0f;
+    const float m = __uint_as_float(most), m_lifted = m * lift;
+    const float inverse = most && finite ? static_cast<float>(127.0 / static_cast<double>(m_lifted)) : 0.0f;
+    int8_t* q = p.q + static_cast<int64_t>(r) * p.pitch;
+#pragma unroll
+    for (int v = 0; v < kVectors; ++v) {
+        const int col = (v * WAVES * kWave + thread) * kE;
+        if (col >= p.pitch) break;
+        uint32_t word[kE / 4];
+#pragma unroll
+        for (int k = 0; k < kE; ++k) {
+            const int l = finite ? level(u[v * kE + k] * lift, m_lifted, inverse) : 0;
+            if (k % 4 == 0) word[k / 4] = 0;
+            word[k / 4] |= (static_cast<uint32_t>(l) & 0xffu) << (8 * (k % 4));
+        }
+        __builtin_memcpy(__builtin_assume_aligned(q + col, kE), word, kE);
+    }
+    if (thread == 0) {
+        double scale = static_cast<double>(m) / 127.0;
+        if constexpr (NORM) scale /= sqrt(squares / p.H + static_cast<double>(p.eps));
+        p.scales[r] = !finite ? __uint_as_float(0x7fc00000u) : most ? static_cast<float>(scale) : 0.0f;
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void ctc_rows_from_8_bits_kernel(const int8_t* __restrict__ q, const float* __restrict__ scales,
+                                                                   const int32_t* __restrict__ frames, int rows, int H, int pitch,
+                                                                   T* __restrict__ out)
+{
+    constexpr int kE = Vector<T>::kElements;
+    const int lane = threadIdx.x % kWave, i = blockIdx.x * 4 + threadIdx.x / kWave;
+    if (i >= listed(frames, rows)) return;
+    const int r = row_of(frames, rows, i);
+    if (r < 0) return;
+    const float scale = scales[r];
+    const int8_t* from = q + static_cast<int64_t>(r) * pitch;
+    T* to = out + static_cast<int64_t>(r) * H;
+    for (int col = lane * kE; col < H; col += kWave * kE) {
+        int8_t b[kE];
+        __builtin_memcpy(b, __builtin_assume_aligned(from + col, kE), kE);
+        Vector<T> v;
+#pragma unroll
+        for (int k = 0; k < kE; ++k) v.v[k] = narrow<T>(static_cast<float>(b[k]) * scale);
+        store_vector(to, col, H, v);
+    }
+}
+
+// ---- the norm's backward pass -----------------------------------------------------------------------------------
+
+struct NormBackArgs {
+    const void* dy;
+    const void* sum;
+    const float* weight;
+    float eps;
+    const void* dresidual;
+    const int32_t* frames;
+    int rows, H;
+    void* dsum;
+    float* partials;             // [groups, H], or null
+};
+
+// A row to a wavefront (four rows to a workgroup) or to all wavefronts of a workgroup; workgroups take rows in turn and
+// keep the sum over theirs of what each of their columns adds to dweight.
+template <typename T, int WAVES, int E>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void ctc_norm_backward_kernel(NormBackArgs p)
+{
+    constexpr int kE = Vector<T>::kElements, kVectors = E / kE, kWidth = WAVES * kWave, kRows = WAVES == 1 ? 4 : 1;
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int thread = WAVES == 1 ? lane : threadIdx.x;
+    const int n = listed(p.frames, p.rows);
+    float w[E], dw[E];
+#pragma unroll
+    for (int v = 0; v < kVectors; ++v)
+#pragma unroll
+        for (int k = 0; k < kE; k += 4) {
+            const int col = (v * kWidth + thread) * kE + k;
+            Vector<float> four = {{1.0f, 1.0f, 1.0f, 1.0f}};
+            if (p.weight) four = load_vector(p.weight, col, p.H);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[v * kE + k + j] = four.v[j];
+        }
+#pragma unroll
+    for (int k = 0; k < E; ++k) dw[k] = 0.0f;
+    int turn = 0;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kRows + (WAVES == 1 ? wave : 0); i < n;
+         i += static_cast<int64_t>(gridDim.x) * kRows) {
+        const int r = row_of(p.frames, p.rows, static_cast<int>(i));
+        if (r < 0) continue;
+        const int64_t row = static_cast<int64_t>(r) * p.H;
+        Vector<T> z[kVectors], dy[kVectors], d[kVectors];
+#pragma unroll
+        for (int v = 0; v < kVectors; ++v) {
+            const int col = (v * kWidth + thread) * kE;
+            z[v] = load_vector(static_cast<const T*>(p.sum) + row, col, p.H);
+            dy[v] = load_vector(static_cast<const T*>(p.dy) + row, col, p.H);
+            d[v] = Vector<T>{};
+            if (p.dresidual) d[v] = load_vector(static_cast<const T*>(p.dresidual) + row, col, p.H);
+        }
+        double squares = 0.0, along = 0.0;
+#pragma unroll
+        for (int v = 0; v < kVectors; ++v)
+#pragma unroll
+            for (int k = 0; k < kE; ++k) {
+                const double f = static_cast<double>(widen(z[v].v[k]));
+                squares += f * f;
+                along += static_cast<double>(widen(dy[v].v[k]) * w[v * kE + k]) * f;
+            }
+        squares = wave_sum(squares);
+        along = wave_sum(along);
+        if constexpr (WAVES > 1) {
+            // (two buffers by turns: who writes one again has passed the barrier that its readers of two turns ago came to)
+            __shared__ double s_sums[2][2][WAVES];
+            if (lane == 0) {
+                s_sums[turn][0][wave] = squares;
+                s_sums[turn][1][wave] = along;
+            }
+            __syncthreads();
+            squares = along = 0.0;
+#pragma unroll
+            for (int o = 0; o < WAVES; ++o) {
+                squares += s_sums[turn][0][o];
+                along += s_sums[turn][1][o];
+            }
+            turn ^= 1;
+        }
+        const double variance = squares / p.H + static_cast<double>(p.eps);
+        const double factor = 1.0 / sqrt(variance);
+        const float f = static_cast<float>(factor), c = static_cast<float>(along / p.H / variance * factor);
+#pragma unroll
+        for (int v = 0; v < kVectors; ++v) {
+#pragma unroll
+            for (int k = 0; k < kE; ++k) {
+                const float g = widen(dy[v].v[k]), zk = widen(z[v].v[k]);
+                dw[v * kE + k] += g * (zk * f);
+                d[v].v[k] = narrow<T>((g * w[v * kE + k]) * f - zk * c + widen(d[v].v[k]));
+            }
+            store_vector(static_cast<T*>(p.dsum) + row, (v * kWidth + thread) * kE, p.H, d[v]);
+        }
+    }
+    if (!p.partials) return;
+    if constexpr (WAVES == 1) {
+        // The four wavefronts' sums, one after another.
+        __shared__ float s_dw[E][kWave];
+        for (int o = 0; o < 4; ++o) {
+            if (wave == o) {
+#pragma unroll
+                for (int k = 0; k < E; ++k) {
+                    if (o) dw[k] += s_dw[k][lane];
+                    s_dw[k][lane] = dw[k];
+                }
+            }
+            __syncthreads();
+        }
+        if (wave != 3) return;
+    }
+    float* out = p.partials + static_cast<int64_t>(blockIdx.x) * p.H;
+#pragma unroll
+    for (int v = 0; v < kVectors; ++v)
+#pragma unroll
+        for (int k = 0; k < kE; k += 4) {
+            Vector<float> four;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) four.v[j] = dw[v * kE + k + j];
+            store_vector(out, (v * kWidth + thread) * kE + k, p.H, four);
+        }
+}
+
+// out[k] = sum over p of partials[p * stride + k], in fp64; 16 lanes of rows and 64 columns to a workgroup of 1024.
+__global__ __launch_bounds__(1024) void ctc_sum_partials_kernel(const float* __restrict__ partials, int count, int64_t stride,
+                                                                int64_t width, float* __restrict__ out)
+{
+    __shared__ double s_sum[16][kWave];
+    const int lane = threadIdx.x % kWave, group = threadIdx.x / kWave;
+    const int64_t col = static_cast<int64_t>(blockIdx.x) * kWave + lane;
+    double sum = 0.0;
+    if (col < width)
+        for (int p = group; p < count; p += 16) sum += static_cast<double>(partials[p * stride + col]);
+    s_sum[group][lane] = sum;
+    __syncthreads();
+    if (group == 0 && col < width) {
+#pragma unroll
+        for (int g = 1; g < 16; ++g) sum += s_sum[g][lane];
+        out[col] = static_cast<float>(sum);
+    }
+}
+
+// ---- activations ------------------------------------------------------------------------------------------------
+
+typedef int int4v __attribute__((ext_vector_type(4)));
+
+struct LinearArgs {
+    const int8_t* q;
+    const float* scales;
+    const int8_t* weight_q;
+    const float* weight_scales;
+    const float* bias;
+    const int32_t* frames;
+    int rows, A, pitch;
+    void* logits;
+};
+
+// 16 rows and 64 symbols to a wavefront, straight from memory.  v_mfma_i32_16x16x64_i8: lane l gives bytes
+// 16 (l / 16) .. of row l % 16 of either operand, and holds rows 4 (l / 16) .. + 3 of column l % 16 of the result.
+template <typename T>
+__global__ __launch_bounds__(256) void ctc_linear_kernel(LinearArgs p)
+{
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int n = listed(p.frames, p.rows);
+    const int64_t m0 = static_cast<int64_t>(blockIdx.x) * 64 + wave * 16;
+    if (m0 >= n) return;
+    const int mine = m0 + lane % 16 < n ? row_of(p.frames, p.rows, static_cast<int>(m0) + lane % 16) : -1;
+    const int a0 = blockIdx.y * 64;
+    int4v sum[4] = {};
+    for (int k = lane / 16 * 16; k < p.pitch; k += 64) {
+        int4v rows = {}, columns;
+        if (mine >= 0) rows = *reinterpret_cast<const int4v*>(p.q + static_cast<int64_t>(mine) * p.pitch + k);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const int a = a0 + c * 16 + lane % 16;
+            columns = int4v{};
+            if (a < p.A) columns = *reinterpret_cast<const int4v*>(p.weight_q + static_cast<int64_t>(a) * p.pitch + k);
+            sum[c] = __builtin_amdgcn_mfma_i32_16x16x64_i8(rows, columns, sum[c], 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = __shfl(mine, lane / 16 * 4 + i, kWave);
+        if (r < 0) continue;
+        const float scale = p.scales[r];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const int a = a0 + c * 16 + lane % 16;
+            if (a >= p.A) continue;
+            const float v = static_cast<float>(sum[c][i]) * (scale * p.weight_scales[a]) + (p.bias ? p.bias[a] : 0.0f);
+            static_cast<T*>(p.logits)[static_cast<int64_t>(r) * p.A + a] = narrow<T>(v);
+        }
+    }
+}
+
+// ---- gradient of the weights ------------------------------------------------------------------------------------
+
+struct GradientArgs {
+    const void* grads;
+    const int8_t* q;
+    const float* scales;
+    const int32_t* frames;
+    int rows, H, A, pitch, slabs;
+    float* partials;             // [slabs, A * H + A]
+};
+
+// 64 symbols by 64 columns to a workgroup, 4 by 4 to a thread; 16 rows at a time in LDS.
+template <typename T>
+__global__ __launch_bounds__(256) void ctc_weight_gradient_kernel(GradientArgs p)
+{
+    __shared__ float s_g[16][65], s_q[16][65], s_plain[16][65];
+    const int n = listed(p.frames, p.rows);
+    const int per = (n + p.slabs - 1) / p.slabs;
+    const int a0 = blockIdx.x * 64, k0 = blockIdx.y * 64, slab = blockIdx.z;
+    const int64_t first = static_cast<int64_t>(slab) * per;
+    const int last = static_cast<int>(first + per < n ? first + per : n);
+    const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
+    float sum[4][4] = {}, bias[4] = {};
+    for (int64_t i0 = first; i0 < last; i0 += 16) {
+        __syncthreads();
+        for (int e = threadIdx.x; e < 16 * 64; e += 256) {
+            const int i = e / 64, c = e % 64;
+            const int r = i0 + i < last ? row_of(p.frames, p.rows, static_cast<int>(i0) + i) : -1;
+            float g = 0.0f, v = 0.0f, scale = 0.0f;
+            if (r >= 0) {
+                scale = p.scales[r];
+                if (a0 + c < p.A) g = widen(static_cast<const T*>(p.grads)[static_cast<int64_t>(r) * p.A + a0 + c]);
+                if (k0 + c < p.H) v = static_cast<float>(p.q[static_cast<int64_t>(r) * p.pitch + k0 + c]);
+            }
+            s_plain[i][c] = g;
+            s_g[i][c] = r >= 0 ? g * scale : 0.0f;
+            s_q[i][c] = v;
+        }
+        __syncthreads();
+        for (int i = 0; i < 16; ++i) {
+#pragma unroll
+            for (int a = 0; a < 4; ++a) {
+                bias[a] += s_plain[i][ty * 4 + a];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) sum[a][k] += s_g[i][ty * 4 + a] * s_q[i][tx * 4 + k];
+            }
+        }
+    }
+    float* out = p.partials + static_cast<int64_t>(slab) * p.A * (p.H + 1);
+#pragma unroll
+    for (int a = 0; a < 4; ++a) {
+        if (a0 + ty * 4 + a >= p.A) continue;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (k0 + tx * 4 + k < p.H) out[static_cast<int64_t>(a0 + ty * 4 + a) * p.H + k0 + tx * 4 + k] = sum[a][k];
+        if (blockIdx.y == 0 && tx == 0) out[static_cast<int64_t>(p.A) * p.H + a0 + ty * 4 + a] = bias[a];
+    }
+}
+
+int last_error() { return static_cast<int>(hipGetLastError()); }
+
+unsigned blocks(int64_t items, int per_block) { return static_cast<unsigned>((items + per_block - 1) / per_block); }
+
+template <typename T, bool NORM> void launch_to_8_bits(const NormArgs& p, hipStream_t s)
+{
+    const dim3 block(256), wide(static_cast<unsigned>(p.rows)), narrow_rows(blocks(p.rows, 4));
+    if (p.pitch <= 512)
+        hipLaunchKernelGGL((ctc_rows_to_8_bits_kernel<T, 1, 8, NORM>), narrow_rows, block, 0, s, p);
+    else if (p.pitch <= 1024)
+        hipLaunchKernelGGL((ctc_rows_to_8_bits_kernel<T, 1, 16, NORM>), narrow_rows, block, 0, s, p);
+    else if (p.pitch <= 2048)
+        hipLaunchKernelGGL((ctc_rows_to_8_bits_kernel<T, 1, 32, NORM>), narrow_rows, block, 0, s, p);
+    else if (p.pitch <= 4096)
+        hipLaunchKernelGGL((ctc_rows_to_8_bits_kernel<T, 1, 64, NORM>), narrow_rows, block, 0, s, p);
+    else if (p.pitch <= 8192)
+        hipLaunchKernelGGL((ctc_rows_to_8_bits_kernel<T, 4, 32, NORM>), wide, block, 0, s, p);
+    else
+        hipLaunchKernelGGL((ctc_rows_to_8_bits_kernel<T, 4, 64, NORM>), wide, block, 0, s, p);
+}
+
+template <typename T> void launch_backward(const NormBackArgs& p, unsigned groups, hipStream_t s)
+{
+    const dim3 grid(groups);
+    if (p.H <= 512)
+        hipLaunchKernelGGL((ctc_norm_backward_kernel<T, 1, 8>), grid, dim3(256), 0, s, p);
+    else if (p.H <= 2048)
+        hipLaunchKernelGGL((ctc_norm_backward_kernel<T, 4, 8>), grid, dim3(256), 0, s, p);
+    else if (p.H <= 4096)
+        hipLaunchKernelGGL((ctc_norm_backward_kernel<T, 4, 16>), grid, dim3(256), 0, s, p);
+    else if (p.H <= 8192)
+        hipLaunchKernelGGL((ctc_norm_backward_kernel<T, 16, 8>), grid, dim3(1024), 0, s, p);
+    else
+        hipLaunchKernelGGL((ctc_norm_backward_kernel<T, 8, 32>), grid, dim3(512), 0, s, p);
+}
+
+}  // namespace
+
+int launch_pack_frames(const int32_t* lengths, int T, int B, int32_t* frames, void* stream)
+{
+    hipLaunchKernelGGL(ctc_pack_frames_kernel, dim3(blocks(T, 4)), dim3(256), 0, static_cast<hipStream_t>(stream), lengths, T, B,
+                       frames);
+    return last_error();
+}
+
+int launch_quantize(const void* x, const int32_t* frames, int rows, int H, bool bf16, int8_t* q, float* scales, void* stream)
+{
+    const NormArgs p = {x, nullptr, nullptr, 0.0f, frames, rows, H, pitch_of(H), nullptr, q, scales};
+    if (bf16)
+        launch_to_8_bits<bf16_t, false>(p, static_cast<hipStream_t>(stream));
+    else
+        launch_to_8_bits<float, false>(p, static_cast<hipStream_t>(stream));
+    return last_error();
+}
+
+int launch_norm(const void* x, const void* residual, const float* weight, float eps, const int32_t* frames, int rows, int H,
+                bool bf16, void* sum, int8_t* q, float* scales, void* stream)
+{
+    const NormArgs p = {x, residual, weight, eps, frames, rows, H, pitch_of(H), sum, q, scales};
+    if (bf16)
+        launch_to_8_bits<bf16_t, true>(p, static_cast<hipStream_t>(stream));
+    else
+        launch_to_8_bits<float, true>(p, static_cast<hipStream_t>(stream));
+    return last_error();
+}
+
+int launch_dequantize(const int8_t* q, const float* scales, const int32_t* frames, int rows, int H, bool bf16, void* out,
+                      void* stream)
+{
+    const dim3 grid(blocks(rows, 4)), block(256);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (bf16)
+        hipLaunchKernelGGL(ctc_rows_from_8_bits_kernel<bf16_t>, grid, block, 0, s, q, scales, frames, rows, H, pitch_of(H),
+                           static_cast<bf16_t*>(out));
+    else
+        hipLaunchKernelGGL(ctc_rows_from_8_bits_kernel<float>, grid, block, 0, s, q, scales, frames, rows, H, pitch_of(H),
+                           static_cast<float*>(out));
+    return last_error();
+}
+
+int launch_norm_backward(const void* dy, const void* sum, const float* weight, float eps, const void* dresidual,
+                         const int32_t* frames, int rows, int H, bool bf16, void* dsum, float* dweight, float* partials,
+                         void* stream)
+{
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const int groups = norm_partials(rows);
+    const NormBackArgs p = {dy, sum, weight, eps, dresidual, frames, rows, H, dsum, dweight ? partials : nullptr};
+    if (bf16)
+        launch_backward<bf16_t>(p, static_cast<unsigned>(groups), s);
+    else
+        launch_backward<float>(p, static_cast<unsigned>(groups), s);
+    const int err = last_error();
+    if (err || !dweight) return err;
+    hipLaunchKernelGGL(ctc_sum_partials_kernel, dim3(blocks(H, kWave)), dim3(1024), 0, s, partials, groups,
+                       static_cast<int64_t>(H), static_cast<int64_t>(H), dweight);
+    return last_error();
+}
+
+int launch_linear(const int8_t* q, const float* scales, const int8_t* weight_q, const float* weight_scales, const float* bias,
+                  const int32_t* frames, int rows, int H, int A, bool bf16, void* logits, void* stream)
+{
+    const LinearArgs p = {q, scales, weight_q, weight_scales, bias, frames, rows, A, pitch_of(H), logits};
+    const dim3 grid(blocks(rows, 64), blocks(A, 64)), block(256);
+    if (bf16)
+        hipLaunchKernelGGL(ctc_linear_kernel<bf16_t>, grid, block, 0, static_cast<hipStream_t>(stream), p);
+    else
+        hipLaunchKernelGGL(ctc_linear_kernel<float>, grid, block, 0, static_cast<hipStream_t>(stream), p);
+    return last_error();
+}
+
+int launch_weight_gradient(const void* grads, const int8_t* q, const float* scales, const int32_t* frames, int rows, int H,
+                           int A, bool bf16, float* dweight, float* dbias, float* partials, void* stream)
+{
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const int slabs = gradient_slabs(rows, H, A);
+    const GradientArgs p = {grads, q, scales, frames, rows, H, A, pitch_of(H), slabs, partials};
+    const dim3 grid(blocks(A, 64), blocks(H, 64), static_cast<unsigned>(slabs)), block(256);
+    if (bf16)
+        hipLaunchKernelGGL(ctc_weight_gradient_kernel<bf16_t>, grid, block, 0, s, p);
+    else
+        hipLaunchKernelGGL(ctc_weight_gradient_kernel<float>, grid, block, 0, s, p);
+    int err = last_error();
+    if (err) return err;
+    const int64_t weights = static_cast<int64_t>(A) * H, stride = weights + A;
+    hipLaunchKernelGGL(ctc_sum_partials_kernel, dim3(blocks(weights, kWave)), dim3(1024), 0, s, partials, slabs, stride, weights,
+                       dweight);
+    err = last_error();
+    if (err || !dbias) return err;
+    hipLaunchKernelGGL(ctc_sum_partials_kernel, dim3(blocks(A, kWave)), dim3(1024), 0, s, partials + weights, slabs, stride,
+                       static_cast<int64_t>(A), dbias);
+    return last_error();
+}
+
+}  // namespace layer
