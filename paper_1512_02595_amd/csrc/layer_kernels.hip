@@ -418,42 +418,240 @@ struct LinearArgs {
     void* logits;
 };
 
-// 16 rows and 64 symbols to a wavefront, straight from memory.  v_mfma_i32_16x16x64_i8: lane l gives bytes
-// 16 (l / 16) .. of row l % 16 of either operand, and holds rows 4 (l / 16) .. + 3 of column l % 16 of the result.
-template <typename T>
-__global__ __launch_bounds__(256) void ctc_linear_kernel(LinearArgs p)
+// What a sum becomes: the scales' product, the sum times it, the bias; then one rounding to T.
+template <typename T> __device__ __forceinline__ T activation(int sum, float scale, float weight_scale, float bias)
 {
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    return narrow<T>(fmaf(static_cast<float>(sum), scale * weight_scale, bias));
+}
+
+// Few rows or few symbols: 16 MB rows by 16 NB symbols to a workgroup, straight from memory into the matrix cores, each of the
+// four wavefronts with every fourth 128 bytes of the rows; their sums are added in LDS.  What is many then (the rows, or the weights)
+// is read once, with nothing between a wavefront's loads.
+// v_mfma_i32_16x16x64_i8: lane l gives bytes 16 (l / 16) .. of row l % 16 of either operand, and holds rows 4 (l / 16) .. + 3 of column
+// l % 16 of the result.
+template <typename T, int MB, int NB>
+__global__ __launch_bounds__(256) void ctc_linear_direct_kernel(LinearArgs p)
+{
+    __shared__ int4v s_sum[4][MB * NB][kWave];
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int n = listed(p.frames, p.rows);
-    const int64_t m0 = static_cast<int64_t>(blockIdx.x) * 64 + wave * 16;
+    const unsigned columns = static_cast<unsigned>((p.A + 16 * NB - 1) / (16 * NB));
+    const int64_t m0 = static_cast<int64_t>(blockIdx.x / columns) * (16 * MB);
+    const int a0 = static_cast<int>(blockIdx.x % columns) * (16 * NB);
     if (m0 >= n) return;
-    const int mine = m0 + lane % 16 < n ? row_of(p.frames, p.rows, static_cast<int>(m0) + lane % 16) : -1;
-    const int a0 = blockIdx.y * 64;
-    int4v sum[4] = {};
-    for (int k = lane / 16 * 16; k < p.pitch; k += 64) {
-        int4v rows = {}, columns;
-        if (mine >= 0) rows = *reinterpret_cast<const int4v*>(p.q + static_cast<int64_t>(mine) * p.pitch + k);
+    int mine[MB];
+    const int8_t* row[MB];
+    const int8_t* column[NB];
+    const int begin = wave * 128 + lane / 16 * 16;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            const int a = a0 + c * 16 + lane % 16;
-            columns = int4v{};
-            if (a < p.A) columns = *reinterpret_cast<const int4v*>(p.weight_q + static_cast<int64_t>(a) * p.pitch + k);
-            sum[c] = __builtin_amdgcn_mfma_i32_16x16x64_i8(rows, columns, sum[c], 0, 0, 0);
-        }
+    for (int b = 0; b < MB; ++b) {
+        const int64_t i = m0 + b * 16 + lane % 16;
+        mine[b] = i < n ? row_of(p.frames, p.rows, static_cast<int>(i)) : -1;
+        // (a row that does not count gives the first symbol's weights: any bytes will do)
+        row[b] = (mine[b] < 0 ? p.weight_q : p.q + static_cast<int64_t>(mine[b]) * p.pitch) + begin;
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = __shfl(mine, lane / 16 * 4 + i, kWave);
-        if (r < 0) continue;
-        const float scale = p.scales[r];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            const int a = a0 + c * 16 + lane % 16;
-            if (a >= p.A) continue;
-            const float v = static_cast<float>(sum[c][i]) * (scale * p.weight_scales[a]) + (p.bias ? p.bias[a] : 0.0f);
-            static_cast<T*>(p.logits)[static_cast<int64_t>(r) * p.A + a] = narrow<T>(v);
-        }
+    for (int b = 0; b < NB; ++b) {
+        const int a = a0 + b * 16 + lane % 16;
+        column[b] = p.weight_q + static_cast<int64_t>(a < p.A ? a : p.A - 1) * p.pitch + begin;
     }
+    int4v sum[MB][NB] = {};
+    for (int k0 = 0; k0 < p.pitch; k0 += 2048) {
+        int4v x[8][MB], w[8][NB];                       // all loads of 2048 bytes of the rows before the first product
+#pragma unroll
+        for (int h = 0; h < 8; ++h) {
+            const int k = k0 + h / 2 * 512 + h % 2 * 64;
+            const bool in = k + wave * 128 < p.pitch;
+#pragma unroll
+            for (int b = 0; b < MB; ++b) x[h][b] = in ? *reinterpret_cast<const int4v*>(row[b] + k) : int4v{};
+#pragma unroll
+            for (int b = 0; b < NB; ++b) w[h][b] = in ? *reinterpret_cast<const int4v*>(column[b] + k) : int4v{};
+        }
+#pragma unroll
+        for (int h = 0; h < 8; ++h)
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int j = 0; j < NB; ++j) sum[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[h][i], w[h][j], sum[i][j], 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) s_sum[wave][i * NB + j][lane] = sum[i][j];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const int block = i * NB + j;
+            if (block % 4 != wave) continue;
+            const int a = a0 + j * 16 + lane % 16;
+            const int4v total = s_sum[0][block][lane] + s_sum[1][block][lane] + s_sum[2][block][lane] + s_sum[3][block][lane];
+            const float weight_scale = a < p.A ? p.weight_scales[a] : 0.0f, bias = a < p.A && p.bias ? p.bias[a] : 0.0f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int r = __shfl(mine[i], lane / 16 * 4 + e, kWave);
+                if (r >= 0 && a < p.A)
+                    static_cast<T*>(p.logits)[static_cast<int64_t>(r) * p.A + a] = activation<T>(total[e], p.scales[r], weight_scale, bias);
+            }
+        }
+}
+
+typedef int int16v __attribute__((ext_vector_type(16)));
+
+// 16 bytes a lane from memory to LDS, lane after lane from `to` on.
+__device__ __forceinline__ void to_lds(const int8_t* from, int8_t* to)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                     (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+
+// Waits for everything this wavefront has asked of memory and LDS, then for the workgroup's others.
+__device__ __forceinline__ void wait_and_meet()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070);                 // vmcnt(0) lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// Many rows by many symbols: 64 WM rows by 64 WN symbols to a workgroup, 32 WM by 32 WN to each of its four wavefronts, 128 bytes of
+// every row at a time in LDS, in two buffers: while the matrix cores work on one, memory fills the other.  A wavefront holds the
+// operands of the next 32 bytes in registers while it multiplies these; the barrier comes before a buffer's last 32, whose
+// operands are in registers by then, so that the other buffer's first are fetched beside them.
+// LDS holds a row's 16-byte pieces in the order piece ^ (row / 2 % 8): eight lanes that read one piece of eight rows then
+// meet eight places of 16 bytes, all 64 banks' worth.
+// v_mfma_i32_32x32x32_i8: lane l gives bytes 16 (l / 32) .. of row l % 32 of either operand and holds rows
+// 8 (v / 4) + 4 (l / 32) + v % 4, v < 16, of column l % 32 of the result.
+template <typename T, int WM, int WN>
+__global__ __launch_bounds__(256) void ctc_linear_tiles_kernel(LinearArgs p)
+{
+    constexpr int kBM = 64 * WM, kBN = 64 * WN, kGroup = 8;
+    __shared__ __align__(1024) int8_t s_even[(kBM + kBN) * 128];
+    __shared__ __align__(1024) int8_t s_odd[(kBM + kBN) * 128];
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int n = listed(p.frames, p.rows);
+    // Workgroups go to the 8 dies in turn: each die takes a contiguous run of tiles, which go down kGroup tiles of rows before
+    // they go on to the next symbols, so that a die's workgroups share rows and weights in its cache.
+    const unsigned down = static_cast<unsigned>((n + kBM - 1) / kBM), across = static_cast<unsigned>((p.A + kBN - 1) / kBN);
+    const unsigned tiles = down * across, per_die = (tiles + 7) / 8;
+    if (blockIdx.x / 8 >= per_die) return;
+    const unsigned tile = blockIdx.x % 8 * per_die + blockIdx.x / 8;
+    if (tile >= tiles) return;
+    const unsigned group = tile / (kGroup * across), in_group = tile % (kGroup * across);
+    const unsigned high = down - group * kGroup < kGroup ? down - group * kGroup : kGroup;
+    const int m0 = static_cast<int>(group * kGroup + in_group % high) * kBM, a0 = static_cast<int>(in_group / high) * kBN;
+
+    const int8_t* from[2 * WM + 2 * WN];
+    const int piece = (lane % 8 ^ (wave % 2 * 4 + lane / 16)) * 16;
+#pragma unroll
+    for (int j = 0; j < 2 * WM; ++j) {
+        const int64_t i = static_cast<int64_t>(m0) + (j * 4 + wave) * 8 + lane / 8;
+        const int r = i < n ? row_of(p.frames, p.rows, static_cast<int>(i)) : -1;
+        from[j] = (r < 0 ? p.weight_q : p.q + static_cast<int64_t>(r) * p.pitch) + piece;    // (any bytes for a row that does not count)
+    }
+#pragma unroll
+    for (int j = 0; j < 2 * WN; ++j) {
+        const int a = a0 + (j * 4 + wave) * 8 + lane / 8;
+        from[2 * WM + j] = p.weight_q + static_cast<int64_t>(a < p.A ? a : p.A - 1) * p.pitch + piece;
+    }
+    const auto fill = [&](int8_t* buffer) {
+#pragma unroll
+        for (int j = 0; j < 2 * (WM + WN); ++j) {
+            to_lds(from[j], buffer + (j * 4 + wave) * 1024);
+            from[j] += 128;
+        }
+    };
+    const int at_row = (wave / 2 * 32 * WM + lane % 32) * 128, at_column = (kBM + wave % 2 * 32 * WN + lane % 32) * 128;
+    const int first_piece = lane / 32 ^ lane % 16 / 2;
+    int4v x[2][WM], w[2][WN];
+    const auto fetch = [&](const int8_t* buffer, int part, int into) {
+        const int at = (first_piece ^ part * 2) * 16;
+#pragma unroll
+        for (int i = 0; i < WM; ++i) x[into][i] = *reinterpret_cast<const int4v*>(buffer + at_row + i * 4096 + at);
+#pragma unroll
+        for (int i = 0; i < WN; ++i) w[into][i] = *reinterpret_cast<const int4v*>(buffer + at_column + i * 4096 + at);
+    };
+    int16v sum[WM][WN] = {};
+    const auto multiply = [&](int of) {
+#pragma unroll
+        for (int i = 0; i < WM; ++i)
+#pragma unroll
+            for (int j = 0; j < WN; ++j) sum[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[of][i], w[of][j], sum[i][j], 0, 0, 0);
+    };
+    const int steps = p.pitch / 128;
+    // A product, a read of LDS and so on; the products that are left hide the last reads (left alone the compiler puts the reads right
+    // before their use).
+    const auto interleave = [&]() {
+#pragma unroll
+        for (int i = 0; i < WM + WN; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, WM * WN - WM - WN, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // One buffer's products.  `full`: the other buffer's bytes, asked for a step ago, are waited for, and with the barrier every wavefront
+    // has what it needs of this one, which is filled again for the step after the next.
+    const auto step = [&](int8_t* now, const int8_t* next, int t, bool full) {
+        fetch(now, 1, 1);
+        multiply(0);
+        interleave();
+        fetch(now, 2, 0);
+        multiply(1);
+        interleave();
+        fetch(now, 3, 1);
+        multiply(0);
+        interleave();
+        if (full) {
+            wait_and_meet();
+            if (t + 2 < steps) fill(now);
+            fetch(next, 0, 0);
+        }
+        multiply(1);
+        if (full) interleave();
+    };
+    fill(s_even);
+    wait_and_meet();
+    if (steps > 1) fill(s_odd);
+    fetch(s_even, 0, 0);
+    int t = 0;
+    for (; t + 1 < steps; t += 2) {
+        step(s_even, s_odd, t, true);
+        step(s_odd, s_even, t + 1, true);               // (the last of an even number fetches what nobody multiplies)
+    }
+    if (t < steps) step(s_even, s_odd, t, false);
+    __syncthreads();
+    // The rows' numbers and scales, for those lanes that hold their results.
+    int* s_row = reinterpret_cast<int*>(s_even);
+    float* s_scale = reinterpret_cast<float*>(s_odd);
+    for (int i = threadIdx.x; i < kBM; i += 256) {
+        const int64_t at = static_cast<int64_t>(m0) + i;
+        const int r = at < n ? row_of(p.frames, p.rows, static_cast<int>(at)) : -1;
+        s_row[i] = r;
+        s_scale[i] = r < 0 ? 0.0f : p.scales[r];
+    }
+    __syncthreads();
+    float weight_scale[WN], bias[WN];
+    const int a = a0 + wave % 2 * 32 * WN + lane % 32;
+#pragma unroll
+    for (int j = 0; j < WN; ++j) {
+        weight_scale[j] = a + j * 32 < p.A ? p.weight_scales[a + j * 32] : 0.0f;
+        bias[j] = a + j * 32 < p.A && p.bias ? p.bias[a + j * 32] : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < WM; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const int in_tile = wave / 2 * 32 * WM + i * 32 + 8 * (v / 4) + 4 * (lane / 32) + v % 4;
+            const int r = s_row[in_tile];
+            if (r < 0) continue;
+            const float scale = s_scale[in_tile];
+            T* out = static_cast<T*>(p.logits) + static_cast<int64_t>(r) * p.A + a;
+#pragma unroll
+            for (int j = 0; j < WN; ++j)
+                if (a + j * 32 < p.A) out[j * 32] = activation<T>(sum[i][j][v], scale, weight_scale[j], bias[j]);
+        }
 }
 
 // ---- gradient of the weights ------------------------------------------------------------------------------------
@@ -551,6 +749,29 @@ template <typename T> void launch_backward(const NormBackArgs& p, unsigned group
         hipLaunchKernelGGL((ctc_norm_backward_kernel<T, 8, 32>), grid, dim3(512), 0, s, p);
 }
 
+template <typename T, int WM, int WN> void launch_tiles(const LinearArgs& p, hipStream_t s)
+{
+    const int64_t tiles = static_cast<int64_t>(blocks(p.rows, 64 * WM)) * blocks(p.A, 64 * WN);
+    hipLaunchKernelGGL((ctc_linear_tiles_kernel<T, WM, WN>), dim3(blocks(tiles, 8) * 8), dim3(256), 0, s, p);
+}
+template <typename T, int MB, int NB> void launch_direct(const LinearArgs& p, hipStream_t s)
+{
+    hipLaunchKernelGGL((ctc_linear_direct_kernel<T, MB, NB>), dim3(blocks(p.rows, 16 * MB) * blocks(p.A, 16 * NB)), dim3(256), 0, s, p);
+}
+template <typename T> void launch_product(const LinearArgs& p, hipStream_t s)
+{
+    const int64_t small = static_cast<int64_t>(blocks(p.rows, 128)) * blocks(p.A, 128);
+    const int64_t large = static_cast<int64_t>(blocks(p.rows, 256)) * blocks(p.A, 256);
+    if (p.rows <= 16)
+        launch_direct<T, 1, 1>(p, s);
+    else if (p.A <= 64 || small < 192)
+        launch_direct<T, 2, 2>(p, s);
+    else if (large < 512)
+        launch_tiles<T, 2, 2>(p, s);
+    else
+        launch_tiles<T, 4, 4>(p, s);
+}
+
 }  // namespace
 
 int launch_pack_frames(const int32_t* lengths, int T, int B, int32_t* frames, void* stream)
@@ -617,11 +838,10 @@ int launch_linear(const int8_t* q, const float* scales, const int8_t* weight_q, 
                   const int32_t* frames, int rows, int H, int A, bool bf16, void* logits, void* stream)
 {
     const LinearArgs p = {q, scales, weight_q, weight_scales, bias, frames, rows, A, pitch_of(H), logits};
-    const dim3 grid(blocks(rows, 64), blocks(A, 64)), block(256);
     if (bf16)
-        hipLaunchKernelGGL(ctc_linear_kernel<bf16_t>, grid, block, 0, static_cast<hipStream_t>(stream), p);
+        launch_product<bf16_t>(p, static_cast<hipStream_t>(stream));
     else
-        hipLaunchKernelGGL(ctc_linear_kernel<float>, grid, block, 0, static_cast<hipStream_t>(stream), p);
+        launch_product<float>(p, static_cast<hipStream_t>(stream));
     return last_error();
 }
 
