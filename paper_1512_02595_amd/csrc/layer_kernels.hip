@@ -506,29 +506,31 @@ __device__ __forceinline__ void to_lds(const int8_t* from, int8_t* to)
                                      (__attribute__((address_space(3))) void*)to, 16, 0, 0);
 }
 
-// Waits for everything this wavefront has asked of memory and LDS, then for the workgroup's others.
-__device__ __forceinline__ void wait_and_meet()
+// Waits until at most N of this wavefront's requests to memory are under way and none to LDS, then for the workgroup's others.
+template <int N> __device__ __forceinline__ void wait_and_meet()
 {
+    static_assert(N < 64);
     asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0x0070);                 // vmcnt(0) lgkmcnt(0)
+    __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | (N >> 4) << 14);
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
 
-// Many rows by many symbols: 64 WM rows by 64 WN symbols to a workgroup, 32 WM by 32 WN to each of its four wavefronts, 128 bytes of
-// every row at a time in LDS, in two buffers: while the matrix cores work on one, memory fills the other.  A wavefront holds the
-// operands of the next 32 bytes in registers while it multiplies these; the barrier comes before a buffer's last 32, whose
-// operands are in registers by then, so that the other buffer's first are fetched beside them.
-// LDS holds a row's 16-byte pieces in the order piece ^ (row / 2 % 8): eight lanes that read one piece of eight rows then
-// meet eight places of 16 bytes, all 64 banks' worth.
+// Many rows by many symbols: 64 WM rows by 64 WN symbols to a workgroup, 32 WM by 32 WN to each of its four wavefronts, 64 bytes of
+// every row at a time in LDS, in kStages buffers: while the matrix cores work on one, memory fills the others.  A wavefront
+// holds the operands of the next 32 bytes in registers while it multiplies these; the barrier comes before a buffer's last 32, whose
+// operands are in registers by then, so that the next buffer's first are fetched beside them.
+// LDS holds a row's four 16-byte pieces in the order piece ^ (row / 4 % 4): eight lanes that read one piece of eight rows then
+// meet eight places of 16 bytes, a different one each modulo the banks.
 // v_mfma_i32_32x32x32_i8: lane l gives bytes 16 (l / 32) .. of row l % 32 of either operand and holds rows
-// 8 (v / 4) + 4 (l / 32) + v % 4, v < 16, of column l % 32 of the result.
+// 8 (v / 4) + 4 (l / 32) + v % 4, v < 16, of column l % 32 of the result; with the weights first those are symbols, and the lane's
+// column is a row of the states.  The sums go through LDS once more, 32 rows at a time, so that rows of activations are written in
+// vectors.
 template <typename T, int WM, int WN>
 __global__ __launch_bounds__(256) void ctc_linear_tiles_kernel(LinearArgs p)
 {
-    constexpr int kBM = 64 * WM, kBN = 64 * WN, kGroup = 8;
-    __shared__ __align__(1024) int8_t s_even[(kBM + kBN) * 128];
-    __shared__ __align__(1024) int8_t s_odd[(kBM + kBN) * 128];
+    constexpr int kBM = 64 * WM, kBN = 64 * WN, kGroup = 8, kStages = 4, kLoads = WM + WN, kBytes = (kBM + kBN) * 64;
+    __shared__ __align__(1024) int8_t s_buffer[kStages][kBytes];
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int n = listed(p.frames, p.rows);
     // Workgroups go to the 8 dies in turn: each die takes a contiguous run of tiles, which go down kGroup tiles of rows before
@@ -542,44 +544,54 @@ __global__ __launch_bounds__(256) void ctc_linear_tiles_kernel(LinearArgs p)
     const unsigned high = down - group * kGroup < kGroup ? down - group * kGroup : kGroup;
     const int m0 = static_cast<int>(group * kGroup + in_group % high) * kBM, a0 = static_cast<int>(in_group / high) * kBN;
 
-    const int8_t* from[2 * WM + 2 * WN];
-    const int piece = (lane % 8 ^ (wave % 2 * 4 + lane / 16)) * 16;
+    // Thread i will say where the tile's row i begins among the activations (-1: it does not count), and its scale.
+    struct Row { int64_t at; float scale; };
+    Row mine = {-1, 0.0f};
+    if (threadIdx.x < kBM && static_cast<int64_t>(m0) + threadIdx.x < n) {
+        const int r = row_of(p.frames, p.rows, m0 + static_cast<int>(threadIdx.x));
+        if (r >= 0) mine = {static_cast<int64_t>(r) * p.A, p.scales[r]};
+    }
+    const int8_t* from[kLoads];
+    const int piece = (lane % 4 ^ lane / 16) * 16;
 #pragma unroll
-    for (int j = 0; j < 2 * WM; ++j) {
-        const int64_t i = static_cast<int64_t>(m0) + (j * 4 + wave) * 8 + lane / 8;
+    for (int j = 0; j < WM; ++j) {
+        const int64_t i = static_cast<int64_t>(m0) + (j * 4 + wave) * 16 + lane / 4;
         const int r = i < n ? row_of(p.frames, p.rows, static_cast<int>(i)) : -1;
         from[j] = (r < 0 ? p.weight_q : p.q + static_cast<int64_t>(r) * p.pitch) + piece;    // (any bytes for a row that does not count)
     }
 #pragma unroll
-    for (int j = 0; j < 2 * WN; ++j) {
-        const int a = a0 + (j * 4 + wave) * 8 + lane / 8;
-        from[2 * WM + j] = p.weight_q + static_cast<int64_t>(a < p.A ? a : p.A - 1) * p.pitch + piece;
+    for (int j = 0; j < WN; ++j) {
+        const int a = a0 + (j * 4 + wave) * 16 + lane / 4;
+        from[WM + j] = p.weight_q + static_cast<int64_t>(a < p.A ? a : p.A - 1) * p.pitch + piece;
     }
-    const auto fill = [&](int8_t* buffer) {
+    // The bytes of step t; behind the last one those of the last again, which nobody reads, so that the number of requests under
+    // way is the same in every step.
+    const int steps = p.pitch / 64;
+    const auto fill = [&](int8_t* buffer, int t) {
+        const int on = t + 1 < steps ? 64 : 0;
 #pragma unroll
-        for (int j = 0; j < 2 * (WM + WN); ++j) {
+        for (int j = 0; j < kLoads; ++j) {
             to_lds(from[j], buffer + (j * 4 + wave) * 1024);
-            from[j] += 128;
+            from[j] += on;
         }
     };
-    const int at_row = (wave / 2 * 32 * WM + lane % 32) * 128, at_column = (kBM + wave % 2 * 32 * WN + lane % 32) * 128;
-    const int first_piece = lane / 32 ^ lane % 16 / 2;
+    const int at_row = (wave / 2 * 32 * WM + lane % 32) * 64, at_column = (kBM + wave % 2 * 32 * WN + lane % 32) * 64;
+    const int first_piece = lane / 32 ^ lane / 4 % 4;
     int4v x[2][WM], w[2][WN];
-    const auto fetch = [&](const int8_t* buffer, int part, int into) {
-        const int at = (first_piece ^ part * 2) * 16;
+    const auto fetch = [&](const int8_t* buffer, int half) {
+        const int at = (first_piece ^ half * 2) * 16;
 #pragma unroll
-        for (int i = 0; i < WM; ++i) x[into][i] = *reinterpret_cast<const int4v*>(buffer + at_row + i * 4096 + at);
+        for (int i = 0; i < WM; ++i) x[half][i] = *reinterpret_cast<const int4v*>(buffer + at_row + i * 2048 + at);
 #pragma unroll
-        for (int i = 0; i < WN; ++i) w[into][i] = *reinterpret_cast<const int4v*>(buffer + at_column + i * 4096 + at);
+        for (int i = 0; i < WN; ++i) w[half][i] = *reinterpret_cast<const int4v*>(buffer + at_column + i * 2048 + at);
     };
     int16v sum[WM][WN] = {};
-    const auto multiply = [&](int of) {
+    const auto multiply = [&](int half) {
 #pragma unroll
         for (int i = 0; i < WM; ++i)
 #pragma unroll
-            for (int j = 0; j < WN; ++j) sum[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[of][i], w[of][j], sum[i][j], 0, 0, 0);
+            for (int j = 0; j < WN; ++j) sum[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[half][j], x[half][i], sum[i][j], 0, 0, 0);
     };
-    const int steps = p.pitch / 128;
     // A product, a read of LDS and so on; the products that are left hide the last reads (left alone the compiler puts the reads right
     // before their use).
     const auto interleave = [&]() {
@@ -591,67 +603,90 @@ __global__ __launch_bounds__(256) void ctc_linear_tiles_kernel(LinearArgs p)
         __builtin_amdgcn_sched_group_barrier(0x008, WM * WN - WM - WN, 0);
         __builtin_amdgcn_sched_barrier(0);
     };
-    // One buffer's products.  `full`: the other buffer's bytes, asked for a step ago, are waited for, and with the barrier every wavefront
-    // has what it needs of this one, which is filled again for the step after the next.
-    const auto step = [&](int8_t* now, const int8_t* next, int t, bool full) {
-        fetch(now, 1, 1);
+    // One buffer's products.  The next one's bytes were asked for kStages - 1 steps ago; behind the barrier every wavefront has what
+    // it needs of this one, which is filled again.
+    const auto step = [&](int stage, int t) {
+        int8_t* const now = s_buffer[stage];
+        fetch(now, 1);
         multiply(0);
         interleave();
-        fetch(now, 2, 0);
+        wait_and_meet<(kStages - 2) * kLoads>();
+        fill(now, t + kStages);
+        fetch(s_buffer[(stage + 1) % kStages], 0);      // (behind the last step what nobody multiplies)
         multiply(1);
         interleave();
-        fetch(now, 3, 1);
-        multiply(0);
-        interleave();
-        if (full) {
-            wait_and_meet();
-            if (t + 2 < steps) fill(now);
-            fetch(next, 0, 0);
-        }
-        multiply(1);
-        if (full) interleave();
     };
-    fill(s_even);
-    wait_and_meet();
-    if (steps > 1) fill(s_odd);
-    fetch(s_even, 0, 0);
-    int t = 0;
-    for (; t + 1 < steps; t += 2) {
-        step(s_even, s_odd, t, true);
-        step(s_odd, s_even, t + 1, true);               // (the last of an even number fetches what nobody multiplies)
+#pragma unroll
+    for (int t = 0; t < kStages; ++t) fill(s_buffer[t], t);
+    wait_and_meet<(kStages - 1) * kLoads>();
+    fetch(s_buffer[0], 0);
+    int t = 0;                                          // (the number of steps is even)
+    for (; t + 3 < steps; t += 4) {
+        step(0, t);
+        step(1, t + 1);
+        step(2, t + 2);
+        step(3, t + 3);
     }
-    if (t < steps) step(s_even, s_odd, t, false);
-    __syncthreads();
-    // The rows' numbers and scales, for those lanes that hold their results.
-    int* s_row = reinterpret_cast<int*>(s_even);
-    float* s_scale = reinterpret_cast<float*>(s_odd);
-    for (int i = threadIdx.x; i < kBM; i += 256) {
-        const int64_t at = static_cast<int64_t>(m0) + i;
-        const int r = at < n ? row_of(p.frames, p.rows, static_cast<int>(at)) : -1;
-        s_row[i] = r;
-        s_scale[i] = r < 0 ? 0.0f : p.scales[r];
+    if (t < steps) {
+        step(0, t);
+        step(1, t + 1);
     }
-    __syncthreads();
-    float weight_scale[WN], bias[WN];
-    const int a = a0 + wave % 2 * 32 * WN + lane % 32;
+    // (From here on memory is asked for nothing but to write: a wait for a load behind the writes would wait for them too.)
+    constexpr int kAcross = 8 * WN, kDown = kWave / kAcross, kLine = 32 * WN + 4;       // lanes to a row, rows at once, ints from row to row
+    const int a = a0 + wave % 2 * 32 * WN + lane % kAcross * 4;
+    float weight_scale[4], bias[4];
 #pragma unroll
-    for (int j = 0; j < WN; ++j) {
-        weight_scale[j] = a + j * 32 < p.A ? p.weight_scales[a + j * 32] : 0.0f;
-        bias[j] = a + j * 32 < p.A && p.bias ? p.bias[a + j * 32] : 0.0f;
+    for (int k = 0; k < 4; ++k) {
+        const int b = a + k < p.A ? a + k : p.A - 1;
+        weight_scale[k] = p.weight_scales[b];
+        bias[k] = p.bias ? p.bias[b] : 0.0f;
     }
+    wait_and_meet<0>();
+    static_assert(kBM <= 256 && kBM * sizeof(Row) + 4 * 32 * kLine * 4 <= kStages * kBytes);
+    Row* const s_row = reinterpret_cast<Row*>(&s_buffer[0][0]);
+    int* const s_sum = reinterpret_cast<int*>(s_row + kBM) + wave * 32 * kLine;
+    if (threadIdx.x < kBM) s_row[threadIdx.x] = mine;
+    wait_and_meet<0>();
+    T* const logits = static_cast<T*>(p.logits) + a;
 #pragma unroll
-    for (int i = 0; i < WM; ++i)
+    for (int i = 0; i < WM; ++i) {
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-            const int in_tile = wave / 2 * 32 * WM + i * 32 + 8 * (v / 4) + 4 * (lane / 32) + v % 4;
-            const int r = s_row[in_tile];
-            if (r < 0) continue;
-            const float scale = s_scale[in_tile];
-            T* out = static_cast<T*>(p.logits) + static_cast<int64_t>(r) * p.A + a;
+        for (int j = 0; j < WN; ++j)
 #pragma unroll
-            for (int j = 0; j < WN; ++j)
-                if (a + j * 32 < p.A) out[j * 32] = activation<T>(sum[i][j][v], scale, weight_scale[j], bias[j]);
-        }
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<int4v*>(s_sum + lane % 32 * kLine + j * 32 + g * 8 + lane / 32 * 4) =
+                    int4v{sum[i][j][g * 4], sum[i][j][g * 4 + 1], sum[i][j][g * 4 + 2], sum[i][j][g * 4 + 3]};
+        const auto write = [&](auto whole) {
+#pragma unroll
+            for (int b0 = 0; b0 < 32 / kDown; b0 += 4) {
+                int4v four[4];
+                Row row[4];
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const int at = (b0 + b) * kDown + lane / kAcross;
+                    four[b] = *reinterpret_cast<const int4v*>(s_sum + at * kLine + lane % kAcross * 4);
+                    row[b] = s_row[(wave / 2 * WM + i) * 32 + at];
+                }
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    T value[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) value[k] = activation<T>(four[b][k], row[b].scale, weight_scale[k], bias[k]);
+                    if (decltype(whole)::value) {
+                        if (row[b].at >= 0) __builtin_memcpy(logits + row[b].at, value, sizeof(value));
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            if (row[b].at >= 0 && a + k < p.A) logits[row[b].at + k] = value[k];
+                    }
+                }
+            }
+        };
+        if (a0 + kBN <= p.A)
+            write(std::true_type{});
+        else
+            write(std::false_type{});
+    }
 }
 
 // ---- gradient of the weights ------------------------------------------------------------------------------------

@@ -378,6 +378,20 @@ def test_linear(rows, H, A, dtype, kind):
     check_linear(out, q, s, wq, ws, bias, dtype, names)
 
 
+@pytest.mark.parametrize("kind", ["all", "some", "odd entries"])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows, H, A", [(5700, 300, 5801), (6000, 128, 5700), (5900, 513, 5640), (9000, 200, 900)])
+def test_linear_of_many_tiles(rows, H, A, dtype, kind):
+    say("many tiles", rows, H, A, dtype, kind)
+    rng = np.random.default_rng(rows + H)
+    q, s = levels(rng, rows, H)
+    wq, ws = levels(rng, A, H)
+    bias = torch.from_numpy(rng.standard_normal(A)).float()
+    frames, names = frame_list(kind, rows, rng)
+    out = linear(q, s, wq, ws, bias, dtype, frames)
+    check_linear(out, q, s, wq, ws, bias, dtype, names)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_linear_without_bias_at_its_extremes(dtype):
     """Every product 127 * 127: sums of 16384 of them are exact."""
