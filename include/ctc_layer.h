@@ -28,8 +28,8 @@
  *
  * Frames.  `frames` (device) [1 + rows] int32 or NULL: the rows that count.  frames[0] is their
  * number n (taken as 0 below 0 and as `rows` above), frames[1..n] their indices, in any order;
- * entries outside [0, rows) are skipped.  Rows that are not listed are neither read nor written:
- * what they hold stays.  Row-wise outputs of a row that is listed twice are those of one
+ * entries outside [0, rows) are skipped.  Rows that are not listed take no part: what they hold is of
+ * no consequence, and stays.  Row-wise outputs of a row that is listed twice are those of one
  * listing, provided that no output is one of the call's inputs; sums over rows count it twice.
  * NULL: all rows.  The grids are sized by `rows`, so that n may change from replay to replay.
  *
@@ -153,9 +153,9 @@ ctc_status_t ctc_linear_i8(const int8_t *q, const float *scales, const int8_t *w
  *     dweight[a][k] = sum over the listed rows of  grads[r][a] * scales[r] * q[r][k]
  *     dbias[a]      = sum over the listed rows of  grads[r][a]
  *
- * grads[r][a] * scales[r] is rounded to fp32; it enters the matrix cores whole, in three bf16 parts;
- * sums are in fp32, in an order that is fixed by the sizes alone.
- * An infinity or a NaN among what is summed gives a NaN.
+ * grads[r][a] * scales[r] is rounded to fp32 and enters the matrix cores in parts of 16 bits that hold it to
+ * within 2^-23 of itself (alphabets of more than 64 symbols: or 2^-38 of its symbol's largest, if that is
+ * more); sums are in fp32, in an order that the sizes and the list fix.  An infinity or a NaN among what is summed gives a NaN.
  *
  *   grads      (device) [rows, A] of type dtype, as ctc_loss_and_grad writes them
  *   q, scales  (device) as ctc_rms_norm_i8 or ctc_quantize_rows wrote them

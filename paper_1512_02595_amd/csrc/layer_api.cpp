@@ -60,10 +60,7 @@ size_t list_bytes(int rows) { return (static_cast<size_t>(rows) + 1) * 4; }
 size_t round_up(size_t v) { return (v + 255) / 256 * 256; }
 
 size_t norm_workspace(int rows, int H) { return round_up(static_cast<size_t>(norm_partials(rows)) * H * 4); }
-size_t gradient_workspace(int rows, int H, int A)
-{
-    return round_up(static_cast<size_t>(gradient_slabs(rows, H, A)) * A * (static_cast<size_t>(H) + 1) * 4);
-}
+size_t gradient_workspace(int rows, int H, int A) { return round_up(gradient_plan(rows, H, A).bytes); }
 
 }  // namespace
 }  // namespace layer

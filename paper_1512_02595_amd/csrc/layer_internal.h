@@ -24,14 +24,41 @@ inline int norm_partials(int rows)
     return groups < 1024 ? groups : 1024;
 }
 
-// The weights' gradient: the listed rows are dealt out to so many slabs, each summed by workgroups of its own.
-inline int gradient_slabs(int rows, int H, int A)
+// The weights' gradient: symbols and columns in tiles, the listed rows dealt out to so many slabs, each summed by workgroups
+// of its own.
+constexpr int kColumnSlabs = 64;                // workgroups that look at one symbol's gradients first
+struct GradientPlan {
+    int symbols;                                // of a tile: 32, 64, 128 or 256
+    int slabs;
+    bool columns_first;                         // a launch that finds the columns' largest, before
+    int bias_slabs;
+    size_t bias_at, largest_at, bytes;          // places in the workspace, in floats; all of it, in bytes
+};
+inline GradientPlan gradient_plan(int rows, int H, int A)
 {
-    const long tiles = ((H + 63L) / 64) * ((A + 63L) / 64);
-    long slabs = (2048 + tiles - 1) / tiles;
-    const long most = (rows + 255L) / 256;
-    if (slabs > most) slabs = most;
-    return static_cast<int>(slabs < 1 ? 1 : slabs > 256 ? 256 : slabs);
+    GradientPlan p{};
+    p.symbols = A <= 32 ? 32 : A <= 64 ? 64 : A <= 128 ? 128 : 256;
+    const long tiles = ((A + p.symbols - 1L) / p.symbols) * ((H + 255L) / 256);
+    const long steps = (rows + 31L) / 32;
+    // Time in steps of 32 rows: as many rounds of workgroups as the 256 compute units take (three workgroups each where tiles are narrow), each of its
+    // share of the steps and a few to begin and end with; and every slab's sums are written and read once more.
+    const long at_once = p.symbols <= 64 ? 768 : 256;
+    const double slab_cost = 8.0 * A * H / 5.0e6 / (p.symbols <= 64 ? 0.2 : p.symbols == 128 ? 0.5 : 0.9);
+    double best = 0.0;
+    for (long s = 1; s <= 256 && s <= (steps + 3) / 4; ++s) {
+        const long rounds = (tiles * s + at_once - 1) / at_once;
+        const double cost = static_cast<double>(rounds) * (static_cast<double>((steps + s - 1) / s) + 6.0) + (s > 1 ? s * slab_cost + 6.0 : 0.0);
+        if (s == 1 || cost < best) {
+            best = cost;
+            p.slabs = static_cast<int>(s);
+        }
+    }
+    p.columns_first = p.symbols >= 128;
+    p.bias_slabs = p.columns_first ? kColumnSlabs : p.slabs;
+    p.bias_at = p.slabs > 1 ? static_cast<size_t>(p.slabs) * A * H : 0;
+    p.largest_at = p.bias_at + static_cast<size_t>(p.bias_slabs) * A;
+    p.bytes = (p.largest_at + (p.columns_first ? static_cast<size_t>(kColumnSlabs) * A : 0)) * 4;
+    return p;
 }
 
 // Every launch returns a hipError_t.

@@ -691,60 +691,393 @@ __global__ __launch_bounds__(256) void ctc_linear_tiles_kernel(LinearArgs p)
 
 // ---- gradient of the weights ------------------------------------------------------------------------------------
 
+// dweight = G^T Q is a product whose inner index, the row, is the slow one of both operands: memory gives 4 symbols' or
+// columns' worth of a row at a time, the matrix cores take 8 rows of one symbol or column.  So the operands pass through registers, where
+// gradients take their scale and are split, and whole numbers become floats, and are laid down in LDS with the rows innermost.
+//
+// A product of gradient and scale, an fp32 number c, enters the matrix cores
+//   as three bf16 numbers, the leading 8 bits, the next 8 and the last (exact at any size): alphabets of at most 64 symbols, whose
+//   gradient is bound by the rows' bytes, or
+//   as two fp16 numbers, each rounded to nearest (22 bits and a sign; c is off by at most half its last bit or 2^-39 of its column's
+//   largest), after a power of two that puts the column's largest in [2^14, 2^15): wider ones, which the matrix cores bind.  The columns' largest
+//   take one more reading of the gradients, a launch of its own, which also forms the bias's gradient.
+// The whole numbers are exact in either type.
+
 struct GradientArgs {
     const void* grads;
     const int8_t* q;
     const float* scales;
     const int32_t* frames;
     int rows, H, A, pitch, slabs;
-    float* partials;             // [slabs, A * H + A]
+    float* out;                  // [slabs, A, H]
+    float* bias;                 // [slabs, A]: sums of the gradients; null: not wanted
+    const uint32_t* largest;     // [kColumnSlabs, A]: bits of the largest |gradient * scale|
 };
 
-// 64 symbols by 64 columns to a workgroup, 4 by 4 to a thread; 16 rows at a time in LDS.
-template <typename T>
-__global__ __launch_bounds__(256) void ctc_weight_gradient_kernel(GradientArgs p)
+typedef float float16v __attribute__((ext_vector_type(16)));
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
+typedef uint32_t uint2v __attribute__((ext_vector_type(2)));
+
+// The power of two that brings numbers of at most `largest` (bits) below 2^15, as an exponent.
+__device__ __forceinline__ int lift_of(uint32_t largest)
 {
-    __shared__ float s_g[16][65], s_q[16][65], s_plain[16][65];
-    const int n = listed(p.frames, p.rows);
-    const int per = (n + p.slabs - 1) / p.slabs;
-    const int a0 = blockIdx.x * 64, k0 = blockIdx.y * 64, slab = blockIdx.z;
+    const int e = static_cast<int>(largest >> 23);
+    return e == 255 ? 0 : e < 14 ? 127 : 141 - e;
+}
+
+// [first, last) of the list's entries for slab `slab` of `slabs`.
+struct Range { int first, last; };
+__device__ __forceinline__ Range slab_of(int n, int slab, int slabs)
+{
+    const int per = (n + slabs - 1) / slabs;
     const int64_t first = static_cast<int64_t>(slab) * per;
-    const int last = static_cast<int>(first + per < n ? first + per : n);
-    const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
-    float sum[4][4] = {}, bias[4] = {};
-    for (int64_t i0 = first; i0 < last; i0 += 16) {
-        __syncthreads();
-        for (int e = threadIdx.x; e < 16 * 64; e += 256) {
-            const int i = e / 64, c = e % 64;
-            const int r = i0 + i < last ? row_of(p.frames, p.rows, static_cast<int>(i0) + i) : -1;
-            float g = 0.0f, v = 0.0f, scale = 0.0f;
-            if (r >= 0) {
-                scale = p.scales[r];
-                if (a0 + c < p.A) g = widen(static_cast<const T*>(p.grads)[static_cast<int64_t>(r) * p.A + a0 + c]);
-                if (k0 + c < p.H) v = static_cast<float>(p.q[static_cast<int64_t>(r) * p.pitch + k0 + c]);
+    return {static_cast<int>(first < n ? first : n), static_cast<int>(first + per < n ? first + per : n)};
+}
+
+// Waits for this wavefront's requests to LDS, then for the workgroup's others; requests to memory stay under way.
+__device__ __forceinline__ void meet()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xc07f);                 // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// Largest |gradient * scale| and sum of the gradients of each symbol, over the rows of a slab: two symbols to a lane, the rows dealt out to
+// four wavefronts, eight at a time.
+template <typename T>
+__global__ __launch_bounds__(256) void ctc_gradient_columns_kernel(GradientArgs p, uint32_t* largest)
+{
+    __shared__ uint32_t s_most[4][2 * kWave];
+    __shared__ double s_sum[4][2 * kWave];
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int a = blockIdx.x * (2 * kWave) + 2 * lane, slab = blockIdx.y;
+    const Range range = slab_of(listed(p.frames, p.rows), slab, gridDim.y);
+    const int at = a + 1 < p.A ? a : a < p.A ? a - 1 : 0;                    // (A is at least 2 here; the last symbol of an odd number is the upper of a pair)
+    uint32_t most[2] = {};
+    double sum[2] = {};
+    for (int i = range.first + wave * 8; i < range.last; i += 32) {
+        T g[8][2];
+        float scale[8];
+        bool in[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int r = i + j < range.last ? row_of(p.frames, p.rows, i + j) : -1;
+            in[j] = r >= 0;
+            scale[j] = p.scales[in[j] ? r : 0];
+            __builtin_memcpy(g[j], static_cast<const T*>(p.grads) + static_cast<int64_t>(in[j] ? r : 0) * p.A + at, sizeof(g[j]));
+        }
+        float eight[2] = {};
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const float v = in[j] ? widen(g[j][k]) : 0.0f;
+                const uint32_t bits = __float_as_uint(v * scale[j]) & 0x7fffffffu;
+                if (in[j]) most[k] = most[k] > bits ? most[k] : bits;
+                eight[k] += v;
             }
-            s_plain[i][c] = g;
-            s_g[i][c] = r >= 0 ? g * scale : 0.0f;
-            s_q[i][c] = v;
+        sum[0] += static_cast<double>(eight[0]);
+        sum[1] += static_cast<double>(eight[1]);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        s_most[wave][2 * lane + k] = most[k];
+        s_sum[wave][2 * lane + k] = sum[k];
+    }
+    __syncthreads();
+    const int mine = blockIdx.x * (2 * kWave) + threadIdx.x;
+    if (threadIdx.x >= 2 * kWave || mine >= p.A) return;
+    const int from = mine == p.A - 1 && mine % 2 == 0 ? threadIdx.x + 1 : threadIdx.x;
+    uint32_t m = 0;
+    double total = 0.0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        m = m > s_most[w][from] ? m : s_most[w][from];
+        total += s_sum[w][from];
+    }
+    largest[static_cast<int64_t>(slab) * p.A + mine] = m;
+    if (p.bias) p.bias[static_cast<int64_t>(slab) * p.A + mine] = static_cast<float>(total);
+}
+
+// 32 WA NA symbols by 256 columns to a workgroup of eight wavefronts, WA of them down the symbols, 32 NA by 32 NK to each; 32 rows a step,
+// in two buffers of LDS: while the matrix cores work on one step, the next one's operands are laid down and those of the one
+// after it (of the two after it where a step is short: kAhead) are asked for.
+// LDS: symbol a's 8-row piece j (16 bytes) lies at 64 a + 16 (j ^ a / 4 % 4), column k's at 64 (64 (k % 4) + k / 4) + 16 (j ^ k % 4 ^ k / 16 % 4):
+// what lanes write or read at once then falls on different banks.
+// v_mfma_f32_32x32x16_{f16,bf16}: lane l gives numbers 8 (l / 32) .. of row l % 32 of either operand, and holds rows
+// 8 (v / 4) + 4 (l / 32) + v % 4, v < 16, of column l % 32 of the result.
+template <typename T, int WA, int NA, int NK, bool HALF>
+__global__ __launch_bounds__(512) void ctc_weight_gradient_kernel(GradientArgs p)
+{
+    constexpr int kTA = 32 * WA * NA, kTK = 256, kParts = HALF ? 2 : 3, kAhead = kTA <= 64 ? 2 : 1;
+    constexpr int kSymbols = kTA == 256 ? 2 : 1;                             // to a lane
+    static_assert(8 / WA * NK * 32 == kTK);
+    __shared__ __align__(1024) int8_t s_g[2][kParts][kTA * 64];
+    __shared__ __align__(1024) int8_t s_q[2][kTK * 64];
+    __shared__ int s_lift[HALF ? kTA : 1];
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int a0 = blockIdx.x * kTA, k0 = blockIdx.y * kTK, slab = blockIdx.z;
+    const Range range = slab_of(listed(p.frames, p.rows), slab, p.slabs);
+    const int steps = (range.last - range.first + 31) / 32;
+
+    // What this lane brings: symbols `symbol` (and the next one, or the one 64 on) of rows 8 (wave % 4) .., columns 4 lane .. of rows 4 wave ..
+    const bool brings = kTA >= 128 || (wave < 4 && lane < kTA);
+    const int symbol = kTA == 256 ? wave / 4 * 128 + (sizeof(T) == 2 ? 2 * lane : lane) : kTA == 128 ? wave / 4 * 64 + lane : lane;
+    constexpr int kNext = sizeof(T) == 2 ? 1 : 64;
+    float lift[kSymbols];
+    if constexpr (HALF) {
+        if (static_cast<int>(threadIdx.x) < kTA) {
+            uint32_t most = 0;
+            if (a0 + static_cast<int>(threadIdx.x) < p.A)
+#pragma unroll 16
+                for (int b = 0; b < kColumnSlabs; ++b) {
+                    const uint32_t m = p.largest[static_cast<int64_t>(b) * p.A + a0 + threadIdx.x];
+                    most = most > m ? most : m;
+                }
+            s_lift[threadIdx.x] = lift_of(most);
         }
         __syncthreads();
-        for (int i = 0; i < 16; ++i) {
 #pragma unroll
-            for (int a = 0; a < 4; ++a) {
-                bias[a] += s_plain[i][ty * 4 + a];
+        for (int j = 0; j < kSymbols; ++j) lift[j] = ldexpf(1.0f, s_lift[symbol + j * kNext]);
+    }
+    // (symbols behind the last and columns behind a row's bytes are others' once more: what becomes of them is not written)
+    const int last_symbol = p.A - 1;
+    // A pair of bf16 is one load; the last symbol of an odd number is the upper of a pair, its bits are moved down.
+    constexpr bool kPair = kSymbols == 2 && sizeof(T) == 2;
+    const int last_at = kPair ? last_symbol - 1 : last_symbol;               // (kPair: more than 128 symbols)
+    const int shift = kPair && a0 + symbol == last_symbol ? 16 : 0;
+    int at[kSymbols];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) sum[a][k] += s_g[i][ty * 4 + a] * s_q[i][tx * 4 + k];
+    for (int j = 0; j < kSymbols; ++j) at[j] = a0 + symbol + j * kNext < last_at ? a0 + symbol + j * kNext : last_at;
+    const int column = k0 + 4 * lane < p.pitch ? k0 + 4 * lane : 0;
+
+    // A step's rows and their scales, a lane each (lanes of 32 and more: none).
+    struct Rows { int row; float scale; };
+    const auto rows_of = [&](int step) {
+        const int64_t i = static_cast<int64_t>(range.first) + static_cast<int64_t>(step) * 32 + lane;
+        if (lane >= 32 || i >= range.last) return -1;
+        return p.frames ? p.frames[1 + i] : static_cast<int>(i);             // (looked at a step later, when it is there)
+    };
+    struct Raw {
+        Rows of;
+        uint32_t g[8][kPair ? 1 : kSymbols];
+        uint32_t q[4];
+    };
+    const auto ask = [&](Raw& to, Rows of) {
+        to.of = of;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int r = __builtin_amdgcn_readlane(of.row, wave * 4 + j);
+            __builtin_memcpy(&to.q[j], p.q + static_cast<int64_t>(r < 0 ? 0 : r) * p.pitch + column, 4);
+        }
+        if (!brings) return;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int r = __builtin_amdgcn_readlane(of.row, wave % 4 * 8 + j);
+            const T* from = static_cast<const T*>(p.grads) + static_cast<int64_t>(r < 0 ? 0 : r) * p.A;
+            if constexpr (kPair) {
+                __builtin_memcpy(&to.g[j][0], from + at[0], 4);
+            } else {
+#pragma unroll
+                for (int k = 0; k < kSymbols; ++k) {
+                    if constexpr (sizeof(T) == 2)
+                        to.g[j][k] = from[at[k]].bits;
+                    else
+                        to.g[j][k] = __float_as_uint(widen(from[at[k]]));
+                }
+            }
+        }
+    };
+    double bias = 0.0;
+    const bool sums = !HALF && p.bias && blockIdx.y == 0;
+    const auto lay_down = [&](Raw& from, int buffer) {
+        if (brings) {
+            if ((__ballot(from.of.row >= 0) & 0xffffffffull) != 0xffffffffull) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (__builtin_amdgcn_readlane(from.of.row, wave % 4 * 8 + j) < 0) {
+#pragma unroll
+                        for (int k = 0; k < (kPair ? 1 : kSymbols); ++k) from.g[j][k] = 0;
+                    }
+            }
+            float scale[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                scale[j] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(from.of.scale), wave % 4 * 8 + j));
+#pragma unroll
+            for (int k = 0; k < kSymbols; ++k) {
+                uint4v part[kParts];
+                float eight = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 8; j += 2) {
+                    float c[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float g;
+                        if constexpr (kPair)
+                            g = __uint_as_float(k ? from.g[j + e][0] & 0xffff0000u : from.g[j + e][0] >> shift << 16);
+                        else
+                            g = __uint_as_float(sizeof(T) == 2 ? from.g[j + e][k] << 16 : from.g[j + e][k]);
+                        eight += g;
+                        c[e] = g * scale[j + e];
+                    }
+                    if constexpr (HALF) {
+                        c[0] *= lift[k];
+                        c[1] *= lift[k];
+                        const half2 high = {static_cast<_Float16>(c[0]), static_cast<_Float16>(c[1])};
+                        const half2 low = {static_cast<_Float16>(c[0] - static_cast<float>(high[0])),
+                                           static_cast<_Float16>(c[1] - static_cast<float>(high[1]))};
+                        part[0][j / 2] = __builtin_bit_cast(uint32_t, high);
+                        part[1][j / 2] = __builtin_bit_cast(uint32_t, low);
+                    } else {
+#pragma unroll
+                        for (int b = 0; b < 3; ++b) {
+                            const uint32_t u = __float_as_uint(c[0]), v = __float_as_uint(c[1]);
+                            part[b][j / 2] = __builtin_amdgcn_perm(v, u, 0x07060302);         // the leading halves of both
+                            c[0] -= __uint_as_float(u & 0xffff0000u);
+                            c[1] -= __uint_as_float(v & 0xffff0000u);
+                        }
+                    }
+                }
+                if (sums) bias += static_cast<double>(eight);
+                const int s = symbol + k * kNext, to = s * 64 + ((wave % 4 ^ s / 4 % 4) * 16);
+#pragma unroll
+                for (int b = 0; b < kParts; ++b) *reinterpret_cast<uint4v*>(&s_g[buffer][b][to]) = part[b];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            uint2v four;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const uint32_t x = from.q[2 * j], y = from.q[2 * j + 1];
+                if constexpr (HALF) {
+                    // byte k of either, 128 more, behind 0x64: 1024 + 128 + the number, as fp16
+                    const uint32_t bytes = __builtin_amdgcn_perm(y ^ 0x80808080u, x ^ 0x80808080u, 0x0c040c00u + 0x00010001u * k) | 0x64006400u;
+                    const half2 offset = {static_cast<_Float16>(-1152.0f), static_cast<_Float16>(-1152.0f)};
+                    four[j] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2, bytes) + offset);
+                } else {
+                    const float u = static_cast<float>(static_cast<int8_t>(x >> 8 * k)), v = static_cast<float>(static_cast<int8_t>(y >> 8 * k));
+                    four[j] = __builtin_amdgcn_perm(__float_as_uint(v), __float_as_uint(u), 0x07060302);
+                }
+            }
+            *reinterpret_cast<uint2v*>(&s_q[buffer][(k * 64 + lane) * 64 + ((wave / 2 ^ k ^ lane / 4 % 4) * 16) + wave % 2 * 8]) = four;
+        }
+    };
+    const int wave_a = wave / (8 / WA), wave_k = wave % (8 / WA);
+    float16v sum[NA][NK] = {};
+    const auto multiply = [&](int buffer) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint4v g[kParts][NA], q[NK];
+#pragma unroll
+            for (int k = 0; k < NK; ++k) {
+                const int first = wave_k * NK + k, piece = (h * 2 + lane / 32) ^ lane % 4 ^ (first % 2 * 2 + lane % 32 / 16);
+                q[k] = *reinterpret_cast<const uint4v*>(&s_q[buffer][(lane % 4 * 64 + first * 8 + lane % 32 / 4) * 64 + piece * 16]);
+            }
+#pragma unroll
+            for (int b = 0; b < kParts; ++b)
+#pragma unroll
+                for (int i = 0; i < NA; ++i)
+                    g[b][i] = *reinterpret_cast<const uint4v*>(
+                        &s_g[buffer][b][((wave_a * NA + i) * 32 + lane % 32) * 64 + (((h * 2 + lane / 32) ^ lane / 4 % 4) * 16)]);
+#pragma unroll
+            for (int b = kParts - 1; b >= 0; --b)
+#pragma unroll
+                for (int i = 0; i < NA; ++i)
+#pragma unroll
+                    for (int k = 0; k < NK; ++k) {
+                        if constexpr (HALF)
+                            sum[i][k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, g[b][i]),
+                                                                               __builtin_bit_cast(half8, q[k]), sum[i][k], 0, 0, 0);
+                        else
+                            sum[i][k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, g[b][i]),
+                                                                                __builtin_bit_cast(bf16x8, q[k]), sum[i][k], 0, 0, 0);
+                    }
+        }
+    };
+    if (steps > 0) {
+        // What a step's loads need, its rows' numbers and scales, is asked for a step and two steps before them: nothing is waited for
+        // that has not been under way for a step.  (Steps behind the last have rows that do not count.)
+        Raw raw[kAhead];
+        const auto with_scales = [&](int entry) {
+            const int row = entry < p.rows ? entry : -1;
+            return Rows{row, row < 0 ? 0.0f : p.scales[row]};
+        };
+        Rows next = with_scales(rows_of(0));
+        ask(raw[0], next);
+        lay_down(raw[0], 0);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) ask(raw[j], with_scales(rows_of(1 + j)));
+        next = with_scales(rows_of(1 + kAhead));
+        int after = rows_of(2 + kAhead);
+        meet();
+        for (int t = 0; t < steps; t += kAhead) {
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+                if (t + j >= steps) break;
+                const int now = kAhead == 2 ? j : t & 1;
+                lay_down(raw[j], now ^ 1);
+                ask(raw[j], next);
+                next = with_scales(after);
+                after = rows_of(t + j + 3 + kAhead);
+                multiply(now);
+                meet();
             }
         }
     }
-    float* out = p.partials + static_cast<int64_t>(slab) * p.A * (p.H + 1);
+    if (sums) {
+        // The four wavefronts that brought the gradients, one after another.
+        double* const s_bias = reinterpret_cast<double*>(&s_q[0][0]);
+        for (int w = 0; w < 4; ++w) {
+            if (wave == w && lane < kTA) {
+                if (w) bias += s_bias[lane];
+                s_bias[lane] = bias;
+            }
+            __syncthreads();
+        }
+        if (wave == 3 && lane < kTA && a0 + lane < p.A) p.bias[static_cast<int64_t>(slab) * p.A + a0 + lane] = static_cast<float>(bias);
+    }
+    float* const out = p.out + static_cast<int64_t>(slab) * p.A * p.H;
 #pragma unroll
-    for (int a = 0; a < 4; ++a) {
-        if (a0 + ty * 4 + a >= p.A) continue;
+    for (int i = 0; i < NA; ++i)
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (k0 + tx * 4 + k < p.H) out[static_cast<int64_t>(a0 + ty * 4 + a) * p.H + k0 + tx * 4 + k] = sum[a][k];
-        if (blockIdx.y == 0 && tx == 0) out[static_cast<int64_t>(p.A) * p.H + a0 + ty * 4 + a] = bias[a];
+        for (int v = 0; v < 16; ++v) {
+            const int s = (wave_a * NA + i) * 32 + 8 * (v / 4) + 4 * (lane / 32) + v % 4;
+            if (a0 + s >= p.A) continue;
+            float* const row = out + static_cast<int64_t>(a0 + s) * p.H;
+#pragma unroll
+            for (int k = 0; k < NK; ++k) {
+                const int c = k0 + (wave_k * NK + k) * 32 + lane % 32;
+                if (c < p.H) row[c] = HALF ? ldexpf(sum[i][k][v], -s_lift[HALF ? s : 0]) : sum[i][k][v];
+            }
+        }
+}
+
+// out[i] = the slabs' sums, in order; four to a thread.
+__global__ __launch_bounds__(256) void ctc_sum_slabs_kernel(const float* __restrict__ partials, int slabs, int64_t width, float* __restrict__ out)
+{
+    const int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
+    if (i >= width) return;
+    if (i + 4 <= width) {
+        float sum[4] = {};
+#pragma unroll 8
+        for (int s = 0; s < slabs; ++s) {
+            const Vector<float> v = load_whole(partials + s * width + i);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sum[k] += v.v[k];
+        }
+        __builtin_memcpy(out + i, sum, sizeof(sum));
+        return;
+    }
+    for (int64_t k = i; k < width; ++k) {
+        float sum = 0.0f;
+        for (int s = 0; s < slabs; ++s) sum += partials[s * width + k];
+        out[k] = sum;
     }
 }
 
@@ -805,6 +1138,26 @@ template <typename T> void launch_product(const LinearArgs& p, hipStream_t s)
         launch_tiles<T, 2, 2>(p, s);
     else
         launch_tiles<T, 4, 4>(p, s);
+}
+
+template <typename T, int WA, int NA, int NK, bool HALF>
+void launch_gradient_tiles(const GradientArgs& p, hipStream_t s)
+{
+    const dim3 grid(blocks(p.A, 32 * WA * NA), blocks(p.H, 256), static_cast<unsigned>(p.slabs));
+    hipLaunchKernelGGL((ctc_weight_gradient_kernel<T, WA, NA, NK, HALF>), grid, dim3(512), 0, s, p);
+}
+template <typename T> void launch_gradient(const GradientArgs& p, const GradientPlan& plan, uint32_t* largest, hipStream_t s)
+{
+    if (plan.columns_first)
+        hipLaunchKernelGGL(ctc_gradient_columns_kernel<T>, dim3(blocks(p.A, 2 * kWave), kColumnSlabs), dim3(256), 0, s, p, largest);
+    if (plan.symbols == 32)
+        launch_gradient_tiles<T, 1, 1, 1, false>(p, s);
+    else if (plan.symbols == 64)
+        launch_gradient_tiles<T, 1, 2, 1, false>(p, s);
+    else if (plan.symbols == 128)
+        launch_gradient_tiles<T, 4, 1, 4, true>(p, s);
+    else
+        launch_gradient_tiles<T, 4, 2, 4, true>(p, s);
 }
 
 }  // namespace
@@ -884,22 +1237,25 @@ int launch_weight_gradient(const void* grads, const int8_t* q, const float* scal
                            int A, bool bf16, float* dweight, float* dbias, float* partials, void* stream)
 {
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const int slabs = gradient_slabs(rows, H, A);
-    const GradientArgs p = {grads, q, scales, frames, rows, H, A, pitch_of(H), slabs, partials};
-    const dim3 grid(blocks(A, 64), blocks(H, 64), static_cast<unsigned>(slabs)), block(256);
+    const GradientPlan plan = gradient_plan(rows, H, A);
+    const int64_t weights = static_cast<int64_t>(A) * H;
+    float* const bias = partials + plan.bias_at;
+    uint32_t* const largest = reinterpret_cast<uint32_t*>(partials + plan.largest_at);
+    const GradientArgs p = {grads, q, scales, frames, rows, H, A, pitch_of(H), plan.slabs,
+                            plan.slabs > 1 ? partials : dweight, dbias ? bias : nullptr, largest};
     if (bf16)
-        hipLaunchKernelGGL(ctc_weight_gradient_kernel<bf16_t>, grid, block, 0, s, p);
+        launch_gradient<bf16_t>(p, plan, largest, s);
     else
-        hipLaunchKernelGGL(ctc_weight_gradient_kernel<float>, grid, block, 0, s, p);
+        launch_gradient<float>(p, plan, largest, s);
     int err = last_error();
     if (err) return err;
-    const int64_t weights = static_cast<int64_t>(A) * H, stride = weights + A;
-    hipLaunchKernelGGL(ctc_sum_partials_kernel, dim3(blocks(weights, kWave)), dim3(1024), 0, s, partials, slabs, stride, weights,
-                       dweight);
-    err = last_error();
+    if (plan.slabs > 1) {
+        hipLaunchKernelGGL(ctc_sum_slabs_kernel, dim3(blocks(weights, 1024)), dim3(256), 0, s, partials, plan.slabs, weights, dweight);
+        err = last_error();
+    }
     if (err || !dbias) return err;
-    hipLaunchKernelGGL(ctc_sum_partials_kernel, dim3(blocks(A, kWave)), dim3(1024), 0, s, partials + weights, slabs, stride,
-                       static_cast<int64_t>(A), dbias);
+    hipLaunchKernelGGL(ctc_sum_partials_kernel, dim3(blocks(A, kWave)), dim3(1024), 0, s, bias, plan.bias_slabs,
+                       static_cast<int64_t>(A), static_cast<int64_t>(A), dbias);
     return last_error();
 }
 

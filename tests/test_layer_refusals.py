@@ -122,7 +122,7 @@ def test_overlapping_buffers(name, a, b):
         assert status(name, **{a: CALLS[name][b]}) == INVALID
     if name == "pack_frames":
         return
-    if b not in ("weight", "bias", "weight_scales", "dweight", "dbias") or (name, b) == ("weight_gradient_i8", "dweight"):
+    if b not in ("weight", "bias", "weight_scales", "dweight", "dbias", "workspace") or (name, b) == ("weight_gradient_i8", "dweight"):
         assert status(name, **{a: CALLS[name][b] + step}) == INVALID
 
 
@@ -149,8 +149,10 @@ def test_workspace():
 
 
 def test_the_largest_sizes_are_counted_in_64_bits():
-    n = layer.weight_gradient_workspace_size(1 << 30, 16384, 1 << 20)
-    assert n >= (1 << 20) * 16385 * 4
+    for H, A in ((16384, 1 << 20), (16384, 4000), (16384, 64), (1, 1)):
+        n = layer.weight_gradient_workspace_size(1 << 30, H, A)
+        assert 0 < n <= 257 * (1 << 20) * 16385 * 4 and n % 256 == 0
+    assert layer.weight_gradient_workspace_size(1 << 30, 1, 1 << 20) > 1 << 28
     assert layer.rms_norm_workspace_size(1 << 30, 16384) >= 16384 * 4
 
 
