@@ -28,7 +28,7 @@ inline int norm_partials(int rows)
 // of its own.
 constexpr int kColumnSlabs = 64;                // workgroups that look at one symbol's gradients first
 struct GradientPlan {
-    int symbols;                                // of a tile: 32, 64, 128 or 256
+    int symbols, columns;                       // of a tile: 32 or 64 by 256, 128 by 512
     int slabs;
     bool columns_first;                         // a launch that finds the columns' largest, before
     int bias_slabs;
@@ -37,13 +37,14 @@ struct GradientPlan {
 inline GradientPlan gradient_plan(int rows, int H, int A)
 {
     GradientPlan p{};
-    p.symbols = A <= 32 ? 32 : A <= 64 ? 64 : A <= 128 ? 128 : 256;
-    const long tiles = ((A + p.symbols - 1L) / p.symbols) * ((H + 255L) / 256);
+    p.symbols = A <= 32 ? 32 : A <= 64 ? 64 : 128;
+    p.columns = A <= 64 ? 256 : 512;
+    const long tiles = ((A + p.symbols - 1L) / p.symbols) * ((H + p.columns - 1L) / p.columns);
     const long steps = (rows + 31L) / 32;
     // Time in steps of 32 rows: as many rounds of workgroups as the 256 compute units take (three workgroups each where tiles are narrow), each of its
     // share of the steps and a few to begin and end with; and every slab's sums are written and read once more.
     const long at_once = p.symbols <= 64 ? 768 : 256;
-    const double slab_cost = 8.0 * A * H / 5.0e6 / (p.symbols <= 64 ? 0.2 : p.symbols == 128 ? 0.5 : 0.9);
+    const double slab_cost = 8.0 * A * H / 5.0e6 / (p.symbols <= 64 ? 0.2 : 0.9);
     double best = 0.0;
     for (long s = 1; s <= 256 && s <= (steps + 3) / 4; ++s) {
         const long rounds = (tiles * s + at_once - 1) / at_once;

@@ -803,32 +803,31 @@ __global__ __launch_bounds__(256) void ctc_gradient_columns_kernel(GradientArgs 
     if (p.bias) p.bias[static_cast<int64_t>(slab) * p.A + mine] = static_cast<float>(total);
 }
 
-// 32 WA NA symbols by 256 columns to a workgroup of eight wavefronts, WA of them down the symbols, 32 NA by 32 NK to each; 32 rows a step,
-// in two buffers of LDS: while the matrix cores work on one step, the next one's operands are laid down and those of the one
-// after it (of the two after it where a step is short: kAhead) are asked for.
-// LDS: symbol a's 8-row piece j (16 bytes) lies at 64 a + 16 (j ^ a / 4 % 4), column k's at 64 (64 (k % 4) + k / 4) + 16 (j ^ k % 4 ^ k / 16 % 4):
-// what lanes write or read at once then falls on different banks.
+// 32 WA NA symbols by 32 WK NK columns to a workgroup of eight wavefronts, WA down the symbols and WK across, 32 NA by 32 NK to each; 32
+// rows a step.  In a step a wavefront multiplies one buffer of LDS, lays down the operands of the next step (where there are three
+// buffers, of the one after the next, so that the next one's first operands are fetched ahead of the barrier) and asks memory for what it
+// will lay down two steps later.
+// LDS: symbol a's 8-row piece j (16 bytes) lies at 64 a + 16 (j ^ a / 4 % 4); column k's at 64 (k % 4 * columns / 4 + k / 4) + 16 (j ^ k % 4 ^
+// k / 16 % 4): what lanes write or read at once then falls on different banks.
 // v_mfma_f32_32x32x16_{f16,bf16}: lane l gives numbers 8 (l / 32) .. of row l % 32 of either operand, and holds rows
 // 8 (v / 4) + 4 (l / 32) + v % 4, v < 16, of column l % 32 of the result.
 template <typename T, int WA, int NA, int NK, bool HALF>
 __global__ __launch_bounds__(512) void ctc_weight_gradient_kernel(GradientArgs p)
 {
-    constexpr int kTA = 32 * WA * NA, kTK = 256, kParts = HALF ? 2 : 3, kAhead = kTA <= 64 ? 2 : 1;
-    constexpr int kSymbols = kTA == 256 ? 2 : 1;                             // to a lane
-    static_assert(8 / WA * NK * 32 == kTK);
-    __shared__ __align__(1024) int8_t s_g[2][kParts][kTA * 64];
-    __shared__ __align__(1024) int8_t s_q[2][kTK * 64];
+    constexpr int WK = 8 / WA, kTA = 32 * WA * NA, kTK = 32 * WK * NK, kParts = HALF ? 2 : 3, kBuffers = HALF ? 3 : 2, kGroups = kTK / 256;
+    static_assert(kTA <= 128 && kTK % 256 == 0);
+    constexpr int kPartBytes = kTA * 64, kNumbers = kParts * kPartBytes, kBytes = kNumbers + kTK * 64;       // gradients, then whole numbers
+    __shared__ __align__(1024) int8_t s_buffer[kBuffers * kBytes];
     __shared__ int s_lift[HALF ? kTA : 1];
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int a0 = blockIdx.x * kTA, k0 = blockIdx.y * kTK, slab = blockIdx.z;
     const Range range = slab_of(listed(p.frames, p.rows), slab, p.slabs);
     const int steps = (range.last - range.first + 31) / 32;
 
-    // What this lane brings: symbols `symbol` (and the next one, or the one 64 on) of rows 8 (wave % 4) .., columns 4 lane .. of rows 4 wave ..
-    const bool brings = kTA >= 128 || (wave < 4 && lane < kTA);
-    const int symbol = kTA == 256 ? wave / 4 * 128 + (sizeof(T) == 2 ? 2 * lane : lane) : kTA == 128 ? wave / 4 * 64 + lane : lane;
-    constexpr int kNext = sizeof(T) == 2 ? 1 : 64;
-    float lift[kSymbols];
+    // What this lane brings: symbol `symbol` of rows 8 (wave % 4) .., columns 4 lane .. (and 256 on) of rows 4 wave ..
+    const bool brings = kTA == 128 || (wave < 4 && lane < kTA);
+    const int symbol = kTA == 128 ? wave / 4 * 64 + lane : lane;
+    float lift = 1.0f;
     if constexpr (HALF) {
         if (static_cast<int>(threadIdx.x) < kTA) {
             uint32_t most = 0;
@@ -841,198 +840,220 @@ __global__ __launch_bounds__(512) void ctc_weight_gradient_kernel(GradientArgs p
             s_lift[threadIdx.x] = lift_of(most);
         }
         __syncthreads();
-#pragma unroll
-        for (int j = 0; j < kSymbols; ++j) lift[j] = ldexpf(1.0f, s_lift[symbol + j * kNext]);
+        lift = ldexpf(1.0f, s_lift[symbol]);
     }
     // (symbols behind the last and columns behind a row's bytes are others' once more: what becomes of them is not written)
-    const int last_symbol = p.A - 1;
-    // A pair of bf16 is one load; the last symbol of an odd number is the upper of a pair, its bits are moved down.
-    constexpr bool kPair = kSymbols == 2 && sizeof(T) == 2;
-    const int last_at = kPair ? last_symbol - 1 : last_symbol;               // (kPair: more than 128 symbols)
-    const int shift = kPair && a0 + symbol == last_symbol ? 16 : 0;
-    int at[kSymbols];
+    const uint32_t at = static_cast<uint32_t>(a0 + symbol < p.A ? a0 + symbol : p.A - 1) * static_cast<uint32_t>(sizeof(T));
+    uint32_t column[kGroups];
 #pragma unroll
-    for (int j = 0; j < kSymbols; ++j) at[j] = a0 + symbol + j * kNext < last_at ? a0 + symbol + j * kNext : last_at;
-    const int column = k0 + 4 * lane < p.pitch ? k0 + 4 * lane : 0;
+    for (int c = 0; c < kGroups; ++c) {
+        const int k = k0 + 256 * c + 4 * lane;
+        column[c] = k < p.pitch ? k : 0;
+    }
 
-    // A step's rows and their scales, a lane each (lanes of 32 and more: none).
-    struct Rows { int row; float scale; };
-    const auto rows_of = [&](int step) {
-        const int64_t i = static_cast<int64_t>(range.first) + static_cast<int64_t>(step) * 32 + lane;
-        if (lane >= 32 || i >= range.last) return -1;
-        return p.frames ? p.frames[1 + i] : static_cast<int>(i);             // (looked at a step later, when it is there)
+    // A step's rows, as the list has them, and their scales, a lane each; what does not count has scale 0 and, once they are there, gradients 0.
+    // (Steps behind the last have rows that do not count; every index is one of the list's, every address a row's.)
+    struct Rows { int entry; float scale; };
+    const int32_t* const entries = p.frames ? p.frames + 1 : reinterpret_cast<const int32_t*>(p.scales);
+    const auto entries_of = [&](int step) {
+        const int i = range.first + step * 32 + lane % 32;
+        return entries[i < range.last ? i : range.last - 1];
+    };
+    const auto rows_of = [&](int step, int entry) {                          // (for the entries that entries_of gave)
+        const int i = range.first + step * 32 + lane % 32;
+        const int r = p.frames ? entry : i;
+        return i < range.last && r >= 0 && r < p.rows ? r : -1;
     };
     struct Raw {
         Rows of;
-        uint32_t g[8][kPair ? 1 : kSymbols];
-        uint32_t q[4];
+        uint32_t g[8];
+        uint32_t q[4][kGroups];
     };
-    const auto ask = [&](Raw& to, Rows of) {
-        to.of = of;
+    // The work on a step's operands, in pieces that the products are put between.
+    // Loads of the whole numbers' rows and of the gradients' rows:
+    const auto ask_numbers = [&](Raw& to, int j) {
+        const int r = __builtin_amdgcn_readlane(to.of.entry, wave * 4 + j);
+        const int8_t* from = p.q + static_cast<uint64_t>(r < 0 ? 0 : r) * static_cast<uint32_t>(p.pitch);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int r = __builtin_amdgcn_readlane(of.row, wave * 4 + j);
-            __builtin_memcpy(&to.q[j], p.q + static_cast<int64_t>(r < 0 ? 0 : r) * p.pitch + column, 4);
-        }
-        if (!brings) return;
+        for (int c = 0; c < kGroups; ++c) to.q[j][c] = *reinterpret_cast<const uint32_t*>(from + column[c]);
+    };
+    const auto ask_gradients = [&](Raw& to, int j) {
+        const int r = __builtin_amdgcn_readlane(to.of.entry, wave % 4 * 8 + j);
+        const char* from = static_cast<const char*>(p.grads) + static_cast<uint64_t>(r < 0 ? 0 : r) * (static_cast<uint32_t>(p.A) * sizeof(T));
+        if constexpr (sizeof(T) == 2)
+            to.g[j] = *reinterpret_cast<const uint16_t*>(from + at);
+        else
+            to.g[j] = *reinterpret_cast<const uint32_t*>(from + at);
+    };
+    // Gradients of rows that do not count: none, whatever is there.
+    const auto clear = [&](Raw& from) {
+        if (__ballot(from.of.entry >= 0) == ~0ull) return;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int r = __builtin_amdgcn_readlane(of.row, wave % 4 * 8 + j);
-            const T* from = static_cast<const T*>(p.grads) + static_cast<int64_t>(r < 0 ? 0 : r) * p.A;
-            if constexpr (kPair) {
-                __builtin_memcpy(&to.g[j][0], from + at[0], 4);
-            } else {
-#pragma unroll
-                for (int k = 0; k < kSymbols; ++k) {
-                    if constexpr (sizeof(T) == 2)
-                        to.g[j][k] = from[at[k]].bits;
-                    else
-                        to.g[j][k] = __float_as_uint(widen(from[at[k]]));
-                }
-            }
-        }
+        for (int j = 0; j < 8; ++j)
+            if (__builtin_amdgcn_readlane(from.of.entry, wave % 4 * 8 + j) < 0) from.g[j] = 0;
+        from.of.scale = from.of.entry < 0 ? 0.0f : from.of.scale;
     };
     double bias = 0.0;
     const bool sums = !HALF && p.bias && blockIdx.y == 0;
-    const auto lay_down = [&](Raw& from, int buffer) {
-        if (brings) {
-            if ((__ballot(from.of.row >= 0) & 0xffffffffull) != 0xffffffffull) {
+    // Two rows' gradients, split, and the write of eight rows' parts with the last of them:
+    uint4v part[kParts];
+    const auto split = [&](const Raw& from, int8_t* buffer, int j) {
+        float g[2], scale[2];
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (__builtin_amdgcn_readlane(from.of.row, wave % 4 * 8 + j) < 0) {
+        for (int e = 0; e < 2; ++e) {
+            g[e] = __uint_as_float(sizeof(T) == 2 ? from.g[j + e] << 16 : from.g[j + e]);
+            scale[e] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(from.of.scale), wave % 4 * 8 + j + e));
+            if (sums) bias += static_cast<double>(g[e]);
+        }
+        if constexpr (HALF) {
+            const float c[2] = {g[0] * scale[0] * lift, g[1] * scale[1] * lift};
+            const half2 high = {static_cast<_Float16>(c[0]), static_cast<_Float16>(c[1])};
+            const half2 low = {static_cast<_Float16>(c[0] - static_cast<float>(high[0])),
+                               static_cast<_Float16>(c[1] - static_cast<float>(high[1]))};
+            part[0][j / 2] = __builtin_bit_cast(uint32_t, high);
+            part[1][j / 2] = __builtin_bit_cast(uint32_t, low);
+        } else {
+            float c[2] = {g[0] * scale[0], g[1] * scale[1]};
 #pragma unroll
-                        for (int k = 0; k < (kPair ? 1 : kSymbols); ++k) from.g[j][k] = 0;
-                    }
-            }
-            float scale[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                scale[j] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(from.of.scale), wave % 4 * 8 + j));
-#pragma unroll
-            for (int k = 0; k < kSymbols; ++k) {
-                uint4v part[kParts];
-                float eight = 0.0f;
-#pragma unroll
-                for (int j = 0; j < 8; j += 2) {
-                    float c[2];
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        float g;
-                        if constexpr (kPair)
-                            g = __uint_as_float(k ? from.g[j + e][0] & 0xffff0000u : from.g[j + e][0] >> shift << 16);
-                        else
-                            g = __uint_as_float(sizeof(T) == 2 ? from.g[j + e][k] << 16 : from.g[j + e][k]);
-                        eight += g;
-                        c[e] = g * scale[j + e];
-                    }
-                    if constexpr (HALF) {
-                        c[0] *= lift[k];
-                        c[1] *= lift[k];
-                        const half2 high = {static_cast<_Float16>(c[0]), static_cast<_Float16>(c[1])};
-                        const half2 low = {static_cast<_Float16>(c[0] - static_cast<float>(high[0])),
-                                           static_cast<_Float16>(c[1] - static_cast<float>(high[1]))};
-                        part[0][j / 2] = __builtin_bit_cast(uint32_t, high);
-                        part[1][j / 2] = __builtin_bit_cast(uint32_t, low);
-                    } else {
-#pragma unroll
-                        for (int b = 0; b < 3; ++b) {
-                            const uint32_t u = __float_as_uint(c[0]), v = __float_as_uint(c[1]);
-                            part[b][j / 2] = __builtin_amdgcn_perm(v, u, 0x07060302);         // the leading halves of both
-                            c[0] -= __uint_as_float(u & 0xffff0000u);
-                            c[1] -= __uint_as_float(v & 0xffff0000u);
-                        }
-                    }
-                }
-                if (sums) bias += static_cast<double>(eight);
-                const int s = symbol + k * kNext, to = s * 64 + ((wave % 4 ^ s / 4 % 4) * 16);
-#pragma unroll
-                for (int b = 0; b < kParts; ++b) *reinterpret_cast<uint4v*>(&s_g[buffer][b][to]) = part[b];
+            for (int b = 0; b < 3; ++b) {
+                const uint32_t u = __float_as_uint(c[0]), v = __float_as_uint(c[1]);
+                part[b][j / 2] = __builtin_amdgcn_perm(v, u, 0x07060302);                     // the leading halves of both
+                c[0] -= __uint_as_float(u & 0xffff0000u);
+                c[1] -= __uint_as_float(v & 0xffff0000u);
             }
         }
+        if (j != 6) return;
+        const int to = symbol * 64 + ((wave % 4 ^ symbol / 4 % 4) * 16);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            uint2v four;
+        for (int b = 0; b < kParts; ++b) *reinterpret_cast<uint4v*>(buffer + b * kPartBytes + to) = part[b];
+    };
+    // Four rows' whole numbers of column 256 c + 4 lane + k:
+    const auto widen_numbers = [&](const Raw& from, int8_t* buffer, int c, int k) {
+        uint2v four;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const uint32_t x = from.q[2 * j], y = from.q[2 * j + 1];
-                if constexpr (HALF) {
-                    // byte k of either, 128 more, behind 0x64: 1024 + 128 + the number, as fp16
-                    const uint32_t bytes = __builtin_amdgcn_perm(y ^ 0x80808080u, x ^ 0x80808080u, 0x0c040c00u + 0x00010001u * k) | 0x64006400u;
-                    const half2 offset = {static_cast<_Float16>(-1152.0f), static_cast<_Float16>(-1152.0f)};
-                    four[j] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2, bytes) + offset);
-                } else {
-                    const float u = static_cast<float>(static_cast<int8_t>(x >> 8 * k)), v = static_cast<float>(static_cast<int8_t>(y >> 8 * k));
-                    four[j] = __builtin_amdgcn_perm(__float_as_uint(v), __float_as_uint(u), 0x07060302);
-                }
+        for (int j = 0; j < 2; ++j) {
+            const uint32_t x = from.q[2 * j][c], y = from.q[2 * j + 1][c];
+            if constexpr (HALF) {
+                // byte k of either, 128 more, behind 0x64: 1024 + 128 + the number, as fp16
+                const uint32_t bytes = __builtin_amdgcn_perm(y ^ 0x80808080u, x ^ 0x80808080u, 0x0c040c00u + 0x00010001u * k) | 0x64006400u;
+                const half2 offset = {static_cast<_Float16>(-1152.0f), static_cast<_Float16>(-1152.0f)};
+                four[j] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2, bytes) + offset);
+            } else {
+                const float u = static_cast<float>(static_cast<int8_t>(x >> 8 * k)), v = static_cast<float>(static_cast<int8_t>(y >> 8 * k));
+                four[j] = __builtin_amdgcn_perm(__float_as_uint(v), __float_as_uint(u), 0x07060302);
             }
-            *reinterpret_cast<uint2v*>(&s_q[buffer][(k * 64 + lane) * 64 + ((wave / 2 ^ k ^ lane / 4 % 4) * 16) + wave % 2 * 8]) = four;
+        }
+        *reinterpret_cast<uint2v*>(buffer + kNumbers + (k * (kTK / 4) + c * 64 + lane) * 64 + ((wave / 2 ^ k ^ lane / 4 % 4) * 16) + wave % 2 * 8) = four;
+    };
+
+    const int wave_a = wave / WK, wave_k = wave % WK;
+    float16v sum[NA][NK] = {};
+    uint4v g[2][kParts][NA], q[2][NK];
+    constexpr int kReads = NK + kParts * NA;
+    const auto fetch = [&](const int8_t* buffer, int h, int n) {             // (the n-th of a half's reads, in the order of the products)
+        if (n < NK) {
+            const int first = wave_k * NK + n, piece = (h * 2 + lane / 32) ^ lane % 4 ^ (first % 2 * 2 + lane % 32 / 16);
+            q[h][n] = *reinterpret_cast<const uint4v*>(buffer + kNumbers + (lane % 4 * (kTK / 4) + first * 8 + lane % 32 / 4) * 64 + piece * 16);
+        } else {
+            const int b = kParts - 1 - (n - NK) / NA, i = (n - NK) % NA;
+            g[h][b][i] = *reinterpret_cast<const uint4v*>(
+                buffer + b * kPartBytes + ((wave_a * NA + i) * 32 + lane % 32) * 64 + (((h * 2 + lane / 32) ^ lane / 4 % 4) * 16));
         }
     };
-    const int wave_a = wave / (8 / WA), wave_k = wave % (8 / WA);
-    float16v sum[NA][NK] = {};
-    const auto multiply = [&](int buffer) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            uint4v g[kParts][NA], q[NK];
-#pragma unroll
-            for (int k = 0; k < NK; ++k) {
-                const int first = wave_k * NK + k, piece = (h * 2 + lane / 32) ^ lane % 4 ^ (first % 2 * 2 + lane % 32 / 16);
-                q[k] = *reinterpret_cast<const uint4v*>(&s_q[buffer][(lane % 4 * 64 + first * 8 + lane % 32 / 4) * 64 + piece * 16]);
-            }
-#pragma unroll
-            for (int b = 0; b < kParts; ++b)
-#pragma unroll
-                for (int i = 0; i < NA; ++i)
-                    g[b][i] = *reinterpret_cast<const uint4v*>(
-                        &s_g[buffer][b][((wave_a * NA + i) * 32 + lane % 32) * 64 + (((h * 2 + lane / 32) ^ lane / 4 % 4) * 16)]);
-#pragma unroll
-            for (int b = kParts - 1; b >= 0; --b)
-#pragma unroll
-                for (int i = 0; i < NA; ++i)
-#pragma unroll
-                    for (int k = 0; k < NK; ++k) {
-                        if constexpr (HALF)
-                            sum[i][k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, g[b][i]),
-                                                                               __builtin_bit_cast(half8, q[k]), sum[i][k], 0, 0, 0);
-                        else
-                            sum[i][k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, g[b][i]),
-                                                                                __builtin_bit_cast(bf16x8, q[k]), sum[i][k], 0, 0, 0);
-                    }
+    constexpr int kProducts = 2 * kParts * NA * NK;
+    const auto product = [&](int n) {
+        const int h = n / (kProducts / 2), b = kParts - 1 - n / (NA * NK) % kParts, i = n / NK % NA, k = n % NK;
+        if constexpr (HALF)
+            sum[i][k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, g[h][b][i]), __builtin_bit_cast(half8, q[h][k]), sum[i][k], 0, 0, 0);
+        else
+            sum[i][k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, g[h][b][i]), __builtin_bit_cast(bf16x8, q[h][k]), sum[i][k], 0, 0, 0);
+    };
+    constexpr int kWork = 4 + 4 * kGroups, kPieces = kWork + 12;
+    const auto ask = [&](Raw& mine, int row, int n) {
+        if (n == 0) mine.of = {row, p.scales[row < 0 ? 0 : row]};
+        if (n < 4)
+            ask_numbers(mine, n);
+        else if (brings)
+            ask_gradients(mine, n - 4);
+    };
+    const auto piece = [&](Raw& mine, int8_t* buffer, int row, int n) {
+        if (n < 4) {
+            if (brings) split(mine, buffer, n * 2);
+        } else if (n < kWork) {
+            widen_numbers(mine, buffer, (n - 4) / 4, n % 4);
+        } else {
+            ask(mine, row, n - kWork);
         }
     };
     if (steps > 0) {
-        // What a step's loads need, its rows' numbers and scales, is asked for a step and two steps before them: nothing is waited for
-        // that has not been under way for a step.  (Steps behind the last have rows that do not count.)
+        // Steps asked for ahead of being laid down, and laid down ahead of being multiplied; a step's rows' numbers are asked for kAhead steps
+        // before its rows.  Nothing is waited for that has not been under way for kAhead steps, and nothing newer.
+        constexpr int kAhead = 2, kDown = kBuffers - 1;
         Raw raw[kAhead];
-        const auto with_scales = [&](int entry) {
-            const int row = entry < p.rows ? entry : -1;
-            return Rows{row, row < 0 ? 0.0f : p.scales[row]};
-        };
-        Rows next = with_scales(rows_of(0));
-        ask(raw[0], next);
-        lay_down(raw[0], 0);
+        int entry[kAhead];
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) ask(raw[j], with_scales(rows_of(1 + j)));
-        next = with_scales(rows_of(1 + kAhead));
-        int after = rows_of(2 + kAhead);
+        for (int t = 0; t < kDown; ++t) {
+            const int row = rows_of(t, entries_of(t));
+#pragma unroll
+            for (int n = 0; n < 12; ++n) ask(raw[0], row, n);
+            clear(raw[0]);
+#pragma unroll
+            for (int n = 0; n < kWork; ++n) piece(raw[0], s_buffer + t * kBytes, row, n);
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            const int row = rows_of(kDown + j, entries_of(kDown + j));
+#pragma unroll
+            for (int n = 0; n < 12; ++n) ask(raw[j], row, n);
+            entry[j] = entries_of(kDown + kAhead + j);
+        }
         meet();
-        for (int t = 0; t < steps; t += kAhead) {
+        int now = 0;                                                         // the buffer that is multiplied, in bytes
+        const auto following = [&](int buffer) { return buffer == (kBuffers - 1) * kBytes ? 0 : buffer + kBytes; };
+        if constexpr (kBuffers == 3) {
+#pragma unroll
+            for (int n = 0; n < kReads; ++n) fetch(s_buffer, 0, n);
+        }
+        for (int t0 = 0; t0 < steps; t0 += kAhead) {
 #pragma unroll
             for (int j = 0; j < kAhead; ++j) {
-                if (t + j >= steps) break;
-                const int now = kAhead == 2 ? j : t & 1;
-                lay_down(raw[j], now ^ 1);
-                ask(raw[j], next);
-                next = with_scales(after);
-                after = rows_of(t + j + 3 + kAhead);
-                multiply(now);
+                const int t = t0 + j;
+                if (t >= steps) break;
+                Raw& mine = raw[j];
+                const int row = rows_of(t + kDown + kAhead, entry[j]);
+                clear(mine);
+                if constexpr (kBuffers == 3) {
+                    int8_t* const down = s_buffer + following(following(now));
+                    // A wavefront's products and its other instructions run beside each other only if they come in turns, and LDS serves eight
+                    // wavefronts' reads beside the products only if they are spread over them.
+#pragma unroll
+                    for (int n = 0; n < kProducts; ++n) {
+                        __builtin_amdgcn_sched_barrier(0);
+                        product(n);
+                        if (n >= 3 && n < 3 + kReads) fetch(s_buffer + now, 1, n - 3);
+                        if (n >= kProducts - 4 - kReads && n < kProducts - 4) fetch(s_buffer + following(now), 0, n - (kProducts - 4 - kReads));
+#pragma unroll
+                        for (int w = 0; w < kPieces; ++w)
+                            if (w * (kProducts - 2) / kPieces + 1 == n) piece(mine, down, row, w);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                } else {
+#pragma unroll
+                    for (int n = 0; n < 2 * kReads; ++n) fetch(s_buffer + now, n / kReads, n % kReads);
+#pragma unroll
+                    for (int w = 0; w < kPieces; ++w) piece(mine, s_buffer + following(now), row, w);
+#pragma unroll
+                    for (int n = 0; n < kProducts; ++n) product(n);
+                }
+                entry[j] = entries_of(t + kDown + 2 * kAhead);
+                now = following(now);
                 meet();
             }
         }
     }
     if (sums) {
         // The four wavefronts that brought the gradients, one after another.
-        double* const s_bias = reinterpret_cast<double*>(&s_q[0][0]);
+        double* const s_bias = reinterpret_cast<double*>(&s_buffer[0]);
         for (int w = 0; w < 4; ++w) {
             if (wave == w && lane < kTA) {
                 if (w) bias += s_bias[lane];
@@ -1143,7 +1164,7 @@ template <typename T> void launch_product(const LinearArgs& p, hipStream_t s)
 template <typename T, int WA, int NA, int NK, bool HALF>
 void launch_gradient_tiles(const GradientArgs& p, hipStream_t s)
 {
-    const dim3 grid(blocks(p.A, 32 * WA * NA), blocks(p.H, 256), static_cast<unsigned>(p.slabs));
+    const dim3 grid(blocks(p.A, 32 * WA * NA), blocks(p.H, 32 * (8 / WA) * NK), static_cast<unsigned>(p.slabs));
     hipLaunchKernelGGL((ctc_weight_gradient_kernel<T, WA, NA, NK, HALF>), grid, dim3(512), 0, s, p);
 }
 template <typename T> void launch_gradient(const GradientArgs& p, const GradientPlan& plan, uint32_t* largest, hipStream_t s)
@@ -1154,10 +1175,8 @@ template <typename T> void launch_gradient(const GradientArgs& p, const Gradient
         launch_gradient_tiles<T, 1, 1, 1, false>(p, s);
     else if (plan.symbols == 64)
         launch_gradient_tiles<T, 1, 2, 1, false>(p, s);
-    else if (plan.symbols == 128)
-        launch_gradient_tiles<T, 4, 1, 4, true>(p, s);
     else
-        launch_gradient_tiles<T, 4, 2, 4, true>(p, s);
+        launch_gradient_tiles<T, 2, 2, 4, true>(p, s);
 }
 
 }  // namespace
