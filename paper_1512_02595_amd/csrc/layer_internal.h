@@ -30,9 +30,8 @@ constexpr int kColumnSlabs = 64;                // workgroups that look at one s
 struct GradientPlan {
     int symbols, columns;                       // of a tile: 32 or 64 by 256, 128 by 512
     int slabs;
-    bool columns_first;                         // a launch that finds the columns' largest, before
     int bias_slabs;
-    size_t bias_at, largest_at, bytes;          // places in the workspace, in floats; all of it, in bytes
+    size_t bias_at, largest_at, wide_at, bytes; // places in the workspace, in floats; all of it, in bytes
 };
 inline GradientPlan gradient_plan(int rows, int H, int A)
 {
@@ -54,11 +53,12 @@ inline GradientPlan gradient_plan(int rows, int H, int A)
             p.slabs = static_cast<int>(s);
         }
     }
-    p.columns_first = p.symbols >= 128;
-    p.bias_slabs = p.columns_first ? kColumnSlabs : p.slabs;
+    const bool wide = p.symbols == 128;         // the columns' largest, and the rows' numbers as fp16, come first
+    p.bias_slabs = wide ? kColumnSlabs : p.slabs;
     p.bias_at = p.slabs > 1 ? static_cast<size_t>(p.slabs) * A * H : 0;
     p.largest_at = p.bias_at + static_cast<size_t>(p.bias_slabs) * A;
-    p.bytes = (p.largest_at + (p.columns_first ? static_cast<size_t>(kColumnSlabs) * A : 0)) * 4;
+    p.wide_at = (p.largest_at + (wide ? static_cast<size_t>(kColumnSlabs) * A : 0) + 63) / 64 * 64;
+    p.bytes = (p.wide_at + (wide ? static_cast<size_t>(steps) * pitch_of(H) * 16 : 0)) * 4;
     return p;
 }
 

@@ -728,12 +728,11 @@ __device__ __forceinline__ int lift_of(uint32_t largest)
     return e == 255 ? 0 : e < 14 ? 127 : 141 - e;
 }
 
-// [first, last) of the list's entries for slab `slab` of `slabs`.
+// [first, last) of the list's entries for slab `slab` of `slabs`; slabs begin at multiples of 32.
 struct Range { int first, last; };
 __device__ __forceinline__ Range slab_of(int n, int slab, int slabs)
 {
-    const int per = (n + slabs - 1) / slabs;
-    const int64_t first = static_cast<int64_t>(slab) * per;
+    const int64_t per = ((n + 31LL) / 32 + slabs - 1) / slabs * 32, first = slab * per;
     return {static_cast<int>(first < n ? first : n), static_cast<int>(first + per < n ? first + per : n)};
 }
 
@@ -803,257 +802,182 @@ __global__ __launch_bounds__(256) void ctc_gradient_columns_kernel(GradientArgs 
     if (p.bias) p.bias[static_cast<int64_t>(slab) * p.A + mine] = static_cast<float>(total);
 }
 
-// 32 WA NA symbols by 32 WK NK columns to a workgroup of eight wavefronts, WA down the symbols and WK across, 32 NA by 32 NK to each; 32
-// rows a step.  In a step a wavefront multiplies one buffer of LDS, lays down the operands of the next step (where there are three
-// buffers, of the one after the next, so that the next one's first operands are fetched ahead of the barrier) and asks memory for what it
-// will lay down two steps later.
-// LDS: symbol a's 8-row piece j (16 bytes) lies at 64 a + 16 (j ^ a / 4 % 4); column k's at 64 (k % 4 * columns / 4 + k / 4) + 16 (j ^ k % 4 ^
-// k / 16 % 4): what lanes write or read at once then falls on different banks.
-// v_mfma_f32_32x32x16_{f16,bf16}: lane l gives numbers 8 (l / 32) .. of row l % 32 of either operand, and holds rows
-// 8 (v / 4) + 4 (l / 32) + v % 4, v < 16, of column l % 32 of the result.
-template <typename T, int WA, int NA, int NK, bool HALF>
-__global__ __launch_bounds__(512) void ctc_weight_gradient_kernel(GradientArgs p)
-{
-    constexpr int WK = 8 / WA, kTA = 32 * WA * NA, kTK = 32 * WK * NK, kParts = HALF ? 2 : 3, kBuffers = HALF ? 3 : 2, kGroups = kTK / 256;
-    static_assert(kTA <= 128 && kTK % 256 == 0);
-    constexpr int kPartBytes = kTA * 64, kNumbers = kParts * kPartBytes, kBytes = kNumbers + kTK * 64;       // gradients, then whole numbers
-    __shared__ __align__(1024) int8_t s_buffer[kBuffers * kBytes];
-    __shared__ int s_lift[HALF ? kTA : 1];
-    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int a0 = blockIdx.x * kTA, k0 = blockIdx.y * kTK, slab = blockIdx.z;
-    const Range range = slab_of(listed(p.frames, p.rows), slab, p.slabs);
-    const int steps = (range.last - range.first + 31) / 32;
-
-    // What this lane brings: symbol `symbol` of rows 8 (wave % 4) .., columns 4 lane .. (and 256 on) of rows 4 wave ..
-    const bool brings = kTA == 128 || (wave < 4 && lane < kTA);
-    const int symbol = kTA == 128 ? wave / 4 * 64 + lane : lane;
-    float lift = 1.0f;
-    if constexpr (HALF) {
-        if (static_cast<int>(threadIdx.x) < kTA) {
-            uint32_t most = 0;
-            if (a0 + static_cast<int>(threadIdx.x) < p.A)
-#pragma unroll 16
-                for (int b = 0; b < kColumnSlabs; ++b) {
-                    const uint32_t m = p.largest[static_cast<int64_t>(b) * p.A + a0 + threadIdx.x];
-                    most = most > m ? most : m;
-                }
-            s_lift[threadIdx.x] = lift_of(most);
-        }
-        __syncthreads();
-        lift = ldexpf(1.0f, s_lift[symbol]);
-    }
-    // (symbols behind the last and columns behind a row's bytes are others' once more: what becomes of them is not written)
-    const uint32_t at = static_cast<uint32_t>(a0 + symbol < p.A ? a0 + symbol : p.A - 1) * static_cast<uint32_t>(sizeof(T));
-    uint32_t column[kGroups];
-#pragma unroll
-    for (int c = 0; c < kGroups; ++c) {
-        const int k = k0 + 256 * c + 4 * lane;
-        column[c] = k < p.pitch ? k : 0;
-    }
-
-    // A step's rows, as the list has them, and their scales, a lane each; what does not count has scale 0 and, once they are there, gradients 0.
-    // (Steps behind the last have rows that do not count; every index is one of the list's, every address a row's.)
-    struct Rows { int entry; float scale; };
-    const int32_t* const entries = p.frames ? p.frames + 1 : reinterpret_cast<const int32_t*>(p.scales);
-    const auto entries_of = [&](int step) {
+// A step's rows, as the list has them; -1: does not count.  (Steps behind the last have rows that do not count; every index is one of the
+// list's, every address a row's.)  The entry is asked for early and looked at late.
+struct StepRows {
+    const int32_t* entries;
+    bool list;
+    int rows;
+    Range range;
+    int lane;
+    __device__ __forceinline__ StepRows(const GradientArgs& p, Range r, int l)
+        : entries(p.frames ? p.frames + 1 : reinterpret_cast<const int32_t*>(p.scales)), list(p.frames), rows(p.rows), range(r), lane(l) {}
+    __device__ __forceinline__ int ask(int step) const
+    {
         const int i = range.first + step * 32 + lane % 32;
         return entries[i < range.last ? i : range.last - 1];
-    };
-    const auto rows_of = [&](int step, int entry) {                          // (for the entries that entries_of gave)
+    }
+    __device__ __forceinline__ int row(int step, int entry) const
+    {
         const int i = range.first + step * 32 + lane % 32;
-        const int r = p.frames ? entry : i;
-        return i < range.last && r >= 0 && r < p.rows ? r : -1;
-    };
+        const int r = list ? entry : i;
+        return i < range.last && r >= 0 && r < rows ? r : -1;
+    }
+};
+
+// Gradients of one symbol in eight rows, as they are in memory; the rows, and their scales, a lane each.
+struct Eight {
+    int row;
+    float scale;
+    uint32_t g[8];
+};
+// Row `row`'s gradient of the symbol at `at` bytes.
+template <typename T> __device__ __forceinline__ uint32_t gradient_of(const GradientArgs& p, int row, uint32_t at)
+{
+    const char* from = static_cast<const char*>(p.grads) + static_cast<uint64_t>(row < 0 ? 0 : row) * (static_cast<uint32_t>(p.A) * sizeof(T));
+    if constexpr (sizeof(T) == 2)
+        return *reinterpret_cast<const uint16_t*>(from + at);
+    else
+        return *reinterpret_cast<const uint32_t*>(from + at);
+}
+template <typename T> __device__ __forceinline__ float gradient_in(uint32_t bits) { return __uint_as_float(sizeof(T) == 2 ? bits << 16 : bits); }
+// Gradients and scales of rows that do not count: 0, whatever is there.
+__device__ __forceinline__ void clear(Eight& e, int first)
+{
+    if (__ballot(e.row >= 0) == ~0ull) return;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (__builtin_amdgcn_readlane(e.row, first + j) < 0) e.g[j] = 0;
+    if (e.row < 0) e.scale = 0.0f;
+}
+__device__ __forceinline__ float scale_of(const Eight& e, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(e.scale), lane)); }
+
+// At most 64 symbols.  32 NA symbols by 256 columns to a workgroup of eight wavefronts, 32 NA by 32 to each; 32 rows a step, in two buffers of
+// LDS: in a step a wavefront lays down the next step's operands, asks memory for what it will lay down kAhead steps later, and multiplies.
+// LDS: symbol a's 8-row piece j (16 bytes) lies at 64 a + 16 (j ^ a / 4 % 4); column k's at 64 (64 (k % 4) + k / 4) + 16 (j ^ k % 4 ^ k / 16 % 4):
+// what lanes write or read at once then falls on different banks.
+// v_mfma_f32_32x32x16_{f16,bf16}: lane l gives numbers 8 (l / 32) .. of row l % 32 of either operand, and holds rows
+// 8 (v / 4) + 4 (l / 32) + v % 4, v < 16, of column l % 32 of the result.
+template <typename T, int NA>
+__global__ __launch_bounds__(512) void ctc_weight_gradient_narrow_kernel(GradientArgs p)
+{
+    constexpr int kTA = 32 * NA, kPartBytes = kTA * 64, kNumbers = 3 * kPartBytes, kBytes = kNumbers + 256 * 64, kAhead = 2;
+    __shared__ __align__(1024) int8_t s_buffer[2][kBytes];
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int k0 = blockIdx.y * 256, slab = blockIdx.z, chunk = wave % 4 * 8;
+    const Range range = slab_of(listed(p.frames, p.rows), slab, p.slabs);
+    const int steps = (range.last - range.first + 31) / 32;
+    const StepRows list(p, range, lane);
+    // What this lane brings: symbol `lane` of rows `chunk` .. (four wavefronts), columns 4 lane .. of rows 4 wave ..  (Symbols behind the
+    // last and columns behind a row's bytes are others' once more: what becomes of them is not written.)
+    const bool brings = wave < 4 && lane < kTA;
+    const uint32_t at = static_cast<uint32_t>(lane < p.A ? lane : p.A - 1) * static_cast<uint32_t>(sizeof(T));
+    const uint32_t column = static_cast<uint32_t>(k0 + 4 * lane < p.pitch ? k0 + 4 * lane : 0);
     struct Raw {
-        Rows of;
-        uint32_t g[8];
-        uint32_t q[4][kGroups];
+        Eight e;
+        uint32_t q[4];
     };
-    // The work on a step's operands, in pieces that the products are put between.
-    // Loads of the whole numbers' rows and of the gradients' rows:
-    const auto ask_numbers = [&](Raw& to, int j) {
-        const int r = __builtin_amdgcn_readlane(to.of.entry, wave * 4 + j);
-        const int8_t* from = p.q + static_cast<uint64_t>(r < 0 ? 0 : r) * static_cast<uint32_t>(p.pitch);
+    const auto ask = [&](Raw& to, int row) {
+        to.e.row = row;
+        to.e.scale = p.scales[row < 0 ? 0 : row];
 #pragma unroll
-        for (int c = 0; c < kGroups; ++c) to.q[j][c] = *reinterpret_cast<const uint32_t*>(from + column[c]);
-    };
-    const auto ask_gradients = [&](Raw& to, int j) {
-        const int r = __builtin_amdgcn_readlane(to.of.entry, wave % 4 * 8 + j);
-        const char* from = static_cast<const char*>(p.grads) + static_cast<uint64_t>(r < 0 ? 0 : r) * (static_cast<uint32_t>(p.A) * sizeof(T));
-        if constexpr (sizeof(T) == 2)
-            to.g[j] = *reinterpret_cast<const uint16_t*>(from + at);
-        else
-            to.g[j] = *reinterpret_cast<const uint32_t*>(from + at);
-    };
-    // Gradients of rows that do not count: none, whatever is there.
-    const auto clear = [&](Raw& from) {
-        if (__ballot(from.of.entry >= 0) == ~0ull) return;
+        for (int j = 0; j < 4; ++j) {
+            const int r = __builtin_amdgcn_readlane(row, wave * 4 + j);
+            to.q[j] = *reinterpret_cast<const uint32_t*>(p.q + static_cast<uint64_t>(r < 0 ? 0 : r) * static_cast<uint32_t>(p.pitch) + column);
+        }
+        if (brings) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (__builtin_amdgcn_readlane(from.of.entry, wave % 4 * 8 + j) < 0) from.g[j] = 0;
-        from.of.scale = from.of.entry < 0 ? 0.0f : from.of.scale;
+            for (int j = 0; j < 8; ++j) to.e.g[j] = gradient_of<T>(p, __builtin_amdgcn_readlane(row, chunk + j), at);
+        }
     };
     double bias = 0.0;
-    const bool sums = !HALF && p.bias && blockIdx.y == 0;
-    // Two rows' gradients, split, and the write of eight rows' parts with the last of them:
-    uint4v part[kParts];
-    const auto split = [&](const Raw& from, int8_t* buffer, int j) {
-        float g[2], scale[2];
+    const bool sums = p.bias && blockIdx.y == 0;
+    const auto lay_down = [&](Raw& from, int8_t* buffer) {
+        clear(from.e, chunk);
+        if (brings) {
+            uint4v part[3];
+            float eight = 0.0f;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            g[e] = __uint_as_float(sizeof(T) == 2 ? from.g[j + e] << 16 : from.g[j + e]);
-            scale[e] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(from.of.scale), wave % 4 * 8 + j + e));
-            if (sums) bias += static_cast<double>(g[e]);
-        }
-        if constexpr (HALF) {
-            const float c[2] = {g[0] * scale[0] * lift, g[1] * scale[1] * lift};
-            const half2 high = {static_cast<_Float16>(c[0]), static_cast<_Float16>(c[1])};
-            const half2 low = {static_cast<_Float16>(c[0] - static_cast<float>(high[0])),
-                               static_cast<_Float16>(c[1] - static_cast<float>(high[1]))};
-            part[0][j / 2] = __builtin_bit_cast(uint32_t, high);
-            part[1][j / 2] = __builtin_bit_cast(uint32_t, low);
-        } else {
-            float c[2] = {g[0] * scale[0], g[1] * scale[1]};
+            for (int j = 0; j < 8; j += 2) {
+                float c[2];
 #pragma unroll
-            for (int b = 0; b < 3; ++b) {
-                const uint32_t u = __float_as_uint(c[0]), v = __float_as_uint(c[1]);
-                part[b][j / 2] = __builtin_amdgcn_perm(v, u, 0x07060302);                     // the leading halves of both
-                c[0] -= __uint_as_float(u & 0xffff0000u);
-                c[1] -= __uint_as_float(v & 0xffff0000u);
+                for (int i = 0; i < 2; ++i) {
+                    const float g = gradient_in<T>(from.e.g[j + i]);
+                    eight += g;
+                    c[i] = g * scale_of(from.e, chunk + j + i);
+                }
+#pragma unroll
+                for (int b = 0; b < 3; ++b) {
+                    const uint32_t u = __float_as_uint(c[0]), v = __float_as_uint(c[1]);
+                    part[b][j / 2] = __builtin_amdgcn_perm(v, u, 0x07060302);                 // the leading halves of both
+                    c[0] -= __uint_as_float(u & 0xffff0000u);
+                    c[1] -= __uint_as_float(v & 0xffff0000u);
+                }
             }
+            if (sums) bias += static_cast<double>(eight);
+#pragma unroll
+            for (int b = 0; b < 3; ++b)
+                *reinterpret_cast<uint4v*>(buffer + b * kPartBytes + lane * 64 + ((wave % 4 ^ lane / 4 % 4) * 16)) = part[b];
         }
-        if (j != 6) return;
-        const int to = symbol * 64 + ((wave % 4 ^ symbol / 4 % 4) * 16);
 #pragma unroll
-        for (int b = 0; b < kParts; ++b) *reinterpret_cast<uint4v*>(buffer + b * kPartBytes + to) = part[b];
-    };
-    // Four rows' whole numbers of column 256 c + 4 lane + k:
-    const auto widen_numbers = [&](const Raw& from, int8_t* buffer, int c, int k) {
-        uint2v four;
+        for (int k = 0; k < 4; ++k) {
+            uint2v four;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const uint32_t x = from.q[2 * j][c], y = from.q[2 * j + 1][c];
-            if constexpr (HALF) {
-                // byte k of either, 128 more, behind 0x64: 1024 + 128 + the number, as fp16
-                const uint32_t bytes = __builtin_amdgcn_perm(y ^ 0x80808080u, x ^ 0x80808080u, 0x0c040c00u + 0x00010001u * k) | 0x64006400u;
-                const half2 offset = {static_cast<_Float16>(-1152.0f), static_cast<_Float16>(-1152.0f)};
-                four[j] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2, bytes) + offset);
-            } else {
-                const float u = static_cast<float>(static_cast<int8_t>(x >> 8 * k)), v = static_cast<float>(static_cast<int8_t>(y >> 8 * k));
+            for (int j = 0; j < 2; ++j) {
+                const float u = static_cast<float>(static_cast<int8_t>(from.q[2 * j] >> 8 * k));
+                const float v = static_cast<float>(static_cast<int8_t>(from.q[2 * j + 1] >> 8 * k));
                 four[j] = __builtin_amdgcn_perm(__float_as_uint(v), __float_as_uint(u), 0x07060302);
             }
-        }
-        *reinterpret_cast<uint2v*>(buffer + kNumbers + (k * (kTK / 4) + c * 64 + lane) * 64 + ((wave / 2 ^ k ^ lane / 4 % 4) * 16) + wave % 2 * 8) = four;
-    };
-
-    const int wave_a = wave / WK, wave_k = wave % WK;
-    float16v sum[NA][NK] = {};
-    uint4v g[2][kParts][NA], q[2][NK];
-    constexpr int kReads = NK + kParts * NA;
-    const auto fetch = [&](const int8_t* buffer, int h, int n) {             // (the n-th of a half's reads, in the order of the products)
-        if (n < NK) {
-            const int first = wave_k * NK + n, piece = (h * 2 + lane / 32) ^ lane % 4 ^ (first % 2 * 2 + lane % 32 / 16);
-            q[h][n] = *reinterpret_cast<const uint4v*>(buffer + kNumbers + (lane % 4 * (kTK / 4) + first * 8 + lane % 32 / 4) * 64 + piece * 16);
-        } else {
-            const int b = kParts - 1 - (n - NK) / NA, i = (n - NK) % NA;
-            g[h][b][i] = *reinterpret_cast<const uint4v*>(
-                buffer + b * kPartBytes + ((wave_a * NA + i) * 32 + lane % 32) * 64 + (((h * 2 + lane / 32) ^ lane / 4 % 4) * 16));
+            *reinterpret_cast<uint2v*>(buffer + kNumbers + (k * 64 + lane) * 64 + ((wave / 2 ^ k ^ lane / 4 % 4) * 16) + wave % 2 * 8) = four;
         }
     };
-    constexpr int kProducts = 2 * kParts * NA * NK;
-    const auto product = [&](int n) {
-        const int h = n / (kProducts / 2), b = kParts - 1 - n / (NA * NK) % kParts, i = n / NK % NA, k = n % NK;
-        if constexpr (HALF)
-            sum[i][k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, g[h][b][i]), __builtin_bit_cast(half8, q[h][k]), sum[i][k], 0, 0, 0);
-        else
-            sum[i][k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, g[h][b][i]), __builtin_bit_cast(bf16x8, q[h][k]), sum[i][k], 0, 0, 0);
-    };
-    constexpr int kWork = 4 + 4 * kGroups, kPieces = kWork + 12;
-    const auto ask = [&](Raw& mine, int row, int n) {
-        if (n == 0) mine.of = {row, p.scales[row < 0 ? 0 : row]};
-        if (n < 4)
-            ask_numbers(mine, n);
-        else if (brings)
-            ask_gradients(mine, n - 4);
-    };
-    const auto piece = [&](Raw& mine, int8_t* buffer, int row, int n) {
-        if (n < 4) {
-            if (brings) split(mine, buffer, n * 2);
-        } else if (n < kWork) {
-            widen_numbers(mine, buffer, (n - 4) / 4, n % 4);
-        } else {
-            ask(mine, row, n - kWork);
+    float16v sum[NA] = {};
+    const auto multiply = [&](const int8_t* buffer) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int piece = (h * 2 + lane / 32) ^ lane % 4 ^ (wave % 2 * 2 + lane % 32 / 16);
+            const bf16x8 q = *reinterpret_cast<const bf16x8*>(buffer + kNumbers + (lane % 4 * 64 + wave * 8 + lane % 32 / 4) * 64 + piece * 16);
+            bf16x8 g[3][NA];
+#pragma unroll
+            for (int b = 0; b < 3; ++b)
+#pragma unroll
+                for (int i = 0; i < NA; ++i)
+                    g[b][i] = *reinterpret_cast<const bf16x8*>(buffer + b * kPartBytes + (i * 32 + lane % 32) * 64 + (((h * 2 + lane / 32) ^ lane / 4 % 4) * 16));
+#pragma unroll
+            for (int b = 2; b >= 0; --b)
+#pragma unroll
+                for (int i = 0; i < NA; ++i) sum[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(g[b][i], q, sum[i], 0, 0, 0);
         }
     };
     if (steps > 0) {
-        // Steps asked for ahead of being laid down, and laid down ahead of being multiplied; a step's rows' numbers are asked for kAhead steps
-        // before its rows.  Nothing is waited for that has not been under way for kAhead steps, and nothing newer.
-        constexpr int kAhead = 2, kDown = kBuffers - 1;
+        // A step's rows' numbers are asked for kAhead steps before its rows, these kAhead steps before they are laid down: nothing is waited for
+        // that has not been under way as long.
         Raw raw[kAhead];
         int entry[kAhead];
-#pragma unroll
-        for (int t = 0; t < kDown; ++t) {
-            const int row = rows_of(t, entries_of(t));
-#pragma unroll
-            for (int n = 0; n < 12; ++n) ask(raw[0], row, n);
-            clear(raw[0]);
-#pragma unroll
-            for (int n = 0; n < kWork; ++n) piece(raw[0], s_buffer + t * kBytes, row, n);
-        }
+        ask(raw[0], list.row(0, list.ask(0)));
+        lay_down(raw[0], s_buffer[0]);
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
-            const int row = rows_of(kDown + j, entries_of(kDown + j));
-#pragma unroll
-            for (int n = 0; n < 12; ++n) ask(raw[j], row, n);
-            entry[j] = entries_of(kDown + kAhead + j);
+            ask(raw[j], list.row(1 + j, list.ask(1 + j)));
+            entry[j] = list.ask(1 + kAhead + j);
         }
         meet();
-        int now = 0;                                                         // the buffer that is multiplied, in bytes
-        const auto following = [&](int buffer) { return buffer == (kBuffers - 1) * kBytes ? 0 : buffer + kBytes; };
-        if constexpr (kBuffers == 3) {
-#pragma unroll
-            for (int n = 0; n < kReads; ++n) fetch(s_buffer, 0, n);
-        }
         for (int t0 = 0; t0 < steps; t0 += kAhead) {
 #pragma unroll
             for (int j = 0; j < kAhead; ++j) {
                 const int t = t0 + j;
                 if (t >= steps) break;
-                Raw& mine = raw[j];
-                const int row = rows_of(t + kDown + kAhead, entry[j]);
-                clear(mine);
-                if constexpr (kBuffers == 3) {
-                    int8_t* const down = s_buffer + following(following(now));
-                    // A wavefront's products and its other instructions run beside each other only if they come in turns, and LDS serves eight
-                    // wavefronts' reads beside the products only if they are spread over them.
-#pragma unroll
-                    for (int n = 0; n < kProducts; ++n) {
-                        __builtin_amdgcn_sched_barrier(0);
-                        product(n);
-                        if (n >= 3 && n < 3 + kReads) fetch(s_buffer + now, 1, n - 3);
-                        if (n >= kProducts - 4 - kReads && n < kProducts - 4) fetch(s_buffer + following(now), 0, n - (kProducts - 4 - kReads));
-#pragma unroll
-                        for (int w = 0; w < kPieces; ++w)
-                            if (w * (kProducts - 2) / kPieces + 1 == n) piece(mine, down, row, w);
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                } else {
-#pragma unroll
-                    for (int n = 0; n < 2 * kReads; ++n) fetch(s_buffer + now, n / kReads, n % kReads);
-#pragma unroll
-                    for (int w = 0; w < kPieces; ++w) piece(mine, s_buffer + following(now), row, w);
-#pragma unroll
-                    for (int n = 0; n < kProducts; ++n) product(n);
-                }
-                entry[j] = entries_of(t + kDown + 2 * kAhead);
-                now = following(now);
+                lay_down(raw[j], s_buffer[j % 2 ^ 1]);
+                ask(raw[j], list.row(t + 1 + kAhead, entry[j]));
+                entry[j] = list.ask(t + 1 + 2 * kAhead);
+                multiply(s_buffer[j % 2]);
                 meet();
             }
         }
     }
     if (sums) {
         // The four wavefronts that brought the gradients, one after another.
-        double* const s_bias = reinterpret_cast<double*>(&s_buffer[0]);
+        double* const s_bias = reinterpret_cast<double*>(&s_buffer[0][0]);
         for (int w = 0; w < 4; ++w) {
             if (wave == w && lane < kTA) {
                 if (w) bias += s_bias[lane];
@@ -1061,20 +985,190 @@ __global__ __launch_bounds__(512) void ctc_weight_gradient_kernel(GradientArgs p
             }
             __syncthreads();
         }
-        if (wave == 3 && lane < kTA && a0 + lane < p.A) p.bias[static_cast<int64_t>(slab) * p.A + a0 + lane] = static_cast<float>(bias);
+        if (wave == 3 && lane < p.A) p.bias[static_cast<int64_t>(slab) * p.A + lane] = static_cast<float>(bias);
     }
     float* const out = p.out + static_cast<int64_t>(slab) * p.A * p.H;
+    const int k = k0 + wave * 32 + lane % 32;
 #pragma unroll
     for (int i = 0; i < NA; ++i)
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
-            const int s = (wave_a * NA + i) * 32 + 8 * (v / 4) + 4 * (lane / 32) + v % 4;
-            if (a0 + s >= p.A) continue;
-            float* const row = out + static_cast<int64_t>(a0 + s) * p.H;
+            const int a = i * 32 + 8 * (v / 4) + 4 * (lane / 32) + v % 4;
+            if (a < p.A && k < p.H) out[static_cast<int64_t>(a) * p.H + k] = sum[i][v];
+        }
+}
+
+// More than 64 symbols: the whole numbers of the listed rows as fp16, once for all symbols' workgroups.  32 listed rows at a time (a step), for each
+// column k 64 bytes, its 8-row pieces in the order j ^ k / 4 % 4: as the kernel below wants them in LDS.  256 columns to a workgroup.
+__global__ __launch_bounds__(256) void ctc_widen_rows_kernel(GradientArgs p, uint16_t* wide)
+{
+    __shared__ __align__(16) int8_t s_row[32][256 + 4];
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int n = listed(p.frames, p.rows), k0 = blockIdx.y * 256;
+    if (static_cast<int64_t>(blockIdx.x) * 32 >= n) return;
+    const StepRows list(p, {0, n}, lane);
+    const int row = list.row(blockIdx.x, list.ask(blockIdx.x));
+    if (k0 + 4 * lane < p.pitch) {
 #pragma unroll
-            for (int k = 0; k < NK; ++k) {
-                const int c = k0 + (wave_k * NK + k) * 32 + lane % 32;
-                if (c < p.H) row[c] = HALF ? ldexpf(sum[i][k][v], -s_lift[HALF ? s : 0]) : sum[i][k][v];
+        for (int j = 0; j < 8; ++j) {
+            const int r = __builtin_amdgcn_readlane(row, wave * 8 + j);
+            *reinterpret_cast<uint32_t*>(&s_row[wave * 8 + j][4 * lane]) =
+                *reinterpret_cast<const uint32_t*>(p.q + static_cast<uint64_t>(r < 0 ? 0 : r) * static_cast<uint32_t>(p.pitch) + k0 + 4 * lane);
+        }
+    }
+    __syncthreads();
+    const int k = threadIdx.x;
+    if (k0 + k >= p.pitch) return;
+    uint16_t* const to = wide + (static_cast<int64_t>(blockIdx.x) * p.pitch + k0 + k) * 32;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        half8 piece;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) piece[i] = static_cast<_Float16>(static_cast<float>(s_row[j * 8 + i][k]));
+        *reinterpret_cast<half8*>(to + (j ^ k / 4 % 4) * 8) = piece;
+    }
+}
+
+// 128 symbols by 512 columns to a workgroup of eight wavefronts, 64 by 128 to each; 32 rows a step, in three buffers of LDS.  The barrier is in
+// a step's middle, when every wavefront has the operands of its second half in registers: behind it the step's buffer of whole numbers is filled, from
+// memory, for three steps on, and the next step's first operands are fetched.  Gradients pass through registers: asked for three steps before they
+// are split and laid down, two steps before they are multiplied.
+// LDS: piece j of symbol a lies at 64 a + 16 (j ^ a / 4 % 4), and so for columns: eight lanes' reads of a piece meet different banks.
+template <typename T>
+__global__ __launch_bounds__(512) void ctc_weight_gradient_wide_kernel(GradientArgs p, const uint16_t* wide)
+{
+    constexpr int kTA = 128, kTK = 512, kPartBytes = kTA * 64;
+    // (six arrays and not one: the compiler waits for what fills an array from memory before it lets anybody use it)
+    __shared__ __align__(1024) int8_t s_g0[2 * kPartBytes];
+    __shared__ __align__(1024) int8_t s_g1[2 * kPartBytes];
+    __shared__ __align__(1024) int8_t s_g2[2 * kPartBytes];
+    __shared__ __align__(1024) int8_t s_q0[kTK * 64];
+    __shared__ __align__(1024) int8_t s_q1[kTK * 64];
+    __shared__ __align__(1024) int8_t s_q2[kTK * 64];
+    int8_t* const s_g[3] = {s_g0, s_g1, s_g2};
+    int8_t* const s_q[3] = {s_q0, s_q1, s_q2};
+    __shared__ int s_lift[kTA];
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int a0 = blockIdx.x * kTA, k0 = blockIdx.y * kTK, slab = blockIdx.z, chunk = wave % 4 * 8;
+    const Range range = slab_of(listed(p.frames, p.rows), slab, p.slabs);
+    const int steps = (range.last - range.first + 31) / 32;
+    const StepRows list(p, range, lane);
+    if (static_cast<int>(threadIdx.x) < kTA) {
+        uint32_t most = 0;
+        if (a0 + static_cast<int>(threadIdx.x) < p.A)
+#pragma unroll 16
+            for (int b = 0; b < kColumnSlabs; ++b) {
+                const uint32_t m = p.largest[static_cast<int64_t>(b) * p.A + a0 + threadIdx.x];
+                most = most > m ? most : m;
+            }
+        s_lift[threadIdx.x] = lift_of(most);
+    }
+    __syncthreads();
+    // What this lane brings: symbol `symbol` of rows `chunk` .., and a sixty-fourth of four KiB of whole numbers.  (Symbols behind the last and
+    // columns behind a row's bytes are others' once more: what becomes of them is not written.)
+    const int symbol = wave / 4 * 64 + lane;
+    const float lift = ldexpf(1.0f, s_lift[symbol]);
+    const uint32_t at = static_cast<uint32_t>(a0 + symbol < p.A ? a0 + symbol : p.A - 1) * static_cast<uint32_t>(sizeof(T));
+    const int8_t* numbers = reinterpret_cast<const int8_t*>(wide) + static_cast<int64_t>(range.first / 32) * p.pitch * 64;
+    const uint32_t step_bytes = static_cast<uint32_t>(p.pitch) * 64, lane_bytes = lane * 16;
+    // (behind a slab's last step that step's once more: multiplied by gradients that are 0, or by nobody)
+    const auto fill = [&](int buffer, int step, int j) {
+        const int k = k0 + (j * 8 + wave) * 16;
+        to_lds(numbers + (k < p.pitch ? k : 0) * 64 + lane_bytes, s_q[buffer] + (j * 8 + wave) * 1024);
+        if (j == 3) numbers += step + 1 < steps ? step_bytes : 0;
+    };
+    uint4v part[2];
+    // Two rows' gradients, split, and the write of eight rows' parts with the last of them.
+    const auto split = [&](const Eight& e, int buffer, int j) {
+        const float c[2] = {gradient_in<T>(e.g[j]) * scale_of(e, chunk + j) * lift, gradient_in<T>(e.g[j + 1]) * scale_of(e, chunk + j + 1) * lift};
+        const half2 high = {static_cast<_Float16>(c[0]), static_cast<_Float16>(c[1])};
+        const half2 low = {static_cast<_Float16>(c[0] - static_cast<float>(high[0])), static_cast<_Float16>(c[1] - static_cast<float>(high[1]))};
+        part[0][j / 2] = __builtin_bit_cast(uint32_t, high);
+        part[1][j / 2] = __builtin_bit_cast(uint32_t, low);
+        if (j != 6) return;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) *reinterpret_cast<uint4v*>(s_g[buffer] + b * kPartBytes + symbol * 64 + ((wave % 4 ^ lane / 4 % 4) * 16)) = part[b];
+    };
+    const int wave_a = wave / 4, wave_k = wave % 4;
+    float16v sum[2][4] = {};
+    half8 g[2][2][2], q[2][4];
+    const auto fetch = [&](int buffer, int h, int n) {                       // (the n-th of a half's eight reads, in the order of the products)
+        const int piece = ((h * 2 + lane / 32) ^ lane / 4 % 4) * 16;
+        if (n < 4)
+            q[h][n] = *reinterpret_cast<const half8*>(s_q[buffer] + ((wave_k * 4 + n) * 32 + lane % 32) * 64 + piece);
+        else
+            g[h][1 - (n - 4) / 2][n % 2] = *reinterpret_cast<const half8*>(s_g[buffer] + (1 - (n - 4) / 2) * kPartBytes + ((wave_a * 2 + n % 2) * 32 + lane % 32) * 64 + piece);
+    };
+    const auto product = [&](int n) {
+        const int h = n / 16, b = 1 - n / 8 % 2, i = n / 4 % 2, k = n % 4;
+        sum[i][k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(g[h][b][i], q[h][k], sum[i][k], 0, 0, 0);
+    };
+    if (steps > 0) {
+        // (A step's rows' numbers are asked for three steps before its rows.)
+        Eight raw[3];
+        int entry[3];
+        const auto ask = [&](Eight& e, int j) { e.g[j] = gradient_of<T>(p, __builtin_amdgcn_readlane(e.row, chunk + j), at); };
+        const auto rows = [&](Eight& e, int row) { e.row = row, e.scale = p.scales[row < 0 ? 0 : row]; };
+#pragma unroll
+        for (int t = 0; t < 3; ++t) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) fill(t, t, j);
+            if (t == 2) break;
+            rows(raw[t], list.row(t, list.ask(t)));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) ask(raw[t], j);
+            clear(raw[t], chunk);
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) split(raw[t], t, j);
+        }
+#pragma unroll
+        for (int j = 0; j < 3; ++j) {
+            rows(raw[j], list.row(2 + j, list.ask(2 + j)));
+#pragma unroll
+            for (int i = 0; i < 8; ++i) ask(raw[j], i);
+            entry[j] = list.ask(5 + j);
+        }
+        wait_and_meet<0>();
+#pragma unroll
+        for (int n = 0; n < 8; ++n) fetch(0, 0, n);
+        for (int t0 = 0; t0 < steps; t0 += 3) {
+#pragma unroll
+            for (int s = 0; s < 3; ++s) {
+                const int t = t0 + s;
+                if (t >= steps) break;
+                const int now = s, next = (s + 1) % 3, down = (s + 2) % 3;
+                Eight& mine = raw[s];
+                clear(mine, chunk);
+                const int row = list.row(t + 5, entry[s]);
+                // A wavefront's products and its other instructions run beside each other only if they come in turns, and LDS serves eight wavefronts'
+                // reads beside the products only if they are spread over them.
+#pragma unroll
+                for (int n = 0; n < 32; ++n) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    product(n);
+                    if (n >= 2 && n < 10) fetch(now, 1, n - 2);
+                    if (n >= 2 && n < 18 && n % 4 == 2) split(mine, down, n / 2 - 1);
+                    if (n == 13) wait_and_meet<24>();   // (the next step's numbers are there: 24 requests came after theirs, 14 in each step)
+                    if (n >= 14 && n < 18) fill(now, t + 3, n - 14);
+                    if (n == 18) rows(mine, row);
+                    if (n >= 20 && n < 28) fetch(next, 0, n - 20), ask(mine, n - 20);
+                    if (n == 28) entry[s] = list.ask(t + 8);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    }
+    float* const out = p.out + static_cast<int64_t>(slab) * p.A * p.H;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const int a = (wave_a * 2 + i) * 32 + 8 * (v / 4) + 4 * (lane / 32) + v % 4;
+            const int lower = -s_lift[a];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int c = k0 + (wave_k * 4 + k) * 32 + lane % 32;
+                if (a0 + a < p.A && c < p.H) out[static_cast<int64_t>(a0 + a) * p.H + c] = ldexpf(sum[i][k][v], lower);
             }
         }
 }
@@ -1161,22 +1255,20 @@ template <typename T> void launch_product(const LinearArgs& p, hipStream_t s)
         launch_tiles<T, 4, 4>(p, s);
 }
 
-template <typename T, int WA, int NA, int NK, bool HALF>
-void launch_gradient_tiles(const GradientArgs& p, hipStream_t s)
+template <typename T> void launch_gradient(const GradientArgs& p, const GradientPlan& plan, float* workspace, hipStream_t s)
 {
-    const dim3 grid(blocks(p.A, 32 * WA * NA), blocks(p.H, 32 * (8 / WA) * NK), static_cast<unsigned>(p.slabs));
-    hipLaunchKernelGGL((ctc_weight_gradient_kernel<T, WA, NA, NK, HALF>), grid, dim3(512), 0, s, p);
-}
-template <typename T> void launch_gradient(const GradientArgs& p, const GradientPlan& plan, uint32_t* largest, hipStream_t s)
-{
-    if (plan.columns_first)
-        hipLaunchKernelGGL(ctc_gradient_columns_kernel<T>, dim3(blocks(p.A, 2 * kWave), kColumnSlabs), dim3(256), 0, s, p, largest);
-    if (plan.symbols == 32)
-        launch_gradient_tiles<T, 1, 1, 1, false>(p, s);
-    else if (plan.symbols == 64)
-        launch_gradient_tiles<T, 1, 2, 1, false>(p, s);
-    else
-        launch_gradient_tiles<T, 2, 2, 4, true>(p, s);
+    const dim3 grid(blocks(p.A, plan.symbols), blocks(p.H, plan.columns), static_cast<unsigned>(p.slabs));
+    if (plan.symbols == 32) {
+        hipLaunchKernelGGL((ctc_weight_gradient_narrow_kernel<T, 1>), grid, dim3(512), 0, s, p);
+    } else if (plan.symbols == 64) {
+        hipLaunchKernelGGL((ctc_weight_gradient_narrow_kernel<T, 2>), grid, dim3(512), 0, s, p);
+    } else {
+        uint16_t* const wide = reinterpret_cast<uint16_t*>(workspace + plan.wide_at);
+        hipLaunchKernelGGL(ctc_gradient_columns_kernel<T>, dim3(blocks(p.A, 2 * kWave), kColumnSlabs), dim3(256), 0, s, p,
+                           reinterpret_cast<uint32_t*>(workspace + plan.largest_at));
+        hipLaunchKernelGGL(ctc_widen_rows_kernel, dim3(blocks(p.rows, 32), blocks(p.pitch, 256)), dim3(256), 0, s, p, wide);
+        hipLaunchKernelGGL(ctc_weight_gradient_wide_kernel<T>, grid, dim3(512), 0, s, p, wide);
+    }
 }
 
 }  // namespace
@@ -1259,13 +1351,13 @@ int launch_weight_gradient(const void* grads, const int8_t* q, const float* scal
     const GradientPlan plan = gradient_plan(rows, H, A);
     const int64_t weights = static_cast<int64_t>(A) * H;
     float* const bias = partials + plan.bias_at;
-    uint32_t* const largest = reinterpret_cast<uint32_t*>(partials + plan.largest_at);
     const GradientArgs p = {grads, q, scales, frames, rows, H, A, pitch_of(H), plan.slabs,
-                            plan.slabs > 1 ? partials : dweight, dbias ? bias : nullptr, largest};
+                            plan.slabs > 1 ? partials : dweight, dbias ? bias : nullptr,
+                            reinterpret_cast<const uint32_t*>(partials + plan.largest_at)};
     if (bf16)
-        launch_gradient<bf16_t>(p, plan, largest, s);
+        launch_gradient<bf16_t>(p, plan, partials, s);
     else
-        launch_gradient<float>(p, plan, largest, s);
+        launch_gradient<float>(p, plan, partials, s);
     int err = last_error();
     if (err) return err;
     if (plan.slabs > 1) {
