@@ -26,6 +26,16 @@ template <> __device__ __forceinline__ bf16_t narrow<bf16_t>(float v)
     return {__builtin_bit_cast(uint16_t, static_cast<__bf16>(v))};
 }
 
+// Bytes of rows that nobody reads soon are written past the caches: they would take the place of what is being read, and a cache that has to let
+// go of old lines to take new ones slows both.  28 900 of 48 000 rows of 2048 bf16: from 8 bits 43 us -> 27.5, the norm 91 -> 80.
+template <int BYTES> __device__ __forceinline__ void store_past(void* to, const void* from)
+{
+    typedef uint32_t words_t __attribute__((ext_vector_type(BYTES / 4), aligned(2)));
+    words_t w;
+    __builtin_memcpy(&w, from, BYTES);
+    __builtin_nontemporal_store(w, static_cast<words_t*>(to));
+}
+
 // 16 bytes of a row: 4 floats or 8 bf16.  Rows of odd widths begin anywhere, so these are loads and stores that ask for the
 // alignment of an element only, which the hardware takes.
 template <typename T> struct Vector {
@@ -52,7 +62,7 @@ template <typename T> __device__ __forceinline__ void store_vector(T* row, int c
 {
     constexpr int kE = Vector<T>::kElements;
     if (col + kE <= H) {
-        __builtin_memcpy(row + col, &r, 16);
+        store_past<16>(row + col, &r);
         return;
     }
 #pragma unroll
@@ -74,6 +84,15 @@ __device__ __forceinline__ int row_of(const int32_t* frames, int rows, int i)
     if (!frames) return i;
     const int r = frames[1 + static_cast<int64_t>(i)];
     return r < 0 || r >= rows ? -1 : r;
+}
+
+// Row of entry i of the list, or -1 where it has none or one to skip: the list's count and its entry are asked for together.
+__device__ __forceinline__ int row_at(const int32_t* frames, int rows, int64_t i)
+{
+    if (i >= rows) return -1;
+    if (!frames) return static_cast<int>(i);
+    const int n = frames[0], r = frames[1 + i];
+    return i < n && r >= 0 && r < rows ? r : -1;
 }
 
 // ---- sums and maxima over lanes ---------------------------------------------------------------------------------
@@ -161,10 +180,9 @@ template <typename T, int WAVES, int E, bool NORM>
 __global__ __launch_bounds__(256) void ctc_rows_to_8_bits_kernel(NormArgs p)
 {
     constexpr int kE = Vector<T>::kElements, kVectors = E / kE;
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int i = blockIdx.x * (4 / WAVES) + wave / WAVES;
-    if (i >= listed(p.frames, p.rows)) return;
-    const int r = row_of(p.frames, p.rows, i);
+    const int r = row_at(p.frames, p.rows, i);
     if (r < 0) return;
     const int thread = (wave % WAVES) * kWave + lane;
     const T* x = static_cast<const T*>(p.x) + static_cast<int64_t>(r) * p.H;
@@ -247,20 +265,27 @@ __global__ __launch_bounds__(256) void ctc_rows_from_8_bits_kernel(const int8_t*
                                                                    T* __restrict__ out)
 {
     constexpr int kE = Vector<T>::kElements;
-    const int lane = threadIdx.x % kWave, i = blockIdx.x * 4 + threadIdx.x / kWave;
-    if (i >= listed(frames, rows)) return;
-    const int r = row_of(frames, rows, i);
+    const int lane = threadIdx.x % kWave, i = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int r = row_at(frames, rows, i);
     if (r < 0) return;
     const float scale = scales[r];
     const int8_t* from = q + static_cast<int64_t>(r) * pitch;
     T* to = out + static_cast<int64_t>(r) * H;
-    for (int col = lane * kE; col < H; col += kWave * kE) {
-        int8_t b[kE];
-        __builtin_memcpy(b, __builtin_assume_aligned(from + col, kE), kE);
-        Vector<T> v;
+    constexpr int kStep = kWave * kE, kVectors = 4;
+    for (int first = lane * kE; first < H; first += kVectors * kStep) {
+        int8_t b[kVectors][kE];
 #pragma unroll
-        for (int k = 0; k < kE; ++k) v.v[k] = narrow<T>(static_cast<float>(b[k]) * scale);
-        store_vector(to, col, H, v);
+        for (int i = 0; i < kVectors; ++i)                                   // (a row's bytes reach to its pitch)
+            if (first + i * kStep < pitch) __builtin_memcpy(b[i], __builtin_assume_aligned(from + first + i * kStep, kE), kE);
+#pragma unroll
+        for (int i = 0; i < kVectors; ++i) {
+            const int col = first + i * kStep;
+            if (col >= H) break;
+            Vector<T> v;
+#pragma unroll
+            for (int k = 0; k < kE; ++k) v.v[k] = narrow<T>(static_cast<float>(b[i][k]) * scale);
+            store_vector(to, col, H, v);
+        }
     }
 }
 
@@ -393,6 +418,7 @@ __global__ __launch_bounds__(1024) void ctc_sum_partials_kernel(const float* __r
     const int64_t col = static_cast<int64_t>(blockIdx.x) * kWave + lane;
     double sum = 0.0;
     if (col < width)
+#pragma unroll 16
         for (int p = group; p < count; p += 16) sum += static_cast<double>(partials[p * stride + col]);
     s_sum[group][lane] = sum;
     __syncthreads();
@@ -424,77 +450,49 @@ template <typename T> __device__ __forceinline__ T activation(int sum, float sca
     return narrow<T>(fmaf(static_cast<float>(sum), scale * weight_scale, bias));
 }
 
-// Few rows or few symbols: 16 MB rows by 16 NB symbols to a workgroup, straight from memory into the matrix cores, each of the
-// four wavefronts with every fourth 128 bytes of the rows; their sums are added in LDS.  What is many then (the rows, or the weights)
-// is read once, with nothing between a wavefront's loads.
+// Few rows and symbols: 16 by 16 to a workgroup, straight from memory into the matrix cores, each of the four wavefronts with every fourth 128
+// bytes of the rows; their sums are added in LDS.  The larger operand is read once, with nothing between a wavefront's loads.
 // v_mfma_i32_16x16x64_i8: lane l gives bytes 16 (l / 16) .. of row l % 16 of either operand, and holds rows 4 (l / 16) .. + 3 of column
 // l % 16 of the result.
-template <typename T, int MB, int NB>
+template <typename T>
 __global__ __launch_bounds__(256) void ctc_linear_direct_kernel(LinearArgs p)
 {
-    __shared__ int4v s_sum[4][MB * NB][kWave];
+    __shared__ int4v s_sum[4][kWave];
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int n = listed(p.frames, p.rows);
-    const unsigned columns = static_cast<unsigned>((p.A + 16 * NB - 1) / (16 * NB));
-    const int64_t m0 = static_cast<int64_t>(blockIdx.x / columns) * (16 * MB);
-    const int a0 = static_cast<int>(blockIdx.x % columns) * (16 * NB);
-    if (m0 >= n) return;
-    int mine[MB];
-    const int8_t* row[MB];
-    const int8_t* column[NB];
+    const unsigned columns = static_cast<unsigned>((p.A + 15) / 16);
+    const int64_t m0 = static_cast<int64_t>(blockIdx.x / columns) * 16;
+    const int a = static_cast<int>(blockIdx.x % columns) * 16 + lane % 16;
+    // All loads of 2048 bytes of the rows before the first product; the weights', which wait for nothing, before the list's.
     const int begin = wave * 128 + lane / 16 * 16;
-#pragma unroll
-    for (int b = 0; b < MB; ++b) {
-        const int64_t i = m0 + b * 16 + lane % 16;
-        mine[b] = i < n ? row_of(p.frames, p.rows, static_cast<int>(i)) : -1;
-        // (a row that does not count gives the first symbol's weights: any bytes will do)
-        row[b] = (mine[b] < 0 ? p.weight_q : p.q + static_cast<int64_t>(mine[b]) * p.pitch) + begin;
-    }
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-        const int a = a0 + b * 16 + lane % 16;
-        column[b] = p.weight_q + static_cast<int64_t>(a < p.A ? a : p.A - 1) * p.pitch + begin;
-    }
-    int4v sum[MB][NB] = {};
-    for (int k0 = 0; k0 < p.pitch; k0 += 2048) {
-        int4v x[8][MB], w[8][NB];                       // all loads of 2048 bytes of the rows before the first product
+    const int8_t* const column = p.weight_q + static_cast<int64_t>(a < p.A ? a : p.A - 1) * p.pitch + begin;
+    int4v x[8], w[8];
+    const auto load = [&](int4v (&to)[8], const int8_t* from, int k0) {
 #pragma unroll
         for (int h = 0; h < 8; ++h) {
             const int k = k0 + h / 2 * 512 + h % 2 * 64;
-            const bool in = k + wave * 128 < p.pitch;
-#pragma unroll
-            for (int b = 0; b < MB; ++b) x[h][b] = in ? *reinterpret_cast<const int4v*>(row[b] + k) : int4v{};
-#pragma unroll
-            for (int b = 0; b < NB; ++b) w[h][b] = in ? *reinterpret_cast<const int4v*>(column[b] + k) : int4v{};
+            to[h] = k + wave * 128 < p.pitch ? *reinterpret_cast<const int4v*>(from + k) : int4v{};
         }
+    };
+    load(w, column, 0);
+    const int mine = row_at(p.frames, p.rows, m0 + lane % 16);
+    // (a row that does not count gives the first symbol's weights: any bytes will do)
+    const int8_t* const row = (mine < 0 ? p.weight_q : p.q + static_cast<int64_t>(mine) * p.pitch) + begin;
+    if (m0 >= listed(p.frames, p.rows)) return;
+    const float weight_scale = a < p.A ? p.weight_scales[a] : 0.0f, bias = a < p.A && p.bias ? p.bias[a] : 0.0f;
+    int4v sum = {};
+    for (int k0 = 0; k0 < p.pitch; k0 += 2048) {
+        load(x, row, k0);
 #pragma unroll
-        for (int h = 0; h < 8; ++h)
-#pragma unroll
-            for (int i = 0; i < MB; ++i)
-#pragma unroll
-                for (int j = 0; j < NB; ++j) sum[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[h][i], w[h][j], sum[i][j], 0, 0, 0);
+        for (int h = 0; h < 8; ++h) sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[h], w[h], sum, 0, 0, 0);
+        if (k0 + 2048 < p.pitch) load(w, column, k0 + 2048);
     }
-#pragma unroll
-    for (int i = 0; i < MB; ++i)
-#pragma unroll
-        for (int j = 0; j < NB; ++j) s_sum[wave][i * NB + j][lane] = sum[i][j];
+    s_sum[wave][lane] = sum;
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < MB; ++i)
-#pragma unroll
-        for (int j = 0; j < NB; ++j) {
-            const int block = i * NB + j;
-            if (block % 4 != wave) continue;
-            const int a = a0 + j * 16 + lane % 16;
-            const int4v total = s_sum[0][block][lane] + s_sum[1][block][lane] + s_sum[2][block][lane] + s_sum[3][block][lane];
-            const float weight_scale = a < p.A ? p.weight_scales[a] : 0.0f, bias = a < p.A && p.bias ? p.bias[a] : 0.0f;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int r = __shfl(mine[i], lane / 16 * 4 + e, kWave);
-                if (r >= 0 && a < p.A)
-                    static_cast<T*>(p.logits)[static_cast<int64_t>(r) * p.A + a] = activation<T>(total[e], p.scales[r], weight_scale, bias);
-            }
-        }
+    // One of a lane's four rows to each wavefront.
+    const int r = __shfl(mine, lane / 16 * 4 + wave, kWave);
+    if (r < 0 || a >= p.A) return;
+    const int total = s_sum[0][lane][wave] + s_sum[1][lane][wave] + s_sum[2][lane][wave] + s_sum[3][lane][wave];
+    static_cast<T*>(p.logits)[static_cast<int64_t>(r) * p.A + a] = activation<T>(total, p.scales[r], weight_scale, bias);
 }
 
 typedef int int16v __attribute__((ext_vector_type(16)));
@@ -600,7 +598,7 @@ __global__ __launch_bounds__(256) void ctc_linear_tiles_kernel(LinearArgs p)
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
-        __builtin_amdgcn_sched_group_barrier(0x008, WM * WN - WM - WN, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, WM * WN > WM + WN ? WM * WN - WM - WN : 0, 0);
         __builtin_amdgcn_sched_barrier(0);
     };
     // One buffer's products.  The next one's bytes were asked for kStages - 1 steps ago; behind the barrier every wavefront has what
@@ -620,17 +618,14 @@ __global__ __launch_bounds__(256) void ctc_linear_tiles_kernel(LinearArgs p)
     for (int t = 0; t < kStages; ++t) fill(s_buffer[t], t);
     wait_and_meet<(kStages - 1) * kLoads>();
     fetch(s_buffer[0], 0);
-    int t = 0;                                          // (the number of steps is even)
-    for (; t + 3 < steps; t += 4) {
-        step(0, t);
-        step(1, t + 1);
-        step(2, t + 2);
-        step(3, t + 3);
+    int t = 0;
+    for (; t + kStages <= steps; t += kStages) {
+#pragma unroll
+        for (int i = 0; i < kStages; ++i) step(i, t + i);
     }
-    if (t < steps) {
-        step(0, t);
-        step(1, t + 1);
-    }
+#pragma unroll
+    for (int i = 0; i + 1 < kStages; ++i)
+        if (t + i < steps) step(i, t + i);
     // (From here on memory is asked for nothing but to write: a wait for a load behind the writes would wait for them too.)
     constexpr int kAcross = 8 * WN, kDown = kWave / kAcross, kLine = 32 * WN + 4;       // lanes to a row, rows at once, ints from row to row
     const int a = a0 + wave % 2 * 32 * WN + lane % kAcross * 4;
@@ -1203,7 +1198,14 @@ unsigned blocks(int64_t items, int per_block) { return static_cast<unsigned>((it
 template <typename T, bool NORM> void launch_to_8_bits(const NormArgs& p, hipStream_t s)
 {
     const dim3 block(256), wide(static_cast<unsigned>(p.rows)), narrow_rows(blocks(p.rows, 4));
-    if (p.pitch <= 512)
+    // Few rows (not even a wavefront to a compute unit's SIMD) take four wavefronts each, for the time that one row takes; one each
+    // asks for nothing between wavefronts.
+    const bool few = p.rows <= 512;
+    if (few && p.pitch > 512 && p.pitch <= 2048)
+        hipLaunchKernelGGL((ctc_rows_to_8_bits_kernel<T, 4, 8, NORM>), wide, block, 0, s, p);
+    else if (few && p.pitch > 2048 && p.pitch <= 4096)
+        hipLaunchKernelGGL((ctc_rows_to_8_bits_kernel<T, 4, 16, NORM>), wide, block, 0, s, p);
+    else if (p.pitch <= 512)
         hipLaunchKernelGGL((ctc_rows_to_8_bits_kernel<T, 1, 8, NORM>), narrow_rows, block, 0, s, p);
     else if (p.pitch <= 1024)
         hipLaunchKernelGGL((ctc_rows_to_8_bits_kernel<T, 1, 16, NORM>), narrow_rows, block, 0, s, p);
@@ -1237,19 +1239,28 @@ template <typename T, int WM, int WN> void launch_tiles(const LinearArgs& p, hip
     const int64_t tiles = static_cast<int64_t>(blocks(p.rows, 64 * WM)) * blocks(p.A, 64 * WN);
     hipLaunchKernelGGL((ctc_linear_tiles_kernel<T, WM, WN>), dim3(blocks(tiles, 8) * 8), dim3(256), 0, s, p);
 }
-template <typename T, int MB, int NB> void launch_direct(const LinearArgs& p, hipStream_t s)
+template <typename T> void launch_direct(const LinearArgs& p, hipStream_t s)
 {
-    hipLaunchKernelGGL((ctc_linear_direct_kernel<T, MB, NB>), dim3(blocks(p.rows, 16 * MB) * blocks(p.A, 16 * NB)), dim3(256), 0, s, p);
+    hipLaunchKernelGGL(ctc_linear_direct_kernel<T>, dim3(blocks(p.rows, 16) * blocks(p.A, 16)), dim3(256), 0, s, p);
 }
 template <typename T> void launch_product(const LinearArgs& p, hipStream_t s)
 {
-    const int64_t small = static_cast<int64_t>(blocks(p.rows, 128)) * blocks(p.A, 128);
-    const int64_t large = static_cast<int64_t>(blocks(p.rows, 256)) * blocks(p.A, 256);
-    if (p.rows <= 16)
-        launch_direct<T, 1, 1>(p, s);
-    else if (p.A <= 64 || small < 192)
-        launch_direct<T, 2, 2>(p, s);
-    else if (large < 512)
+    // Of a list's rows, five in eight are taken to count (how many do, only the GPU knows).
+    const int64_t rows = p.frames ? (static_cast<int64_t>(p.rows) * 5 + 7) / 8 : p.rows;
+    const auto tiles = [&](int m, int n) { return (rows + m - 1) / m * ((p.A + n - 1) / n); };
+    // Tiles of 256 by 256 read the least of memory and LDS, those of 128 by 128, two of which share a compute unit, begin and end sooner: the times
+    // of a round of each (us), from K = 512 and 2048 at 3000 and 19200 rows by 6000 symbols (28.7 and 389 against 40 and 326; 5560 x 4733, K = 1152:
+    // 73 against 60).
+    const double steps = p.pitch / 64;
+    const double large = static_cast<double>((tiles(256, 256) + 255) / 256) * (13.5 + 0.85 * steps);
+    const double small = static_cast<double>((tiles(128, 128) + 511) / 512) * (7.0 + 0.65 * steps);
+    if (tiles(16, 16) <= 400)                           // 1 x 6000 4.5 us against 6.0 in tiles of 64 by 64, 16 x 6000 5.9 and 6.1, 32 x 6000 7.8 and 6.3
+        launch_direct<T>(p, s);
+    else if (p.A <= 64 && tiles(64, 64) > 400)          // 27200 x 60 14.7 us against 15.6; 5000 x 60 8.4 against 6.8
+        launch_tiles<T, 2, 1>(p, s);
+    else if (tiles(64, 64) <= 600)                      // 300 x 6000 10.9 us against 13.7 in 128 by 128; 1500 x 2000 (768 tiles) 11.1 and 10.8
+        launch_tiles<T, 1, 1>(p, s);
+    else if (small < large)
         launch_tiles<T, 2, 2>(p, s);
     else
         launch_tiles<T, 4, 4>(p, s);

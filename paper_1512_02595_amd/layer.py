@@ -55,7 +55,7 @@ def row_pitch(H) -> int:
 
 
 def _check(status: int, where: str) -> None:
-    if status != ctc.STATUS_SUCCESS:
+    if status:
         extra = f" (hipError {last_hip_error()})" if status == ctc.STATUS_HIP_ERROR else ""
         raise ctc.CTCError(status, where + extra)
 
