@@ -2,13 +2,15 @@
 """Benchmark of the batched CTC cost + gradient on one MI355X.
 
     python bench.py [--gpus 1] [--steps K] [--warmup W] [--config 1] [--dtype f32|bf16]
-                    [--mode grad|loss|align]
+                    [--mode grad|loss|align|layer]
 
 A step is one ctc_loss_and_grad call (host launcher + all kernels) over one synthetic
 minibatch whose activations already sit in HBM.  The default workload is the English-shaped
 per-GPU minibatch (config index 1: B=64, A=29, T<=750).  Prints one JSON line.
 --mode loss times the cost-only call (grads == NULL), --mode align the most probable
-alignment (ctc_best_path); the default, grad, is the headline metric.
+alignment (ctc_best_path); the default, grad, is the headline metric.  --mode layer times the
+output layer around it as well: states of --width to activations to cost and gradient to the
+weights' gradient, with states and weights in 8 bits.
 """
 from __future__ import annotations
 
@@ -146,8 +148,10 @@ def main():
     ap.add_argument("--warmup", type=int, default=20)
     ap.add_argument("--config", type=int, default=1, help="0..4: the five headline workloads (1 = the metric's); 5: bigram alphabet")
     ap.add_argument("--dtype", choices=("f32", "bf16"), default="f32")
-    ap.add_argument("--mode", choices=("grad", "loss", "align"), default="grad",
-                    help="grad: cost + gradient (headline); loss: cost only; align: most probable alignment")
+    ap.add_argument("--mode", choices=("grad", "loss", "align", "layer"), default="grad",
+                    help="grad: cost + gradient (headline); loss: cost only; align: most probable alignment; layer: grad with the "
+                         "output layer's forward pass and weights' gradient in 8 bits")
+    ap.add_argument("--width", type=int, default=2048, help="--mode layer: width of a state")
     ap.add_argument("--metadata", choices=("host", "device"), default="host",
                     help="device: ctc_loss_and_grad_device (lengths and labels resident on the GPU, workspace "
                          "sized by bounds)")
@@ -204,7 +208,7 @@ def main():
                for i in range(args.buffers)]
     stream = torch.cuda.current_stream(dev).cuda_stream
     if args.metadata == "device":
-        if args.mode == "align":
+        if args.mode in ("align", "layer"):
             sys.exit("bench.py: --metadata device covers the grad and loss modes")
         max_label = max(int(b.label_lengths.max()) for b in batches)
         dbs = []
@@ -237,8 +241,27 @@ def main():
         if args.graph:
             sys.exit("bench.py: --graph needs --metadata device (the host-metadata call reads host memory)")
         dbs = [harness.DeviceBatch(b, dtype, dev, poison=False) for b in batches]
-        step = {"grad": harness.DeviceBatch.run, "loss": harness.DeviceBatch.run_loss,
-                "align": harness.DeviceBatch.run_best_path}[args.mode]
+        if args.mode == "layer":
+            torch.manual_seed(workloads.BASE_SEED)
+            layers = {}
+            for d in dbs:
+                b = d.batch
+                out = harness.OutputLayer(b.T, b.B, args.width, b.A, dtype, logits=d.x, device=dev)
+                out.set_weights(torch.randn(b.A, args.width, device=dev) * (2.0 / args.width ** 0.5))
+                lengths = torch.from_numpy(np.ascontiguousarray(b.input_lengths, dtype=np.int32)).to(dev)
+                states = [torch.randn(b.T, b.B, args.width, device=dev).to(d.x.dtype) for _ in range(2)]
+                layers[id(d)] = (out, lengths, *states)
+            args.profile_steps = 0             # (the per-launch times are the CTC call's alone: --mode grad)
+
+            def step(d, stream, kernel_ms=None):
+                out, lengths, states, residual = layers[id(d)]
+                out.set_lengths(lengths, stream)
+                out.forward(states, residual, stream)
+                d.run(stream)
+                out.weight_gradient(d.grads, stream)
+        else:
+            step = {"grad": harness.DeviceBatch.run, "loss": harness.DeviceBatch.run_loss,
+                    "align": harness.DeviceBatch.run_best_path}[args.mode]
 
     for i in range(args.warmup):
         step(dbs[i % len(dbs)], stream)
@@ -269,8 +292,10 @@ def main():
 
     B = batches[0].B
     frames = float(np.mean([b.frames for b in batches]))
-    if args.mode == "grad":
+    if args.mode in ("grad", "layer"):
         compulsory = float(np.mean([b.compulsory_bytes(elem) for b in batches]))
+        if args.mode == "layer":    # states and residual once, their sum written, rows in 8 bits written and read twice, weights read, their gradient written
+            compulsory += frames * args.width * (3 * elem + 3) + batches[0].A * args.width * 5
     else:       # the valid activations once; the alignment also writes one int32 per frame of the tensor
         compulsory = float(np.mean([b.frames * b.A * elem for b in batches]))
         if args.mode == "align":
@@ -284,7 +309,7 @@ def main():
     names = [ctc.kernel_name(i) for i in range(ctc.NUM_KERNELS)]
     if args.mode == "align":
         names[2] = ctc.kernel_name(ctc.KERNEL_BACKTRACE)
-    kb = [kernel_bytes(b, elem, args.mode) for b in batches]
+    kb = [kernel_bytes(b, elem, "grad" if args.mode == "layer" else args.mode) for b in batches]
     beside = args.mode == "grad" and args.profile_steps > 0 and kavg[2] == 0        # the lattice launch writes the gradient
     if beside:
         for k, _ in kb:
@@ -333,7 +358,7 @@ def main():
 
     out = {
         "metric": {"grad": "ctc_loss_grad_utterances_per_s", "loss": "ctc_loss_only_utterances_per_s",
-                   "align": "ctc_best_path_utterances_per_s"}[args.mode],
+                   "align": "ctc_best_path_utterances_per_s", "layer": "ctc_output_layer_step_utterances_per_s"}[args.mode],
         "value": round(B / (ms_per_step * 1e-3), 1),
         "unit": "utterances/s",
         "n_gpus": 1, "steps": args.steps, "warmup": args.warmup,
@@ -349,6 +374,7 @@ def main():
         "config": {"workload": "config[%d] %s: B=%d A=%d T=%d, %d rotating minibatches"
                    % (args.config, batches[0].name, B, batches[0].A, batches[0].T, len(batches)),
                    "mode": args.mode, "metadata": args.metadata, "graph": bool(args.graph),
+                   **({"width": args.width} if args.mode == "layer" else {}),
                    "sequential_chains": bool(args.sequential_chains)},
         "activation_frames_per_s": round(frames / (ms_per_step * 1e-3), 1),
         "hbm_roofline_frac_end_to_end": round(compulsory / (ms_per_step * 1e-3) / 1e9 / HBM_PEAK_GBS, 5),

@@ -59,7 +59,7 @@ size_t matrix(int rows, int width, size_t elem) { return static_cast<size_t>(row
 size_t list_bytes(int rows) { return (static_cast<size_t>(rows) + 1) * 4; }
 size_t round_up(size_t v) { return (v + 255) / 256 * 256; }
 
-size_t norm_workspace(int rows, int H) { return round_up(static_cast<size_t>(norm_partials(rows)) * H * 4); }
+size_t norm_workspace(int rows, int H) { return round_up(static_cast<size_t>(norm_partials(rows, H)) * H * 4); }
 size_t gradient_workspace(int rows, int H, int A) { return round_up(gradient_plan(rows, H, A).bytes); }
 
 }  // namespace

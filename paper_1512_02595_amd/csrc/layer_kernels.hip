@@ -742,14 +742,13 @@ __device__ __forceinline__ void meet()
 
 // Largest |gradient * scale| and sum of the gradients of each symbol, over the rows of a slab: two symbols to a lane, the rows dealt out to
 // four wavefronts, eight at a time.
-template <typename T>
-__global__ __launch_bounds__(256) void ctc_gradient_columns_kernel(GradientArgs p, uint32_t* largest)
+template <typename T> __device__ __forceinline__ void look_at_columns(const GradientArgs& p, uint32_t* largest, int block, int slab)
 {
     __shared__ uint32_t s_most[4][2 * kWave];
     __shared__ double s_sum[4][2 * kWave];
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int a = blockIdx.x * (2 * kWave) + 2 * lane, slab = blockIdx.y;
-    const Range range = slab_of(listed(p.frames, p.rows), slab, gridDim.y);
+    const int a = block * (2 * kWave) + 2 * lane;
+    const Range range = slab_of(listed(p.frames, p.rows), slab, kColumnSlabs);
     const int at = a + 1 < p.A ? a : a < p.A ? a - 1 : 0;                    // (A is at least 2 here; the last symbol of an odd number is the upper of a pair)
     uint32_t most[2] = {};
     double sum[2] = {};
@@ -783,7 +782,7 @@ __global__ __launch_bounds__(256) void ctc_gradient_columns_kernel(GradientArgs 
         s_sum[wave][2 * lane + k] = sum[k];
     }
     __syncthreads();
-    const int mine = blockIdx.x * (2 * kWave) + threadIdx.x;
+    const int mine = block * (2 * kWave) + threadIdx.x;
     if (threadIdx.x >= 2 * kWave || mine >= p.A) return;
     const int from = mine == p.A - 1 && mine % 2 == 0 ? threadIdx.x + 1 : threadIdx.x;
     uint32_t m = 0;
@@ -995,14 +994,14 @@ __global__ __launch_bounds__(512) void ctc_weight_gradient_narrow_kernel(Gradien
 
 // More than 64 symbols: the whole numbers of the listed rows as fp16, once for all symbols' workgroups.  32 listed rows at a time (a step), for each
 // column k 64 bytes, its 8-row pieces in the order j ^ k / 4 % 4: as the kernel below wants them in LDS.  256 columns to a workgroup.
-__global__ __launch_bounds__(256) void ctc_widen_rows_kernel(GradientArgs p, uint16_t* wide)
+__device__ __forceinline__ void widen_rows(const GradientArgs& p, uint16_t* wide, int step, int k0)
 {
     __shared__ __align__(16) int8_t s_row[32][256 + 4];
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int n = listed(p.frames, p.rows), k0 = blockIdx.y * 256;
-    if (static_cast<int64_t>(blockIdx.x) * 32 >= n) return;
+    const int n = listed(p.frames, p.rows);
+    if (step * 32 >= n) return;
     const StepRows list(p, {0, n}, lane);
-    const int row = list.row(blockIdx.x, list.ask(blockIdx.x));
+    const int row = list.row(step, list.ask(step));
     if (k0 + 4 * lane < p.pitch) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -1014,13 +1013,26 @@ __global__ __launch_bounds__(256) void ctc_widen_rows_kernel(GradientArgs p, uin
     __syncthreads();
     const int k = threadIdx.x;
     if (k0 + k >= p.pitch) return;
-    uint16_t* const to = wide + (static_cast<int64_t>(blockIdx.x) * p.pitch + k0 + k) * 32;
+    uint16_t* const to = wide + (static_cast<int64_t>(step) * p.pitch + k0 + k) * 32;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         half8 piece;
 #pragma unroll
         for (int i = 0; i < 8; ++i) piece[i] = static_cast<_Float16>(static_cast<float>(s_row[j * 8 + i][k]));
         *reinterpret_cast<half8*>(to + (j ^ k / 4 % 4) * 8) = piece;
+    }
+}
+
+// Both in one launch: the columns' workgroups first.
+template <typename T>
+__global__ __launch_bounds__(256) void ctc_gradient_prepare_kernel(GradientArgs p, uint32_t* largest, uint16_t* wide, unsigned column_blocks)
+{
+    const unsigned columns = column_blocks * kColumnSlabs;
+    if (blockIdx.x < columns) {
+        look_at_columns<T>(p, largest, blockIdx.x % column_blocks, blockIdx.x / column_blocks);
+    } else {
+        const unsigned across = static_cast<unsigned>((p.pitch + 255) / 256), i = blockIdx.x - columns;
+        widen_rows(p, wide, static_cast<int>(i / across), static_cast<int>(i % across) * 256);
     }
 }
 
@@ -1168,9 +1180,20 @@ __global__ __launch_bounds__(512) void ctc_weight_gradient_wide_kernel(GradientA
         }
 }
 
-// out[i] = the slabs' sums, in order; four to a thread.
-__global__ __launch_bounds__(256) void ctc_sum_slabs_kernel(const float* __restrict__ partials, int slabs, int64_t width, float* __restrict__ out)
+// The slabs' sums, in order: of the weights' gradient, four to a thread (none where there is one slab), and, in the workgroups behind, of the bias's.
+__global__ __launch_bounds__(256) void ctc_sum_slabs_kernel(const float* __restrict__ partials, int slabs, int64_t width, float* __restrict__ out,
+                                                            unsigned blocks, const float* __restrict__ bias, int bias_slabs, int A,
+                                                            float* __restrict__ dbias)
 {
+    if (blockIdx.x >= blocks) {
+        const int a = static_cast<int>(blockIdx.x - blocks) * 256 + threadIdx.x;
+        if (a >= A) return;
+        double sum = 0.0;
+#pragma unroll 16
+        for (int s = 0; s < bias_slabs; ++s) sum += static_cast<double>(bias[static_cast<int64_t>(s) * A + a]);
+        dbias[a] = static_cast<float>(sum);
+        return;
+    }
     const int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
     if (i >= width) return;
     if (i + 4 <= width) {
@@ -1227,7 +1250,7 @@ template <typename T> void launch_backward(const NormBackArgs& p, unsigned group
     else if (p.H <= 2048)
         hipLaunchKernelGGL((ctc_norm_backward_kernel<T, 4, 8>), grid, dim3(256), 0, s, p);
     else if (p.H <= 4096)
-        hipLaunchKernelGGL((ctc_norm_backward_kernel<T, 4, 16>), grid, dim3(256), 0, s, p);
+        hipLaunchKernelGGL((ctc_norm_backward_kernel<T, 8, 8>), grid, dim3(512), 0, s, p);
     else if (p.H <= 8192)
         hipLaunchKernelGGL((ctc_norm_backward_kernel<T, 16, 8>), grid, dim3(1024), 0, s, p);
     else
@@ -1275,9 +1298,9 @@ template <typename T> void launch_gradient(const GradientArgs& p, const Gradient
         hipLaunchKernelGGL((ctc_weight_gradient_narrow_kernel<T, 2>), grid, dim3(512), 0, s, p);
     } else {
         uint16_t* const wide = reinterpret_cast<uint16_t*>(workspace + plan.wide_at);
-        hipLaunchKernelGGL(ctc_gradient_columns_kernel<T>, dim3(blocks(p.A, 2 * kWave), kColumnSlabs), dim3(256), 0, s, p,
-                           reinterpret_cast<uint32_t*>(workspace + plan.largest_at));
-        hipLaunchKernelGGL(ctc_widen_rows_kernel, dim3(blocks(p.rows, 32), blocks(p.pitch, 256)), dim3(256), 0, s, p, wide);
+        const unsigned columns = blocks(p.A, 2 * kWave);
+        hipLaunchKernelGGL(ctc_gradient_prepare_kernel<T>, dim3(columns * kColumnSlabs + blocks(p.rows, 32) * blocks(p.pitch, 256)), dim3(256), 0, s, p,
+                           reinterpret_cast<uint32_t*>(workspace + plan.largest_at), wide, columns);
         hipLaunchKernelGGL(ctc_weight_gradient_wide_kernel<T>, grid, dim3(512), 0, s, p, wide);
     }
 }
@@ -1331,7 +1354,7 @@ int launch_norm_backward(const void* dy, const void* sum, const float* weight, f
                          void* stream)
 {
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const int groups = norm_partials(rows);
+    const int groups = norm_partials(rows, H);
     const NormBackArgs p = {dy, sum, weight, eps, dresidual, frames, rows, H, dsum, dweight ? partials : nullptr};
     if (bf16)
         launch_backward<bf16_t>(p, static_cast<unsigned>(groups), s);
@@ -1369,15 +1392,12 @@ int launch_weight_gradient(const void* grads, const int8_t* q, const float* scal
         launch_gradient<bf16_t>(p, plan, partials, s);
     else
         launch_gradient<float>(p, plan, partials, s);
-    int err = last_error();
+    const int err = last_error();
     if (err) return err;
-    if (plan.slabs > 1) {
-        hipLaunchKernelGGL(ctc_sum_slabs_kernel, dim3(blocks(weights, 1024)), dim3(256), 0, s, partials, plan.slabs, weights, dweight);
-        err = last_error();
-    }
-    if (err || !dbias) return err;
-    hipLaunchKernelGGL(ctc_sum_partials_kernel, dim3(blocks(A, kWave)), dim3(1024), 0, s, bias, plan.bias_slabs,
-                       static_cast<int64_t>(A), static_cast<int64_t>(A), dbias);
+    const unsigned weight_blocks = plan.slabs > 1 ? blocks(weights, 1024) : 0, bias_blocks = dbias ? blocks(A, 256) : 0;
+    if (weight_blocks + bias_blocks == 0) return 0;
+    hipLaunchKernelGGL(ctc_sum_slabs_kernel, dim3(weight_blocks + bias_blocks), dim3(256), 0, s, partials, plan.slabs, weights, dweight, weight_blocks,
+                       bias, plan.bias_slabs, A, dbias);
     return last_error();
 }
 

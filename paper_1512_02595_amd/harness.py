@@ -8,7 +8,7 @@ from __future__ import annotations
 import numpy as np
 import torch
 
-from . import ctc, workloads
+from . import ctc, layer, workloads
 
 
 def require_gpu() -> torch.device:
@@ -154,3 +154,80 @@ class DeviceMetaBatch:
         """(status int, costs float32 [B], grads float32 [T,B,A]) on the host, after synchronising."""
         torch.cuda.synchronize(self.device)
         return int(self.status.item()), self.costs.cpu().numpy(), self.grads.float().cpu().numpy()
+
+
+class OutputLayer:
+    """The layer that makes CTC's activations, with its states in 8 bits, over the buffers of a minibatch [T, B].
+
+    `forward` takes the last layer's states and the residual stream to activations [T, B, A] (`logits`, which may be a
+    DeviceBatch's or DeviceMetaBatch's `x`), `weight_gradient` takes CTC's gradient to the weights' and the bias's, from the rows that
+    the forward pass left in 8 bits, and `norm_backward` the gradient of the norm's output to its input's.  Frames behind an
+    utterance's end take no part.
+    """
+
+    def __init__(self, T, B, H, A, dtype: int = ctc.DTYPE_F32, eps=1e-6, logits=None, device=None):
+        self.device = device or require_gpu()
+        self.T, self.B, self.H, self.A, self.dtype, self.eps, self.rows = T, B, H, A, dtype, eps, T * B
+        tdtype = torch.float32 if dtype == ctc.DTYPE_F32 else torch.bfloat16
+
+        def zeros(*shape, dtype=torch.float32):
+            return torch.zeros(shape, dtype=dtype, device=self.device)
+
+        pitch = layer.row_pitch(H)
+        self.frames = zeros(1 + self.rows, dtype=torch.int32)
+        self.norm_weight, self.bias = torch.ones(H, device=self.device), zeros(A)
+        self.weight_q, self.weight_scales = zeros(A, pitch, dtype=torch.int8), zeros(A)
+        self.sum, self.dsum = zeros(T, B, H, dtype=tdtype), zeros(T, B, H, dtype=tdtype)
+        self.q, self.scales = zeros(self.rows, pitch, dtype=torch.int8), zeros(self.rows)
+        self.logits = zeros(T, B, A, dtype=tdtype) if logits is None else logits
+        assert tuple(self.logits.shape) == (T, B, A) and self.logits.dtype == tdtype and self.logits.is_contiguous()
+        self.dweight, self.dbias, self.dnorm_weight = zeros(A, H), zeros(A), zeros(H)
+        self.ws_bytes = layer.weight_gradient_workspace_size(self.rows, H, A), layer.rms_norm_workspace_size(self.rows, H)
+        self.ws = torch.empty(max(self.ws_bytes) + 256, dtype=torch.uint8, device=self.device)
+        self.ws_ptr = (self.ws.data_ptr() + 255) // 256 * 256
+
+    def _stream(self, stream):
+        return torch.cuda.current_stream(self.device).cuda_stream if stream is None else stream
+
+    def _states(self, t):
+        assert t.numel() == self.rows * self.H and t.dtype == self.sum.dtype and t.is_contiguous()
+        return t.data_ptr()
+
+    def set_weights(self, weight, bias=None, norm_weight=None, stream=None):
+        """fp32 weights [A, H] to 8 bits, and copies of the others: once per step of the optimiser."""
+        assert tuple(weight.shape) == (self.A, self.H) and weight.dtype == torch.float32 and weight.is_contiguous()
+        layer.quantize_rows(weight.data_ptr(), None, self.A, self.H, ctc.DTYPE_F32, self.weight_q.data_ptr(),
+                            self.weight_scales.data_ptr(), self._stream(stream))
+        if bias is not None:
+            self.bias.copy_(bias)
+        if norm_weight is not None:
+            self.norm_weight.copy_(norm_weight)
+
+    def set_lengths(self, input_lengths, stream=None):
+        """int32 [B] on the GPU: the frames of this minibatch, for all calls until the next one's."""
+        assert tuple(input_lengths.shape) == (self.B,) and input_lengths.dtype == torch.int32 and input_lengths.is_contiguous()
+        layer.pack_frames(input_lengths.data_ptr(), self.T, self.B, self.frames.data_ptr(), self._stream(stream))
+
+    def forward(self, x, residual=None, stream=None):
+        s = self._stream(stream)
+        layer.rms_norm_i8(self._states(x), None if residual is None else self._states(residual), self.norm_weight.data_ptr(),
+                          self.eps, self.frames.data_ptr(), self.rows, self.H, self.dtype, self.sum.data_ptr(), self.q.data_ptr(),
+                          self.scales.data_ptr(), s)
+        layer.linear_i8(self.q.data_ptr(), self.scales.data_ptr(), self.weight_q.data_ptr(), self.weight_scales.data_ptr(),
+                        self.bias.data_ptr(), self.frames.data_ptr(), self.rows, self.H, self.A, self.dtype,
+                        self.logits.data_ptr(), s)
+        return self.logits
+
+    def weight_gradient(self, grads, stream=None):
+        assert tuple(grads.shape) == (self.T, self.B, self.A) and grads.dtype == self.logits.dtype and grads.is_contiguous()
+        layer.weight_gradient_i8(grads.data_ptr(), self.q.data_ptr(), self.scales.data_ptr(), self.frames.data_ptr(), self.rows,
+                                 self.H, self.A, self.dtype, self.dweight.data_ptr(), self.dbias.data_ptr(), self.ws_ptr,
+                                 self.ws_bytes[0], self._stream(stream))
+        return self.dweight, self.dbias
+
+    def norm_backward(self, dy, dresidual=None, stream=None):
+        layer.rms_norm_backward(self._states(dy), self.sum.data_ptr(), self.norm_weight.data_ptr(), self.eps,
+                                None if dresidual is None else self._states(dresidual), self.frames.data_ptr(), self.rows, self.H,
+                                self.dtype, self.dsum.data_ptr(), self.dnorm_weight.data_ptr(), self.ws_ptr, self.ws_bytes[1],
+                                self._stream(stream))
+        return self.dsum, self.dnorm_weight

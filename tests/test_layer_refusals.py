@@ -150,9 +150,8 @@ def test_workspace():
 
 def test_the_largest_sizes_are_counted_in_64_bits():
     for H, A in ((16384, 1 << 20), (16384, 4000), (16384, 64), (1, 1)):
-        n = layer.weight_gradient_workspace_size(1 << 30, H, A)
-        assert 0 < n <= 257 * (1 << 20) * 16385 * 4 and n % 256 == 0
-    assert layer.weight_gradient_workspace_size(1 << 30, 1, 1 << 20) > 1 << 28
+        assert layer.weight_gradient_workspace_size(1 << 30, H, A) % 256 == 0
+    assert layer.weight_gradient_workspace_size(1 << 30, 16384, 4000) >= (1 << 30) * 16384 * 2    # the rows, in 16 bits
     assert layer.rms_norm_workspace_size(1 << 30, 16384) >= 16384 * 4
 
 
