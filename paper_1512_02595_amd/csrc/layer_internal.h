@@ -41,10 +41,10 @@ inline GradientPlan gradient_plan(int rows, int H, int A)
     p.columns = A <= 64 ? 256 : 512;
     const long tiles = ((A + p.symbols - 1L) / p.symbols) * ((H + p.columns - 1L) / p.columns);
     const long steps = (rows + 31L) / 32;
-    // Time in steps of 32 rows: as many rounds of workgroups as the 256 compute units take (three workgroups each where tiles are narrow), each of its
+    // Time in steps of 32 rows: as many rounds of workgroups as the 256 compute units take (two workgroups each where tiles are narrow), each of its
     // share of the steps and a few to begin and end with; and every slab's sums are written and read once more.
-    const long at_once = p.symbols <= 64 ? 768 : 256;
-    const double slab_cost = 8.0 * A * H / 5.0e6 / (p.symbols <= 64 ? 0.2 : 0.9);
+    const long at_once = p.symbols <= 64 ? 512 : 256;
+    const double slab_cost = 8.0 * A * H / 5.0e6 / (p.symbols <= 64 ? 1.5 : 1.7);
     double best = 0.0;
     for (long s = 1; s <= 256 && s <= (steps + 3) / 4; ++s) {
         const long rounds = (tiles * s + at_once - 1) / at_once;
