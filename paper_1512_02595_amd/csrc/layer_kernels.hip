@@ -740,62 +740,6 @@ __device__ __forceinline__ void meet()
     asm volatile("" ::: "memory");
 }
 
-// Largest |gradient * scale| and sum of the gradients of each symbol, over the rows of a slab: two symbols to a lane, the rows dealt out to
-// four wavefronts, eight at a time.
-template <typename T> __device__ __forceinline__ void look_at_columns(const GradientArgs& p, uint32_t* largest, int block, int slab)
-{
-    __shared__ uint32_t s_most[4][2 * kWave];
-    __shared__ double s_sum[4][2 * kWave];
-    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int a = block * (2 * kWave) + 2 * lane;
-    const Range range = slab_of(listed(p.frames, p.rows), slab, kColumnSlabs);
-    const int at = a + 1 < p.A ? a : a < p.A ? a - 1 : 0;                    // (A is at least 2 here; the last symbol of an odd number is the upper of a pair)
-    uint32_t most[2] = {};
-    double sum[2] = {};
-    for (int i = range.first + wave * 8; i < range.last; i += 32) {
-        T g[8][2];
-        float scale[8];
-        bool in[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int r = i + j < range.last ? row_of(p.frames, p.rows, i + j) : -1;
-            in[j] = r >= 0;
-            scale[j] = p.scales[in[j] ? r : 0];
-            __builtin_memcpy(g[j], static_cast<const T*>(p.grads) + static_cast<int64_t>(in[j] ? r : 0) * p.A + at, sizeof(g[j]));
-        }
-        float eight[2] = {};
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const float v = in[j] ? widen(g[j][k]) : 0.0f;
-                const uint32_t bits = __float_as_uint(v * scale[j]) & 0x7fffffffu;
-                if (in[j]) most[k] = most[k] > bits ? most[k] : bits;
-                eight[k] += v;
-            }
-        sum[0] += static_cast<double>(eight[0]);
-        sum[1] += static_cast<double>(eight[1]);
-    }
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        s_most[wave][2 * lane + k] = most[k];
-        s_sum[wave][2 * lane + k] = sum[k];
-    }
-    __syncthreads();
-    const int mine = block * (2 * kWave) + threadIdx.x;
-    if (threadIdx.x >= 2 * kWave || mine >= p.A) return;
-    const int from = mine == p.A - 1 && mine % 2 == 0 ? threadIdx.x + 1 : threadIdx.x;
-    uint32_t m = 0;
-    double total = 0.0;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        m = m > s_most[w][from] ? m : s_most[w][from];
-        total += s_sum[w][from];
-    }
-    largest[static_cast<int64_t>(slab) * p.A + mine] = m;
-    if (p.bias) p.bias[static_cast<int64_t>(slab) * p.A + mine] = static_cast<float>(total);
-}
-
 // A step's rows, as the list has them; -1: does not count.  (Steps behind the last have rows that do not count; every index is one of the
 // list's, every address a row's.)  The entry is asked for early and looked at late.
 struct StepRows {
@@ -818,6 +762,67 @@ struct StepRows {
         return i < range.last && r >= 0 && r < rows ? r : -1;
     }
 };
+
+// Largest |gradient * scale| and sum of the gradients of each symbol, over the rows of a slab: two symbols to a lane, the rows dealt out to
+// four wavefronts, eight at a time.
+template <typename T> __device__ __forceinline__ void look_at_columns(const GradientArgs& p, uint32_t* largest, int block, int slab)
+{
+    __shared__ uint32_t s_most[4][2 * kWave];
+    __shared__ double s_sum[4][2 * kWave];
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int a = block * (2 * kWave) + 2 * lane;
+    const Range range = slab_of(listed(p.frames, p.rows), slab, kColumnSlabs);
+    const int at = a + 1 < p.A ? a : a < p.A ? a - 1 : 0;                    // (A is at least 2 here; the last symbol of an odd number is the upper of a pair)
+    uint32_t most[2] = {};
+    double sum[2] = {};
+    const int steps = (range.last - range.first + 31) / 32;
+    const StepRows list(p, range, lane);
+    int entry = steps > 0 ? list.ask(0) : 0;
+    for (int t = 0; t < steps; ++t) {
+        const int row = list.row(t, entry);
+        const float scales = row < 0 ? 0.0f : p.scales[row];
+        entry = list.ask(t + 1);
+        T g[8][2];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int r = __builtin_amdgcn_readlane(row, wave * 8 + j);
+            __builtin_memcpy(g[j], static_cast<const T*>(p.grads) + static_cast<int64_t>(r < 0 ? 0 : r) * p.A + at, sizeof(g[j]));
+        }
+        float eight[2] = {};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (__builtin_amdgcn_readlane(row, wave * 8 + j) < 0) continue;
+            const float scale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scales), wave * 8 + j));
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const float v = widen(g[j][k]);
+                const uint32_t bits = __float_as_uint(v * scale) & 0x7fffffffu;
+                most[k] = most[k] > bits ? most[k] : bits;
+                eight[k] += v;
+            }
+        }
+        sum[0] += static_cast<double>(eight[0]);
+        sum[1] += static_cast<double>(eight[1]);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        s_most[wave][2 * lane + k] = most[k];
+        s_sum[wave][2 * lane + k] = sum[k];
+    }
+    __syncthreads();
+    const int mine = block * (2 * kWave) + threadIdx.x;
+    if (threadIdx.x >= 2 * kWave || mine >= p.A) return;
+    const int from = mine == p.A - 1 && mine % 2 == 0 ? threadIdx.x + 1 : threadIdx.x;
+    uint32_t m = 0;
+    double total = 0.0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        m = m > s_most[w][from] ? m : s_most[w][from];
+        total += s_sum[w][from];
+    }
+    largest[static_cast<int64_t>(slab) * p.A + mine] = m;
+    if (p.bias) p.bias[static_cast<int64_t>(slab) * p.A + mine] = static_cast<float>(total);
+}
 
 // Gradients of one symbol in eight rows, as they are in memory; the rows, and their scales, a lane each.
 struct Eight {
