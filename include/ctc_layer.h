@@ -20,6 +20,7 @@
  * only, and on an error found during validation nothing has been enqueued.  No call reads host
  * memory or keeps anything between calls, so all of them may be recorded into a HIP graph; a replay
  * reads every device buffer afresh.  Results are bitwise repeatable from run to run on one device.
+ * Calls that may overlap in time need outputs and workspaces of their own.
  * As for the other calls, `stream` and all buffers belong to the calling thread's current device.
  *
  * Rows.  States are matrices [rows, H], activations [rows, A], the last index fastest, without gaps.

@@ -95,6 +95,9 @@ __device__ __forceinline__ int row_at(const int32_t* frames, int rows, int64_t i
     return i < n && r >= 0 && r < rows ? r : -1;
 }
 
+// Number of this workgroup in a grid that launch code has spread over two dimensions (spread() below).
+__device__ __forceinline__ int64_t group_number() { return static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x; }
+
 // ---- sums and maxima over lanes ---------------------------------------------------------------------------------
 
 __device__ __forceinline__ uint32_t wave_max(uint32_t v)
@@ -119,8 +122,10 @@ template <typename V> __device__ __forceinline__ V wave_sum(V v)
 __global__ __launch_bounds__(256) void ctc_pack_frames_kernel(const int32_t* __restrict__ lengths, int T, int B,
                                                               int32_t* __restrict__ frames)
 {
-    const int lane = threadIdx.x % kWave, t = blockIdx.x * 4 + threadIdx.x / kWave;
-    if (t >= T) return;
+    const int lane = threadIdx.x % kWave;
+    const int64_t frame = group_number() * 4 + threadIdx.x / kWave;
+    if (frame >= T) return;
+    const int t = static_cast<int>(frame);
     int before = 0, all = 0;
     for (int b = lane; b < B; b += kWave) {
         int n = lengths[b];
@@ -181,7 +186,7 @@ __global__ __launch_bounds__(256) void ctc_rows_to_8_bits_kernel(NormArgs p)
 {
     constexpr int kE = Vector<T>::kElements, kVectors = E / kE;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int i = blockIdx.x * (4 / WAVES) + wave / WAVES;
+    const int64_t i = group_number() * (4 / WAVES) + wave / WAVES;
     const int r = row_at(p.frames, p.rows, i);
     if (r < 0) return;
     const int thread = (wave % WAVES) * kWave + lane;
@@ -265,7 +270,8 @@ __global__ __launch_bounds__(256) void ctc_rows_from_8_bits_kernel(const int8_t*
                                                                    T* __restrict__ out)
 {
     constexpr int kE = Vector<T>::kElements;
-    const int lane = threadIdx.x % kWave, i = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int lane = threadIdx.x % kWave;
+    const int64_t i = group_number() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int r = row_at(frames, rows, i);
     if (r < 0) return;
     const float scale = scales[r];
@@ -1223,9 +1229,16 @@ int last_error() { return static_cast<int>(hipGetLastError()); }
 
 unsigned blocks(int64_t items, int per_block) { return static_cast<unsigned>((items + per_block - 1) / per_block); }
 
+// A grid of `groups` workgroups and some: a dimension has fewer than 2^32 threads, rows may be 2^30.
+dim3 spread(unsigned groups)
+{
+    constexpr unsigned kAcross = 1u << 22;
+    return groups <= kAcross ? dim3(groups) : dim3(kAcross, (groups + kAcross - 1) / kAcross);
+}
+
 template <typename T, bool NORM> void launch_to_8_bits(const NormArgs& p, hipStream_t s)
 {
-    const dim3 block(256), wide(static_cast<unsigned>(p.rows)), narrow_rows(blocks(p.rows, 4));
+    const dim3 block(256), wide = spread(static_cast<unsigned>(p.rows)), narrow_rows = spread(blocks(p.rows, 4));
     // Few rows (not even a wavefront to a compute unit's SIMD) take four wavefronts each, for the time that one row takes; one each
     // asks for nothing between wavefronts.
     const bool few = p.rows <= 512;
@@ -1314,7 +1327,7 @@ template <typename T> void launch_gradient(const GradientArgs& p, const Gradient
 
 int launch_pack_frames(const int32_t* lengths, int T, int B, int32_t* frames, void* stream)
 {
-    hipLaunchKernelGGL(ctc_pack_frames_kernel, dim3(blocks(T, 4)), dim3(256), 0, static_cast<hipStream_t>(stream), lengths, T, B,
+    hipLaunchKernelGGL(ctc_pack_frames_kernel, spread(blocks(T, 4)), dim3(256), 0, static_cast<hipStream_t>(stream), lengths, T, B,
                        frames);
     return last_error();
 }
@@ -1343,7 +1356,7 @@ int launch_norm(const void* x, const void* residual, const float* weight, float 
 int launch_dequantize(const int8_t* q, const float* scales, const int32_t* frames, int rows, int H, bool bf16, void* out,
                       void* stream)
 {
-    const dim3 grid(blocks(rows, 4)), block(256);
+    const dim3 grid = spread(blocks(rows, 4)), block(256);
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (bf16)
         hipLaunchKernelGGL(ctc_rows_from_8_bits_kernel<bf16_t>, grid, block, 0, s, q, scales, frames, rows, H, pitch_of(H),

@@ -600,6 +600,27 @@ def test_places_beyond_32_bits():
     check_gradient(dweight, dbias, grads, got_q, got_s, np.arange(len(names)))
 
 
+def test_more_rows_than_a_grid_has_in_a_line():
+    """More than 2^26 rows, a wavefront each: 2^32 threads."""
+    rows, H = (1 << 26) + 3, 2
+    frames = torch.empty(1 + rows, dtype=torch.int32, device="cuda")
+    lengths = torch.tensor([rows], dtype=torch.int32, device="cuda")
+    layer.pack_frames(lengths.data_ptr(), rows, 1, frames.data_ptr(), stream())
+    torch.cuda.synchronize()
+    assert int(frames[0]) == rows and int(frames[1]) == 0 and int(frames[rows]) == rows - 1
+    names = [0, (1 << 26) - 1, 1 << 26, rows - 1]
+    frames[:5] = torch.tensor([4] + names, dtype=torch.int32, device="cuda")
+    x = torch.empty((rows, H), dtype=torch.bfloat16, device="cuda")
+    x[names] = torch.tensor([[1.0, -2.0], [3.0, 0.5], [0.0, 4.0], [-8.0, 8.0]], dtype=torch.bfloat16, device="cuda")
+    want = x[names].clone()
+    q, scales = torch.empty((rows, 128), dtype=torch.int8, device="cuda"), torch.empty(rows, device="cuda")
+    layer.quantize_rows(x.data_ptr(), frames.data_ptr(), rows, H, BF16, q.data_ptr(), scales.data_ptr(), stream())
+    assert torch.equal(q[names][:, :H].cpu().double(), ref.to_levels(want.float().cpu())[0])
+    x.zero_()
+    layer.dequantize_rows(q.data_ptr(), scales.data_ptr(), frames.data_ptr(), rows, H, BF16, x.data_ptr(), stream())
+    assert torch.equal(x[names].cpu(), (q[names][:, :H].cpu().float() * scales[names].cpu()[:, None]).to(torch.bfloat16))
+
+
 # ---- how the calls may be used ----------------------------------------------------------------------------------
 
 class Step:
