@@ -96,7 +96,9 @@ def pack_frames_status(input_lengths_ptr, T, B, frames_ptr, stream=0) -> int:
 
 def pack_frames(input_lengths_ptr, T, B, frames_ptr, stream=0) -> None:
     """The list of a minibatch's frames, int32 [1 + T * B], from its input lengths on the GPU."""
-    _check(pack_frames_status(input_lengths_ptr, T, B, frames_ptr, stream), "ctc_pack_frames")
+    st = (_native or _module()).pack_frames(input_lengths_ptr, T, B, frames_ptr, stream)
+    if st:
+        _check(st, "ctc_pack_frames")
 
 
 def quantize_rows_status(x_ptr, frames_ptr, rows, H, dtype, q_ptr, scales_ptr, stream=0) -> int:
@@ -105,7 +107,9 @@ def quantize_rows_status(x_ptr, frames_ptr, rows, H, dtype, q_ptr, scales_ptr, s
 
 def quantize_rows(x_ptr, frames_ptr, rows, H, dtype, q_ptr, scales_ptr, stream=0) -> None:
     """Rows to 8 bits: int8 [rows, row_pitch(H)] and a scale each."""
-    _check(quantize_rows_status(x_ptr, frames_ptr, rows, H, dtype, q_ptr, scales_ptr, stream), "ctc_quantize_rows")
+    st = (_native or _module()).quantize_rows(x_ptr, frames_ptr, rows, H, dtype, q_ptr, scales_ptr, stream)
+    if st:
+        _check(st, "ctc_quantize_rows")
 
 
 def dequantize_rows_status(q_ptr, scales_ptr, frames_ptr, rows, H, dtype, out_ptr, stream=0) -> int:
@@ -114,7 +118,9 @@ def dequantize_rows_status(q_ptr, scales_ptr, frames_ptr, rows, H, dtype, out_pt
 
 def dequantize_rows(q_ptr, scales_ptr, frames_ptr, rows, H, dtype, out_ptr, stream=0) -> None:
     """Rows from 8 bits."""
-    _check(dequantize_rows_status(q_ptr, scales_ptr, frames_ptr, rows, H, dtype, out_ptr, stream), "ctc_dequantize_rows")
+    st = (_native or _module()).dequantize_rows(q_ptr, scales_ptr, frames_ptr, rows, H, dtype, out_ptr, stream)
+    if st:
+        _check(st, "ctc_dequantize_rows")
 
 
 def rms_norm_i8_status(x_ptr, residual_ptr, weight_ptr, eps, frames_ptr, rows, H, dtype, sum_ptr, q_ptr, scales_ptr,
@@ -125,8 +131,10 @@ def rms_norm_i8_status(x_ptr, residual_ptr, weight_ptr, eps, frames_ptr, rows, H
 
 def rms_norm_i8(x_ptr, residual_ptr, weight_ptr, eps, frames_ptr, rows, H, dtype, sum_ptr, q_ptr, scales_ptr, stream=0) -> None:
     """Residual added, root-mean-square norm, rows to 8 bits."""
-    _check(rms_norm_i8_status(x_ptr, residual_ptr, weight_ptr, eps, frames_ptr, rows, H, dtype, sum_ptr, q_ptr, scales_ptr,
-                              stream), "ctc_rms_norm_i8")
+    st = (_native or _module()).rms_norm_i8(x_ptr, residual_ptr, weight_ptr, eps, frames_ptr, rows, H, dtype, sum_ptr, q_ptr,
+                                            scales_ptr, stream)
+    if st:
+        _check(st, "ctc_rms_norm_i8")
 
 
 def rms_norm_backward_status(dy_ptr, sum_ptr, weight_ptr, eps, dresidual_ptr, frames_ptr, rows, H, dtype, dsum_ptr,
@@ -138,8 +146,10 @@ def rms_norm_backward_status(dy_ptr, sum_ptr, weight_ptr, eps, dresidual_ptr, fr
 def rms_norm_backward(dy_ptr, sum_ptr, weight_ptr, eps, dresidual_ptr, frames_ptr, rows, H, dtype, dsum_ptr, dweight_ptr,
                       workspace_ptr, workspace_bytes, stream=0) -> None:
     """Gradient of the norm."""
-    _check(rms_norm_backward_status(dy_ptr, sum_ptr, weight_ptr, eps, dresidual_ptr, frames_ptr, rows, H, dtype, dsum_ptr,
-                                    dweight_ptr, workspace_ptr, workspace_bytes, stream), "ctc_rms_norm_backward")
+    st = (_native or _module()).rms_norm_backward(dy_ptr, sum_ptr, weight_ptr, eps, dresidual_ptr, frames_ptr, rows, H, dtype,
+                                                  dsum_ptr, dweight_ptr, workspace_ptr, workspace_bytes, stream)
+    if st:
+        _check(st, "ctc_rms_norm_backward")
 
 
 def linear_i8_status(q_ptr, scales_ptr, weight_q_ptr, weight_scales_ptr, bias_ptr, frames_ptr, rows, H, A, dtype, logits_ptr,
@@ -151,8 +161,10 @@ def linear_i8_status(q_ptr, scales_ptr, weight_q_ptr, weight_scales_ptr, bias_pt
 def linear_i8(q_ptr, scales_ptr, weight_q_ptr, weight_scales_ptr, bias_ptr, frames_ptr, rows, H, A, dtype, logits_ptr,
               stream=0) -> None:
     """Activations from rows and weights in 8 bits."""
-    _check(linear_i8_status(q_ptr, scales_ptr, weight_q_ptr, weight_scales_ptr, bias_ptr, frames_ptr, rows, H, A, dtype,
-                            logits_ptr, stream), "ctc_linear_i8")
+    st = (_native or _module()).linear_i8(q_ptr, scales_ptr, weight_q_ptr, weight_scales_ptr, bias_ptr, frames_ptr, rows, H, A,
+                                          dtype, logits_ptr, stream)
+    if st:
+        _check(st, "ctc_linear_i8")
 
 
 def weight_gradient_i8_status(grads_ptr, q_ptr, scales_ptr, frames_ptr, rows, H, A, dtype, dweight_ptr, dbias_ptr,
@@ -164,5 +176,7 @@ def weight_gradient_i8_status(grads_ptr, q_ptr, scales_ptr, frames_ptr, rows, H,
 def weight_gradient_i8(grads_ptr, q_ptr, scales_ptr, frames_ptr, rows, H, A, dtype, dweight_ptr, dbias_ptr, workspace_ptr,
                        workspace_bytes, stream=0) -> None:
     """The weights' and the bias's gradient from the activations' gradient and the rows in 8 bits."""
-    _check(weight_gradient_i8_status(grads_ptr, q_ptr, scales_ptr, frames_ptr, rows, H, A, dtype, dweight_ptr, dbias_ptr,
-                                     workspace_ptr, workspace_bytes, stream), "ctc_weight_gradient_i8")
+    st = (_native or _module()).weight_gradient_i8(grads_ptr, q_ptr, scales_ptr, frames_ptr, rows, H, A, dtype, dweight_ptr,
+                                                   dbias_ptr, workspace_ptr, workspace_bytes, stream)
+    if st:
+        _check(st, "ctc_weight_gradient_i8")
