@@ -1263,12 +1263,14 @@ template <typename T, bool NORM> void launch_to_8_bits(const NormArgs& p, hipStr
 template <typename T> void launch_backward(const NormBackArgs& p, unsigned groups, hipStream_t s)
 {
     const dim3 grid(groups);
+    // As few wavefronts to a row as hold it in registers, for each wavefront more is one more to wait for in the row's sum (5556 rows
+    // of 3204 fp32: four wavefronts of 16 a lane 54.7 us, eight of 8 58.6), until registers are what a compute unit runs out of.
     if (p.H <= 512)
         hipLaunchKernelGGL((ctc_norm_backward_kernel<T, 1, 8>), grid, dim3(256), 0, s, p);
     else if (p.H <= 2048)
         hipLaunchKernelGGL((ctc_norm_backward_kernel<T, 4, 8>), grid, dim3(256), 0, s, p);
     else if (p.H <= 4096)
-        hipLaunchKernelGGL((ctc_norm_backward_kernel<T, 8, 8>), grid, dim3(512), 0, s, p);
+        hipLaunchKernelGGL((ctc_norm_backward_kernel<T, 4, 16>), grid, dim3(256), 0, s, p);
     else if (p.H <= 8192)
         hipLaunchKernelGGL((ctc_norm_backward_kernel<T, 16, 8>), grid, dim3(1024), 0, s, p);
     else
