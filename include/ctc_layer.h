@@ -156,7 +156,8 @@ ctc_status_t ctc_linear_i8(const int8_t *q, const float *scales, const int8_t *w
  *
  * grads[r][a] * scales[r] is rounded to fp32 and enters the matrix cores in parts of 16 bits that hold it to
  * within 2^-23 of itself (alphabets of more than 64 symbols: or 2^-38 of its symbol's largest, if that is
- * more); sums are in fp32, in an order that the sizes and the list fix.  An infinity or a NaN among what is summed gives a NaN.
+ * more); sums are in fp32, in an order that the sizes and the list fix.  A product that is an infinity or a NaN gives
+ * its symbol's row of dweight NaNs.
  *
  *   grads      (device) [rows, A] of type dtype, as ctc_loss_and_grad writes them
  *   q, scales  (device) as ctc_rms_norm_i8 or ctc_quantize_rows wrote them

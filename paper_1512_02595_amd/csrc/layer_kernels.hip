@@ -374,15 +374,15 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void ctc_norm_bac
             turn ^= 1;
         }
         const double variance = squares / p.H + static_cast<double>(p.eps);
-        const double factor = 1.0 / sqrt(variance);
-        const float f = static_cast<float>(factor), c = static_cast<float>(along / p.H / variance * factor);
+        // (the mean's share without the factor: with it, it would vanish in fp32 for rows of 1e20 and more)
+        const float f = static_cast<float>(1.0 / sqrt(variance)), c = static_cast<float>(along / p.H / variance);
 #pragma unroll
         for (int v = 0; v < kVectors; ++v) {
 #pragma unroll
             for (int k = 0; k < kE; ++k) {
                 const float g = widen(dy[v].v[k]), zk = widen(z[v].v[k]);
                 dw[v * kE + k] += g * (zk * f);
-                d[v].v[k] = narrow<T>((g * w[v * kE + k]) * f - zk * c + widen(d[v].v[k]));
+                d[v].v[k] = narrow<T>((g * w[v * kE + k] - zk * c) * f + widen(d[v].v[k]));
             }
             store_vector(static_cast<T*>(p.dsum) + row, (v * kWidth + thread) * kE, p.H, d[v]);
         }

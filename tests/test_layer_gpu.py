@@ -287,6 +287,19 @@ def test_rms_norm_backward_without_its_options(rows, H, dtype):
     assert torch.equal(again.t, out.t) and out.intact()
 
 
+def test_norm_gradients_of_huge_and_tiny_rows():
+    """Both terms of a gradient of ordinary size, where the sums and their gradients are far from it on either side."""
+    rng = np.random.default_rng(12)
+    rows, H = 5, 700
+    size = torch.tensor([1e25, 1e-25, 1e30, 1e-15, 1e19])[:, None]
+    z, dy = (torch.from_numpy(rng.standard_normal((rows, H)) + 1.0).float() * size for _ in range(2))
+    w = torch.from_numpy(1.0 + 0.5 * rng.standard_normal(H)).float()
+    out, dweight = backward(put(dy, torch.float32), put(z, torch.float32), put(w, torch.float32), None, F32, rows, H, 1e-30)
+    for r in range(rows):
+        check_backward(out, None, dy, z, w, None, F32, rows, H, 1e-30, np.array([r]))
+    check_backward(out, dweight, dy, z, w, None, F32, rows, H, 1e-30, np.arange(rows))
+
+
 @pytest.mark.parametrize("which", ["dy", "sum", "dresidual"])
 def test_the_gradient_may_replace_an_input(which):
     rng = np.random.default_rng(8)
