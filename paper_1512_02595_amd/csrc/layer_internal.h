@@ -16,11 +16,12 @@ constexpr int kMaxSymbols = 1 << 20;
 
 inline int pitch_of(int H) { return (H + kPitch - 1) / kPitch * kPitch; }
 
-// The norm's backward pass: so many workgroups leave a partial sum of dweight each, two turns of rows to each (four rows at once up to
-// 512 wide) or more.  (684 rows of 1483, whole call: two rows to a workgroup 14.4 us, eight 23.4.)
+// The norm's backward pass: so many workgroups leave a partial sum of dweight each; they take one turn of rows (four rows at once up to
+// 1024 wide) or two.  (300 rows of 1024 bf16: one turn of four 6.6 us, two 7.4; 300 of 2048: two rows 8.0, four 9.1; 27200 of 1024 fp32: 1024
+// workgroups 57.2, 2048 59.6.)
 inline int norm_partials(int rows, int H)
 {
-    const int per_group = H <= 512 ? 8 : 2;
+    const int per_group = H <= 1024 ? 4 : 2;
     const int groups = (rows + per_group - 1) / per_group;
     return groups < 1024 ? groups : 1024;
 }

@@ -179,17 +179,17 @@ struct NormArgs {
     float* scales;
 };
 
-// One row to a wavefront, or to the four of a workgroup; a row's elements stay in registers (E to a thread) from its one
+// One row to a wavefront (four rows to a workgroup), or to all wavefronts of a workgroup; a row's elements stay in registers (E to a thread) from its one
 // reading to its writing, its maximum and its sum of squares are formed across lanes.  Bound by the bytes.
 template <typename T, int WAVES, int E, bool NORM>
-__global__ __launch_bounds__(256) void ctc_rows_to_8_bits_kernel(NormArgs p)
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void ctc_rows_to_8_bits_kernel(NormArgs p)
 {
     constexpr int kE = Vector<T>::kElements, kVectors = E / kE;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int64_t i = group_number() * (4 / WAVES) + wave / WAVES;
+    const int64_t i = WAVES == 1 ? group_number() * 4 + wave : group_number();
     const int r = row_at(p.frames, p.rows, i);
     if (r < 0) return;
-    const int thread = (wave % WAVES) * kWave + lane;
+    const int thread = WAVES == 1 ? lane : threadIdx.x;
     const T* x = static_cast<const T*>(p.x) + static_cast<int64_t>(r) * p.H;
     const T* residual = NORM && p.residual ? static_cast<const T*>(p.residual) + static_cast<int64_t>(r) * p.H : nullptr;
     float u[E];
@@ -227,16 +227,20 @@ __global__ __launch_bounds__(256) void ctc_rows_to_8_bits_kernel(NormArgs p)
     most = wave_max(most);
     if constexpr (NORM) squares = wave_sum(squares);
     if constexpr (WAVES > 1) {
-        __shared__ uint32_t s_most[4];
-        __shared__ double s_squares[4];
+        __shared__ uint32_t s_most[WAVES];
+        __shared__ double s_squares[WAVES];
         if (lane == 0) {
             s_most[wave] = most;
-            s_squares[wave] = squares;
+            if constexpr (NORM) s_squares[wave] = squares;
         }
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < 4; ++w) most = most > s_most[w] ? most : s_most[w];
-        squares = s_squares[0] + s_squares[1] + s_squares[2] + s_squares[3];
+        for (int w = 0; w < WAVES; ++w) most = most > s_most[w] ? most : s_most[w];
+        if constexpr (NORM) {
+            squares = 0.0;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) squares += s_squares[w];
+        }
     }
     // A row that is not finite: zeros, and a scale that says so.  Rows of tiny values are lifted, which is exact.
     const bool finite = most < kInfinity;
@@ -415,20 +419,23 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void ctc_norm_bac
         }
 }
 
-// out[k] = sum over p of partials[p * stride + k], in fp64; 16 lanes of rows and 64 columns to a workgroup of 1024.
+// out[k] = sum over p of partials[p * stride + k], in fp64; 64 rows by 16 columns to a workgroup at once, so that few columns make enough workgroups
+// and a thread's loads are under way together (16 rows by 64 columns: the norm's gradient of 1500 rows of 1024 bf16 11.4 us, so 9.9).
 __global__ __launch_bounds__(1024) void ctc_sum_partials_kernel(const float* __restrict__ partials, int count, int64_t stride,
                                                                 int64_t width, float* __restrict__ out)
 {
-    __shared__ double s_sum[16][kWave];
-    const int lane = threadIdx.x % kWave, group = threadIdx.x / kWave;
-    const int64_t col = static_cast<int64_t>(blockIdx.x) * kWave + lane;
+    __shared__ double s_sum[16][16];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int64_t col = static_cast<int64_t>(blockIdx.x) * 16 + lane % 16;
     double sum = 0.0;
     if (col < width)
 #pragma unroll 16
-        for (int p = group; p < count; p += 16) sum += static_cast<double>(partials[p * stride + col]);
-    s_sum[group][lane] = sum;
+        for (int p = wave * 4 + lane / 16; p < count; p += 64) sum += static_cast<double>(partials[p * stride + col]);
+    sum += __shfl_xor(sum, 16, kWave);
+    sum += __shfl_xor(sum, 32, kWave);
+    if (lane < 16) s_sum[wave][lane] = sum;
     __syncthreads();
-    if (group == 0 && col < width) {
+    if (threadIdx.x < 16 && col < width) {
 #pragma unroll
         for (int g = 1; g < 16; ++g) sum += s_sum[g][lane];
         out[col] = static_cast<float>(sum);
@@ -1038,11 +1045,11 @@ __device__ __forceinline__ void widen_rows(const GradientArgs& p, uint16_t* wide
 template <typename T>
 __global__ __launch_bounds__(256) void ctc_gradient_prepare_kernel(GradientArgs p, uint32_t* largest, uint16_t* wide, unsigned column_blocks)
 {
-    const unsigned columns = column_blocks * kColumnSlabs;
-    if (blockIdx.x < columns) {
-        look_at_columns<T>(p, largest, blockIdx.x % column_blocks, blockIdx.x / column_blocks);
+    const unsigned columns = column_blocks * kColumnSlabs, group = static_cast<unsigned>(group_number());
+    if (group < columns) {
+        look_at_columns<T>(p, largest, group % column_blocks, group / column_blocks);
     } else {
-        const unsigned across = static_cast<unsigned>((p.pitch + 255) / 256), i = blockIdx.x - columns;
+        const unsigned across = static_cast<unsigned>((p.pitch + 255) / 256), i = group - columns;
         widen_rows(p, wide, static_cast<int>(i / across), static_cast<int>(i % across) * 256);
     }
 }
@@ -1236,37 +1243,49 @@ dim3 spread(unsigned groups)
     return groups <= kAcross ? dim3(groups) : dim3(kAcross, (groups + kAcross - 1) / kAcross);
 }
 
+template <typename T, bool NORM, int WAVES, int E> void launch_rows(const NormArgs& p, hipStream_t s)
+{
+    const unsigned groups = WAVES == 1 ? blocks(p.rows, 4) : static_cast<unsigned>(p.rows);
+    hipLaunchKernelGGL((ctc_rows_to_8_bits_kernel<T, WAVES, E, NORM>), spread(groups), dim3(WAVES == 1 ? 256 : WAVES * kWave), 0, s, p);
+}
 template <typename T, bool NORM> void launch_to_8_bits(const NormArgs& p, hipStream_t s)
 {
-    const dim3 block(256), wide = spread(static_cast<unsigned>(p.rows)), narrow_rows = spread(blocks(p.rows, 4));
-    // Few rows (not even a wavefront to a compute unit's SIMD) take four wavefronts each, for the time that one row takes; one each
-    // asks for nothing between wavefronts.
-    const bool few = p.rows <= 512;
-    if (few && p.pitch > 512 && p.pitch <= 2048)
-        hipLaunchKernelGGL((ctc_rows_to_8_bits_kernel<T, 4, 8, NORM>), wide, block, 0, s, p);
-    else if (few && p.pitch > 2048 && p.pitch <= 4096)
-        hipLaunchKernelGGL((ctc_rows_to_8_bits_kernel<T, 4, 16, NORM>), wide, block, 0, s, p);
-    else if (p.pitch <= 512)
-        hipLaunchKernelGGL((ctc_rows_to_8_bits_kernel<T, 1, 8, NORM>), narrow_rows, block, 0, s, p);
+    // 16 elements a lane, and so wavefronts by the width: more elements leave too few wavefronts to a compute unit for what memory takes (the
+    // norm's 27200 rows of 2048 fp32 by one wavefront with 32 a lane 137 us, by two with 16 125; 6000 of 3500 by
+    // two with 32 50 us, by four with 16 46).  Where rows are few, 8 a lane, for the time that one row takes (one row of 2048 bf16 4.1 us with 16, 3.4 with 8; 1500 rows 6.9
+    // and 6.0; 27200 rows to 8 bits 31.3 and 35.3).
+    const bool few = p.rows <= 2048;
+    if (p.pitch <= 512)
+        launch_rows<T, NORM, 1, 8>(p, s);
+    else if (few && p.pitch <= 1024)
+        launch_rows<T, NORM, 2, 8>(p, s);
+    else if (few && p.pitch <= 2048)
+        launch_rows<T, NORM, 4, 8>(p, s);
+    else if (few && p.pitch <= 4096)
+        launch_rows<T, NORM, 8, 8>(p, s);
     else if (p.pitch <= 1024)
-        hipLaunchKernelGGL((ctc_rows_to_8_bits_kernel<T, 1, 16, NORM>), narrow_rows, block, 0, s, p);
+        launch_rows<T, NORM, 1, 16>(p, s);
     else if (p.pitch <= 2048)
-        hipLaunchKernelGGL((ctc_rows_to_8_bits_kernel<T, 1, 32, NORM>), narrow_rows, block, 0, s, p);
+        launch_rows<T, NORM, 2, 16>(p, s);
     else if (p.pitch <= 4096)
-        hipLaunchKernelGGL((ctc_rows_to_8_bits_kernel<T, 1, 64, NORM>), narrow_rows, block, 0, s, p);
+        launch_rows<T, NORM, 4, 16>(p, s);
     else if (p.pitch <= 8192)
-        hipLaunchKernelGGL((ctc_rows_to_8_bits_kernel<T, 4, 32, NORM>), wide, block, 0, s, p);
-    else
-        hipLaunchKernelGGL((ctc_rows_to_8_bits_kernel<T, 4, 64, NORM>), wide, block, 0, s, p);
+        launch_rows<T, NORM, 8, 16>(p, s);
+    else                                                // (16 wavefronts with 16 a lane: the norm's 1500 rows of 12000 bf16 38 us, eight with 32 31)
+        launch_rows<T, NORM, 8, 32>(p, s);
 }
 
 template <typename T> void launch_backward(const NormBackArgs& p, unsigned groups, hipStream_t s)
 {
     const dim3 grid(groups);
-    // As few wavefronts to a row as hold it in registers, for each wavefront more is one more to wait for in the row's sum (5556 rows
-    // of 3204 fp32: four wavefronts of 16 a lane 54.7 us, eight of 8 58.6), until registers are what a compute unit runs out of.
+    // As few wavefronts to a row as hold it in registers, for each wavefront more is one more to wait for in the row's sums (27200 rows
+    // of 1024 bf16: one wavefront with 16 a lane 39 us, two with 8 50, four with 8 67; 5556 of 3204 fp32: four with 16 54.7, eight with 8 58.6),
+    // until registers are what a compute unit runs out of (5600 of 1999 fp32: two with 16 37.3, four with 8 35.1; 4000 of 5000: eight with
+    // 16 66, sixteen with 8 62).
     if (p.H <= 512)
         hipLaunchKernelGGL((ctc_norm_backward_kernel<T, 1, 8>), grid, dim3(256), 0, s, p);
+    else if (p.H <= 1024)
+        hipLaunchKernelGGL((ctc_norm_backward_kernel<T, 1, 16>), grid, dim3(256), 0, s, p);
     else if (p.H <= 2048)
         hipLaunchKernelGGL((ctc_norm_backward_kernel<T, 4, 8>), grid, dim3(256), 0, s, p);
     else if (p.H <= 4096)
@@ -1319,7 +1338,7 @@ template <typename T> void launch_gradient(const GradientArgs& p, const Gradient
     } else {
         uint16_t* const wide = reinterpret_cast<uint16_t*>(workspace + plan.wide_at);
         const unsigned columns = blocks(p.A, 2 * kWave);
-        hipLaunchKernelGGL(ctc_gradient_prepare_kernel<T>, dim3(columns * kColumnSlabs + blocks(p.rows, 32) * blocks(p.pitch, 256)), dim3(256), 0, s, p,
+        hipLaunchKernelGGL(ctc_gradient_prepare_kernel<T>, spread(columns * kColumnSlabs + blocks(p.rows, 32) * blocks(p.pitch, 256)), dim3(256), 0, s, p,
                            reinterpret_cast<uint32_t*>(workspace + plan.largest_at), wide, columns);
         hipLaunchKernelGGL(ctc_weight_gradient_wide_kernel<T>, grid, dim3(512), 0, s, p, wide);
     }
@@ -1382,7 +1401,7 @@ int launch_norm_backward(const void* dy, const void* sum, const float* weight, f
         launch_backward<float>(p, static_cast<unsigned>(groups), s);
     const int err = last_error();
     if (err || !dweight) return err;
-    hipLaunchKernelGGL(ctc_sum_partials_kernel, dim3(blocks(H, kWave)), dim3(1024), 0, s, partials, groups,
+    hipLaunchKernelGGL(ctc_sum_partials_kernel, dim3(blocks(H, 16)), dim3(1024), 0, s, partials, groups,
                        static_cast<int64_t>(H), static_cast<int64_t>(H), dweight);
     return last_error();
 }
