@@ -155,7 +155,7 @@ ctc_status_t ctc_linear_i8(const int8_t *q, const float *scales, const int8_t *w
  *     dbias[a]      = sum over the listed rows of  grads[r][a]
  *
  * grads[r][a] * scales[r] is rounded to fp32 and enters the matrix cores in parts of 16 bits that hold it to
- * within 2^-23 of itself (alphabets of more than 64 symbols: or 2^-38 of its symbol's largest, if that is
+ * within 2^-23 of itself (where symbols, states and rows are many: or 2^-38 of its symbol's largest, if that is
  * more); sums are in fp32, in an order that the sizes and the list fix.  A product that is an infinity or a NaN gives
  * its symbol's row of dweight NaNs.
  *

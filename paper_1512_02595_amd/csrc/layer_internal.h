@@ -32,30 +32,42 @@ constexpr int kColumnSlabs = 64;                // workgroups that look at one s
 struct GradientPlan {
     int symbols, columns;                       // of a tile: 32 or 64 by 256, 128 by 512
     int slabs;
+    double time;                                // a guess, for choices
     int bias_slabs;
     size_t bias_at, largest_at, wide_at, bytes; // places in the workspace, in floats; all of it, in bytes
 };
 inline GradientPlan gradient_plan(int rows, int H, int A)
 {
-    GradientPlan p{};
-    p.symbols = A <= 32 ? 32 : A <= 64 ? 64 : 128;
-    p.columns = A <= 64 ? 256 : 512;
-    const long tiles = ((A + p.symbols - 1L) / p.symbols) * ((H + p.columns - 1L) / p.columns);
     const long steps = (rows + 31L) / 32;
-    // Time in steps of 32 rows: as many rounds of workgroups as the 256 compute units take (two workgroups each where tiles are narrow), each of its
-    // share of the steps and a few to begin and end with; and every slab's sums are written and read once more.
-    const long at_once = p.symbols <= 64 ? 512 : 256;
-    const double slab_cost = 8.0 * A * H / 5.0e6 / (p.symbols <= 64 ? 1.5 : 1.7);
-    double best = 0.0;
-    for (long s = 1; s <= 256 && s <= (steps + 3) / 4; ++s) {
-        const long rounds = (tiles * s + at_once - 1) / at_once;
-        const double cost = static_cast<double>(rounds) * (static_cast<double>((steps + s - 1) / s) + 6.0) + (s > 1 ? s * slab_cost + 6.0 : 0.0);
-        if (s == 1 || cost < best) {
-            best = cost;
-            p.slabs = static_cast<int>(s);
+    const auto plan = [&](int symbols) {
+        GradientPlan p{};
+        const bool wide = symbols == 128;
+        p.symbols = symbols;
+        p.columns = wide ? 512 : 256;
+        const long tiles = ((A + symbols - 1L) / symbols) * ((H + p.columns - 1L) / p.columns);
+        // Time (us): as many rounds of workgroups as the 256 compute units take (two workgroups each where tiles are narrow), each of its share of the
+        // steps of 32 rows and a few to begin and end with; every slab's sums written and read once more.
+        const long at_once = wide ? 256 : 512;
+        const double step = wide ? 1.7 : 1.5, slab_cost = 8.0 * A * H / 5.0e6;
+        for (long s = 1; s <= 256 && s <= (steps + 3) / 4; ++s) {
+            const long rounds = (tiles * s + at_once - 1) / at_once;
+            const double time = static_cast<double>(rounds) * (static_cast<double>((steps + s - 1) / s) + 6.0) * step + (s > 1 ? s * slab_cost + 6.0 * step : 0.0);
+            if (s == 1 || time < p.time) {
+                p.time = time;
+                p.slabs = static_cast<int>(s);
+            }
         }
+        return p;
+    };
+    GradientPlan p = plan(A <= 32 ? 32 : 64);
+    if (A > 64) {
+        // Wide tiles need a launch before theirs (the columns' largest, the rows' numbers as fp16) and are a fourth as many, each of which takes a
+        // third fewer products.  (Narrow and wide, us, fp32: 514 rows, 2048 wide, 172 symbols 15 and 27, 6000 symbols 59 and 52; 4000 rows,
+        // 1000 symbols 70 and 70; 12000 rows, 172 symbols 46 and 69, 1000 symbols 178 and 139, 6000 symbols 1035 and 662.)
+        const GradientPlan wide = plan(128);
+        if (wide.time + 20.0 <= 1.1 * p.time) p = wide;
     }
-    const bool wide = p.symbols == 128;         // the columns' largest, and the rows' numbers as fp16, come first
+    const bool wide = p.symbols == 128;
     p.bias_slabs = wide ? kColumnSlabs : p.slabs;
     p.bias_at = p.slabs > 1 ? static_cast<size_t>(p.slabs) * A * H : 0;
     p.largest_at = p.bias_at + static_cast<size_t>(p.bias_slabs) * A;

@@ -704,10 +704,10 @@ __global__ __launch_bounds__(256) void ctc_linear_tiles_kernel(LinearArgs p)
 // gradients take their scale and are split, and whole numbers become floats, and are laid down in LDS with the rows innermost.
 //
 // A product of gradient and scale, an fp32 number c, enters the matrix cores
-//   as three bf16 numbers, the leading 8 bits, the next 8 and the last (exact at any size): alphabets of at most 64 symbols, whose
-//   gradient is bound by the rows' bytes, or
+//   as three bf16 numbers, the leading 8 bits, the next 8 and the last (exact at any size): narrow tiles, whose gradients' work is done as
+//   they come, or
 //   as two fp16 numbers, each rounded to nearest (22 bits and a sign; c is off by at most half its last bit or 2^-39 of its column's
-//   largest), after a power of two that puts the column's largest in [2^14, 2^15): wider ones, which the matrix cores bind.  The columns' largest
+//   largest), after a power of two that puts the column's largest in [2^14, 2^15): wide tiles, which the matrix cores bind.  The columns' largest
 //   take one more reading of the gradients, a launch of its own, which also forms the bias's gradient.
 // The whole numbers are exact in either type.
 
@@ -864,7 +864,7 @@ __device__ __forceinline__ void clear(Eight& e, int first)
 }
 __device__ __forceinline__ float scale_of(const Eight& e, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(e.scale), lane)); }
 
-// At most 64 symbols.  32 NA symbols by 256 columns to a workgroup of eight wavefronts, 32 NA by 32 to each; 32 rows a step, in two buffers of
+// Narrow tiles: 32 NA symbols by 256 columns to a workgroup of eight wavefronts, 32 NA by 32 to each; 32 rows a step, in two buffers of
 // LDS: in a step a wavefront lays down the next step's operands, asks memory for what it will lay down kAhead steps later, and multiplies.
 // LDS: symbol a's 8-row piece j (16 bytes) lies at 64 a + 16 (j ^ a / 4 % 4); column k's at 64 (64 (k % 4) + k / 4) + 16 (j ^ k % 4 ^ k / 16 % 4):
 // what lanes write or read at once then falls on different banks.
@@ -876,14 +876,14 @@ __global__ __launch_bounds__(512) void ctc_weight_gradient_narrow_kernel(Gradien
     constexpr int kTA = 32 * NA, kPartBytes = kTA * 64, kNumbers = 3 * kPartBytes, kBytes = kNumbers + 256 * 64, kAhead = 2;
     __shared__ __align__(1024) int8_t s_buffer[2][kBytes];
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int k0 = blockIdx.y * 256, slab = blockIdx.z, chunk = wave % 4 * 8;
+    const int a0 = blockIdx.x * kTA, k0 = blockIdx.y * 256, slab = blockIdx.z, chunk = wave % 4 * 8;
     const Range range = slab_of(listed(p.frames, p.rows), slab, p.slabs);
     const int steps = (range.last - range.first + 31) / 32;
     const StepRows list(p, range, lane);
-    // What this lane brings: symbol `lane` of rows `chunk` .. (four wavefronts), columns 4 lane .. of rows 4 wave ..  (Symbols behind the
+    // What this lane brings: symbol a0 + lane of rows `chunk` .. (four wavefronts), columns 4 lane .. of rows 4 wave ..  (Symbols behind the
     // last and columns behind a row's bytes are others' once more: what becomes of them is not written.)
     const bool brings = wave < 4 && lane < kTA;
-    const uint32_t at = static_cast<uint32_t>(lane < p.A ? lane : p.A - 1) * static_cast<uint32_t>(sizeof(T));
+    const uint32_t at = static_cast<uint32_t>(a0 + lane < p.A ? a0 + lane : p.A - 1) * static_cast<uint32_t>(sizeof(T));
     const uint32_t column = static_cast<uint32_t>(k0 + 4 * lane < p.pitch ? k0 + 4 * lane : 0);
     struct Raw {
         Eight e;
@@ -997,7 +997,7 @@ __global__ __launch_bounds__(512) void ctc_weight_gradient_narrow_kernel(Gradien
             }
             __syncthreads();
         }
-        if (wave == 3 && lane < p.A) p.bias[static_cast<int64_t>(slab) * p.A + lane] = static_cast<float>(bias);
+        if (wave == 3 && lane < kTA && a0 + lane < p.A) p.bias[static_cast<int64_t>(slab) * p.A + a0 + lane] = static_cast<float>(bias);
     }
     float* const out = p.out + static_cast<int64_t>(slab) * p.A * p.H;
     const int k = k0 + wave * 32 + lane % 32;
@@ -1005,12 +1005,12 @@ __global__ __launch_bounds__(512) void ctc_weight_gradient_narrow_kernel(Gradien
     for (int i = 0; i < NA; ++i)
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
-            const int a = i * 32 + 8 * (v / 4) + 4 * (lane / 32) + v % 4;
+            const int a = a0 + i * 32 + 8 * (v / 4) + 4 * (lane / 32) + v % 4;
             if (a < p.A && k < p.H) out[static_cast<int64_t>(a) * p.H + k] = sum[i][v];
         }
 }
 
-// More than 64 symbols: the whole numbers of the listed rows as fp16, once for all symbols' workgroups.  32 listed rows at a time (a step), for each
+// For wide tiles: the whole numbers of the listed rows as fp16, once for all symbols' workgroups.  32 listed rows at a time (a step), for each
 // column k 64 bytes, its 8-row pieces in the order j ^ k / 4 % 4: as the kernel below wants them in LDS.  256 columns to a workgroup.
 __device__ __forceinline__ void widen_rows(const GradientArgs& p, uint16_t* wide, int step, int k0)
 {

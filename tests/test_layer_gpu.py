@@ -498,6 +498,56 @@ def test_weight_gradient(rows, H, A, dtype, kind):
         assert not dweight.t.any() and not dbias.t.any()
 
 
+# (two tiles of symbols or more that the narrow kernel takes, and tiles of 128 symbols by 512 columns: several slabs, one)
+MANY_SYMBOLS = [(130, 1999, 200), (3000, 300, 191), (5000, 520, 65), (33, 5000, 5001), (200, 1999, 5001), (4000, 1111, 2999), (9000, 700, 2001)]
+
+
+@pytest.mark.parametrize("kind", LISTS)
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows, H, A", MANY_SYMBOLS)
+def test_weight_gradient_of_many_symbols(rows, H, A, dtype, kind):
+    say("weight gradient, many symbols", rows, H, A, dtype, kind)
+    rng = np.random.default_rng(rows + H + A)
+    q, s = levels(rng, rows, H)
+    grads = gradients(rng, rows, A, dtype)
+    frames, names = frame_list(kind, rows, rng)
+    dweight, dbias = weight_gradient(grads, q, s, dtype, frames, names=names)
+    check_gradient(dweight, dbias, grads, q, s, names)
+    again, _ = weight_gradient(grads, q, s, dtype, frames, want_bias=False, names=names)
+    assert torch.equal(again.t, dweight.t)
+
+
+@pytest.mark.parametrize("dtype, shift", [(F32, 4), (BF16, 2)])
+def test_gradients_of_many_symbols_off_alignment_with_a_nan(dtype, shift):
+    rng = np.random.default_rng(shift + 50)
+    rows, H, A = 200, 1999, 5001
+    q, s = levels(rng, rows, H)
+    grads = gradients(rng, rows, A, dtype)
+    check_gradient(*weight_gradient(grads, q, s, dtype, shift=shift), grads, q, s, np.arange(rows))
+    grads[77, 5000] = float("nan")
+    grads[78, 5] = float("inf")
+    dweight, dbias = weight_gradient(grads, q, s, dtype, shift=shift)
+    whole = torch.ones(A, dtype=torch.bool)
+    whole[[5, 5000]] = False
+    got = dweight.t.cpu()
+    assert torch.isnan(got[~whole]).all() and torch.isfinite(got[whole]).all()
+    assert not torch.isfinite(dbias.t.cpu()[~whole]).any() and torch.isfinite(dbias.t.cpu()[whole]).all()
+
+
+def test_weight_gradient_of_many_symbols_holds_gradients_of_every_size():
+    """As below, where symbols share tiles of 128 and are lifted by powers of two of their own."""
+    rng = np.random.default_rng(13)
+    rows, H, A = 240, 1999, 5001
+    grads = (gradients(rng, rows, A, F32).double() * torch.from_numpy(10.0 ** rng.integers(-22, 23, (1, A)))).float()
+    q, s = levels(rng, rows, H)
+    s = s * torch.from_numpy(10.0 ** rng.integers(-2, 3, rows)).float()
+    dweight, dbias = weight_gradient(grads, q, s, F32)
+    y = q.double() * s.double()[:, None]
+    want = grads.double().t().contiguous() @ y
+    off = (dweight.t.cpu().double() - want).norm(dim=1) / want.norm(dim=1)
+    assert off.max() < 2e-6
+
+
 @pytest.mark.parametrize("A", [40, 100, 301])
 @pytest.mark.parametrize("dtype", TYPES)
 def test_weight_gradient_holds_gradients_of_every_size(dtype, A):
@@ -710,6 +760,23 @@ def test_graphs_are_replayed_on_new_contents(T, B, H, A, dtype):
         got = step.results()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
         assert any(t.any() for t in got)
+
+
+def test_a_graph_of_a_large_layer_between_eager_calls():
+    step = Step(22, 12, 20, 1999, 5001, BF16)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step.run(torch.cuda.current_stream().cuda_stream)
+    for _ in range(3):
+        step.fill()
+        step.clear()                                     # (rows that this minibatch does not list stay as they were)
+        step.run(stream())
+        want = step.results()
+        step.clear()
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(step.results(), want))
 
 
 def test_two_streams_at_once():
