@@ -760,17 +760,17 @@ struct StepRows {
     bool list;
     int rows;
     Range range;
-    int lane;
-    __device__ __forceinline__ StepRows(const GradientArgs& p, Range r, int l)
-        : entries(p.frames ? p.frames + 1 : reinterpret_cast<const int32_t*>(p.scales)), list(p.frames), rows(p.rows), range(r), lane(l) {}
+    int place;                   // which of a step's 32 this lane has
+    __device__ __forceinline__ StepRows(const GradientArgs& p, Range r, int which)
+        : entries(p.frames ? p.frames + 1 : reinterpret_cast<const int32_t*>(p.scales)), list(p.frames), rows(p.rows), range(r), place(which) {}
     __device__ __forceinline__ int ask(int step) const
     {
-        const int i = range.first + step * 32 + lane % 32;
+        const int i = range.first + step * 32 + place;
         return entries[i < range.last ? i : range.last - 1];
     }
     __device__ __forceinline__ int row(int step, int entry) const
     {
-        const int i = range.first + step * 32 + lane % 32;
+        const int i = range.first + step * 32 + place;
         const int r = list ? entry : i;
         return i < range.last && r >= 0 && r < rows ? r : -1;
     }
@@ -789,7 +789,7 @@ template <typename T> __device__ __forceinline__ void look_at_columns(const Grad
     uint32_t most[2] = {};
     double sum[2] = {};
     const int steps = (range.last - range.first + 31) / 32;
-    const StepRows list(p, range, lane);
+    const StepRows list(p, range, wave * 8 + lane % 8);
     int entry = steps > 0 ? list.ask(0) : 0;
     for (int t = 0; t < steps; ++t) {
         const int row = list.row(t, entry);
@@ -798,14 +798,14 @@ template <typename T> __device__ __forceinline__ void look_at_columns(const Grad
         T g[8][2];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int r = __builtin_amdgcn_readlane(row, wave * 8 + j);
+            const int r = __builtin_amdgcn_readlane(row, j);
             __builtin_memcpy(g[j], static_cast<const T*>(p.grads) + static_cast<int64_t>(r < 0 ? 0 : r) * p.A + at, sizeof(g[j]));
         }
         float eight[2] = {};
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            if (__builtin_amdgcn_readlane(row, wave * 8 + j) < 0) continue;
-            const float scale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scales), wave * 8 + j));
+            if (__builtin_amdgcn_readlane(row, j) < 0) continue;
+            const float scale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scales), j));
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const float v = widen(g[j][k]);
@@ -837,7 +837,25 @@ template <typename T> __device__ __forceinline__ void look_at_columns(const Grad
     if (p.bias) p.bias[static_cast<int64_t>(slab) * p.A + mine] = static_cast<float>(total);
 }
 
-// Gradients of one symbol in eight rows, as they are in memory; the rows, and their scales, a lane each.
+// What lies `at` bytes behind an address that is the same in all lanes and stays in scalar registers, as `at` stays 32 bits if it comes from here():
+// left alone the compiler adds a lane's place to the address before it multiplies the row by its pitch, with a vector instruction of
+// quarter rate for each load (27200 rows of 2048, 29 symbols: 33.3 us, so and with a step's rows in the same lanes of every wavefront 31.7).
+template <typename V> __device__ __forceinline__ V load_from(const void* row, uint32_t at)
+{
+    typedef const __attribute__((address_space(1))) char* Global;
+    Global from = (Global)row;
+    asm("" : "+s"(from));
+    return *(const __attribute__((address_space(1))) V*)(from + at);
+}
+
+// `at`, as far as the compiler knows another one for each `row`.
+__device__ __forceinline__ uint32_t here(uint32_t at, int row)
+{
+    asm("" : "+v"(at) : "v"(row));
+    return at;
+}
+
+// Gradients of one symbol in eight rows, as they are in memory; the rows, and their scales, in lanes 0 to 7 (and again in 8 to 15 and so on).
 struct Eight {
     int row;
     float scale;
@@ -848,18 +866,18 @@ template <typename T> __device__ __forceinline__ uint32_t gradient_of(const Grad
 {
     const char* from = static_cast<const char*>(p.grads) + static_cast<uint64_t>(row < 0 ? 0 : row) * (static_cast<uint32_t>(p.A) * sizeof(T));
     if constexpr (sizeof(T) == 2)
-        return *reinterpret_cast<const uint16_t*>(from + at);
+        return load_from<uint16_t>(from, at);
     else
-        return *reinterpret_cast<const uint32_t*>(from + at);
+        return load_from<uint32_t>(from, at);
 }
 template <typename T> __device__ __forceinline__ float gradient_in(uint32_t bits) { return __uint_as_float(sizeof(T) == 2 ? bits << 16 : bits); }
 // Gradients and scales of rows that do not count: 0, whatever is there.
-__device__ __forceinline__ void clear(Eight& e, int first)
+__device__ __forceinline__ void clear(Eight& e)
 {
     if (__ballot(e.row >= 0) == ~0ull) return;
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-        if (__builtin_amdgcn_readlane(e.row, first + j) < 0) e.g[j] = 0;
+        if (__builtin_amdgcn_readlane(e.row, j) < 0) e.g[j] = 0;
     if (e.row < 0) e.scale = 0.0f;
 }
 __device__ __forceinline__ float scale_of(const Eight& e, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(e.scale), lane)); }
@@ -879,8 +897,9 @@ __global__ __launch_bounds__(512) void ctc_weight_gradient_narrow_kernel(Gradien
     const int a0 = blockIdx.x * kTA, k0 = blockIdx.y * 256, slab = blockIdx.z, chunk = wave % 4 * 8;
     const Range range = slab_of(listed(p.frames, p.rows), slab, p.slabs);
     const int steps = (range.last - range.first + 31) / 32;
-    const StepRows list(p, range, lane);
-    // What this lane brings: symbol a0 + lane of rows `chunk` .. (four wavefronts), columns 4 lane .. of rows 4 wave ..  (Symbols behind the
+    // (wavefronts w and w + 4 have the same eight rows, the second with its four of whole numbers in front)
+    const StepRows list(p, range, chunk + (lane % 8 ^ wave / 4 * 4));
+    // What this lane brings: symbol a0 + lane of rows `chunk` .. (four wavefronts), columns 4 lane .. of half of these rows.  (Symbols behind the
     // last and columns behind a row's bytes are others' once more: what becomes of them is not written.)
     const bool brings = wave < 4 && lane < kTA;
     const uint32_t at = static_cast<uint32_t>(a0 + lane < p.A ? a0 + lane : p.A - 1) * static_cast<uint32_t>(sizeof(T));
@@ -892,20 +911,22 @@ __global__ __launch_bounds__(512) void ctc_weight_gradient_narrow_kernel(Gradien
     const auto ask = [&](Raw& to, int row) {
         to.e.row = row;
         to.e.scale = p.scales[row < 0 ? 0 : row];
+        const uint32_t from = here(column, row);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int r = __builtin_amdgcn_readlane(row, wave * 4 + j);
-            to.q[j] = *reinterpret_cast<const uint32_t*>(p.q + static_cast<uint64_t>(r < 0 ? 0 : r) * static_cast<uint32_t>(p.pitch) + column);
+            const int r = __builtin_amdgcn_readlane(row, j);
+            to.q[j] = load_from<uint32_t>(p.q + static_cast<uint64_t>(r < 0 ? 0 : r) * static_cast<uint32_t>(p.pitch), from);
         }
         if (brings) {
+            const uint32_t mine = here(at, row);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) to.e.g[j] = gradient_of<T>(p, __builtin_amdgcn_readlane(row, chunk + j), at);
+            for (int j = 0; j < 8; ++j) to.e.g[j] = gradient_of<T>(p, __builtin_amdgcn_readlane(row, j), mine);
         }
     };
     double bias = 0.0;
     const bool sums = p.bias && blockIdx.y == 0;
     const auto lay_down = [&](Raw& from, int8_t* buffer) {
-        clear(from.e, chunk);
+        clear(from.e);
         if (brings) {
             uint4v part[3];
             float eight = 0.0f;
@@ -916,7 +937,7 @@ __global__ __launch_bounds__(512) void ctc_weight_gradient_narrow_kernel(Gradien
                 for (int i = 0; i < 2; ++i) {
                     const float g = gradient_in<T>(from.e.g[j + i]);
                     eight += g;
-                    c[i] = g * scale_of(from.e, chunk + j + i);
+                    c[i] = g * scale_of(from.e, j + i);
                 }
 #pragma unroll
                 for (int b = 0; b < 3; ++b) {
@@ -940,7 +961,7 @@ __global__ __launch_bounds__(512) void ctc_weight_gradient_narrow_kernel(Gradien
                 const float v = static_cast<float>(static_cast<int8_t>(from.q[2 * j + 1] >> 8 * k));
                 four[j] = __builtin_amdgcn_perm(__float_as_uint(v), __float_as_uint(u), 0x07060302);
             }
-            *reinterpret_cast<uint2v*>(buffer + kNumbers + (k * 64 + lane) * 64 + ((wave / 2 ^ k ^ lane / 4 % 4) * 16) + wave % 2 * 8) = four;
+            *reinterpret_cast<uint2v*>(buffer + kNumbers + (k * 64 + lane) * 64 + ((wave % 4 ^ k ^ lane / 4 % 4) * 16) + wave / 4 * 8) = four;
         }
     };
     float16v sum[NA] = {};
@@ -1018,12 +1039,12 @@ __device__ __forceinline__ void widen_rows(const GradientArgs& p, uint16_t* wide
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int n = listed(p.frames, p.rows);
     if (step * 32 >= n) return;
-    const StepRows list(p, {0, n}, lane);
+    const StepRows list(p, {0, n}, wave * 8 + lane % 8);
     const int row = list.row(step, list.ask(step));
     if (k0 + 4 * lane < p.pitch) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int r = __builtin_amdgcn_readlane(row, wave * 8 + j);
+            const int r = __builtin_amdgcn_readlane(row, j);
             *reinterpret_cast<uint32_t*>(&s_row[wave * 8 + j][4 * lane]) =
                 *reinterpret_cast<const uint32_t*>(p.q + static_cast<uint64_t>(r < 0 ? 0 : r) * static_cast<uint32_t>(p.pitch) + k0 + 4 * lane);
         }
@@ -1077,7 +1098,7 @@ __global__ __launch_bounds__(512) void ctc_weight_gradient_wide_kernel(GradientA
     const int a0 = blockIdx.x * kTA, k0 = blockIdx.y * kTK, slab = blockIdx.z, chunk = wave % 4 * 8;
     const Range range = slab_of(listed(p.frames, p.rows), slab, p.slabs);
     const int steps = (range.last - range.first + 31) / 32;
-    const StepRows list(p, range, lane);
+    const StepRows list(p, range, chunk + lane % 8);
     if (static_cast<int>(threadIdx.x) < kTA) {
         uint32_t most = 0;
         if (a0 + static_cast<int>(threadIdx.x) < p.A)
@@ -1105,7 +1126,7 @@ __global__ __launch_bounds__(512) void ctc_weight_gradient_wide_kernel(GradientA
     uint4v part[2];
     // Two rows' gradients, split, and the write of eight rows' parts with the last of them.
     const auto split = [&](const Eight& e, int buffer, int j) {
-        const float c[2] = {gradient_in<T>(e.g[j]) * scale_of(e, chunk + j) * lift, gradient_in<T>(e.g[j + 1]) * scale_of(e, chunk + j + 1) * lift};
+        const float c[2] = {gradient_in<T>(e.g[j]) * scale_of(e, j) * lift, gradient_in<T>(e.g[j + 1]) * scale_of(e, j + 1) * lift};
         const half2 high = {static_cast<_Float16>(c[0]), static_cast<_Float16>(c[1])};
         const half2 low = {static_cast<_Float16>(c[0] - static_cast<float>(high[0])), static_cast<_Float16>(c[1] - static_cast<float>(high[1]))};
         part[0][j / 2] = __builtin_bit_cast(uint32_t, high);
@@ -1132,8 +1153,9 @@ __global__ __launch_bounds__(512) void ctc_weight_gradient_wide_kernel(GradientA
         // (A step's rows' numbers are asked for three steps before its rows.)
         Eight raw[3];
         int entry[3];
-        const auto ask = [&](Eight& e, int j) { e.g[j] = gradient_of<T>(p, __builtin_amdgcn_readlane(e.row, chunk + j), at); };
-        const auto rows = [&](Eight& e, int row) { e.row = row, e.scale = p.scales[row < 0 ? 0 : row]; };
+        uint32_t mine_at = at;
+        const auto ask = [&](Eight& e, int j) { e.g[j] = gradient_of<T>(p, __builtin_amdgcn_readlane(e.row, j), mine_at); };
+        const auto rows = [&](Eight& e, int row) { e.row = row, e.scale = p.scales[row < 0 ? 0 : row], mine_at = here(at, row); };
 #pragma unroll
         for (int t = 0; t < 3; ++t) {
 #pragma unroll
@@ -1142,7 +1164,7 @@ __global__ __launch_bounds__(512) void ctc_weight_gradient_wide_kernel(GradientA
             rows(raw[t], list.row(t, list.ask(t)));
 #pragma unroll
             for (int j = 0; j < 8; ++j) ask(raw[t], j);
-            clear(raw[t], chunk);
+            clear(raw[t]);
 #pragma unroll
             for (int j = 0; j < 8; j += 2) split(raw[t], t, j);
         }
@@ -1163,7 +1185,7 @@ __global__ __launch_bounds__(512) void ctc_weight_gradient_wide_kernel(GradientA
                 if (t >= steps) break;
                 const int now = s, next = (s + 1) % 3, down = (s + 2) % 3;
                 Eight& mine = raw[s];
-                clear(mine, chunk);
+                clear(mine);
                 const int row = list.row(t + 5, entry[s]);
                 // A wavefront's products and its other instructions run beside each other only if they come in turns, and LDS serves eight wavefronts'
                 // reads beside the products only if they are spread over them.
