@@ -839,12 +839,13 @@ template <typename T> __device__ __forceinline__ void look_at_columns(const Grad
 
 // What lies `at` bytes behind an address that is the same in all lanes and stays in scalar registers, as `at` stays 32 bits if it comes from here():
 // left alone the compiler adds a lane's place to the address before it multiplies the row by its pitch, with a vector instruction of
-// quarter rate for each load (27200 rows of 2048, 29 symbols: 33.3 us, so and with a step's rows in the same lanes of every wavefront 31.7).
+// quarter rate for each load (27200 rows of 2048, 29 symbols: 33.3 us, so, with a step's rows in the same lanes of every wavefront, 31.7).
 template <typename V> __device__ __forceinline__ V load_from(const void* row, uint32_t at)
 {
     typedef const __attribute__((address_space(1))) char* Global;
-    Global from = (Global)row;
-    asm("" : "+s"(from));
+    const uint64_t whole = reinterpret_cast<uint64_t>(row);
+    const uint32_t low = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(whole)), high = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(whole >> 32));
+    const Global from = reinterpret_cast<Global>(static_cast<uint64_t>(high) << 32 | low);
     return *(const __attribute__((address_space(1))) V*)(from + at);
 }
 
@@ -864,7 +865,7 @@ struct Eight {
 // Row `row`'s gradient of the symbol at `at` bytes.
 template <typename T> __device__ __forceinline__ uint32_t gradient_of(const GradientArgs& p, int row, uint32_t at)
 {
-    const char* from = static_cast<const char*>(p.grads) + static_cast<uint64_t>(row < 0 ? 0 : row) * (static_cast<uint32_t>(p.A) * sizeof(T));
+    const char* from = static_cast<const char*>(p.grads) + static_cast<uint64_t>(row < 0 ? 0 : row) * static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(p.A * static_cast<int>(sizeof(T))));
     if constexpr (sizeof(T) == 2)
         return load_from<uint16_t>(from, at);
     else
@@ -985,15 +986,17 @@ __global__ __launch_bounds__(512) void ctc_weight_gradient_narrow_kernel(Gradien
     if (steps > 0) {
         // A step's rows' numbers are asked for kAhead steps before its rows, these kAhead steps before they are laid down: nothing is waited for
         // that has not been under way as long.
-        Raw raw[kAhead];
-        int entry[kAhead];
-        ask(raw[0], list.row(0, list.ask(0)));
-        lay_down(raw[0], s_buffer[0]);
+        // (The first steps' are asked for together: three round trips to memory before the loop, and not five.)
+        Raw first, raw[kAhead];
+        int early[1 + kAhead], entry[kAhead];
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            ask(raw[j], list.row(1 + j, list.ask(1 + j)));
-            entry[j] = list.ask(1 + kAhead + j);
-        }
+        for (int j = 0; j <= kAhead; ++j) early[j] = list.ask(j);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) entry[j] = list.ask(1 + kAhead + j);
+        ask(first, list.row(0, early[0]));
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) ask(raw[j], list.row(1 + j, early[1 + j]));
+        lay_down(first, s_buffer[0]);
         meet();
         for (int t0 = 0; t0 < steps; t0 += kAhead) {
 #pragma unroll
