@@ -5,6 +5,8 @@ in the HIP library.  Used by the GPU tests, the smoke check and the benchmark.
 """
 from __future__ import annotations
 
+import contextlib
+
 import numpy as np
 import torch
 
@@ -163,6 +165,8 @@ class OutputLayer:
     DeviceBatch's or DeviceMetaBatch's `x`), `weight_gradient` takes CTC's gradient to the weights' and the bias's, from the rows that
     the forward pass left in 8 bits, and `norm_backward` the gradient of the norm's output to its input's.  Frames behind an
     utterance's end take no part.
+
+    All of a call's work is on `stream` (a handle; None: torch's current one), whose owner keeps the tensors until it is done.
     """
 
     def __init__(self, T, B, H, A, dtype: int = ctc.DTYPE_F32, eps=1e-6, logits=None, device=None):
@@ -189,6 +193,13 @@ class OutputLayer:
     def _stream(self, stream):
         return torch.cuda.current_stream(self.device).cuda_stream if stream is None else stream
 
+    def _on(self, stream):
+        """Where torch does its part of a call: on the call's stream."""
+        s = self._stream(stream)
+        if s == torch.cuda.current_stream(self.device).cuda_stream:
+            return contextlib.nullcontext()
+        return torch.cuda.stream(torch.cuda.ExternalStream(s, device=self.device))
+
     def _states(self, t):
         assert t.numel() == self.rows * self.H and t.dtype == self.sum.dtype and t.is_contiguous()
         return t.data_ptr()
@@ -198,10 +209,11 @@ class OutputLayer:
         assert tuple(weight.shape) == (self.A, self.H) and weight.dtype == torch.float32 and weight.is_contiguous()
         layer.quantize_rows(weight.data_ptr(), None, self.A, self.H, ctc.DTYPE_F32, self.weight_q.data_ptr(),
                             self.weight_scales.data_ptr(), self._stream(stream))
-        if bias is not None:
-            self.bias.copy_(bias)
-        if norm_weight is not None:
-            self.norm_weight.copy_(norm_weight)
+        with self._on(stream):
+            if bias is not None:
+                self.bias.copy_(bias)
+            if norm_weight is not None:
+                self.norm_weight.copy_(norm_weight)
 
     def set_lengths(self, input_lengths, stream=None):
         """int32 [B] on the GPU: the frames of this minibatch, for all calls until the next one's."""
