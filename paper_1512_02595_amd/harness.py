@@ -187,8 +187,9 @@ class OutputLayer:
         assert tuple(self.logits.shape) == (T, B, A) and self.logits.dtype == tdtype and self.logits.is_contiguous()
         self.dweight, self.dbias, self.dnorm_weight = zeros(A, H), zeros(A), zeros(H)
         self.ws_bytes = layer.weight_gradient_workspace_size(self.rows, H, A), layer.rms_norm_workspace_size(self.rows, H)
-        self.ws = torch.empty(max(self.ws_bytes) + 256, dtype=torch.uint8, device=self.device)
-        self.ws_ptr = (self.ws.data_ptr() + 255) // 256 * 256
+        # (the two gradients need nothing of each other and may be on two streams: a workspace each)
+        self.ws = [torch.empty(n + 256, dtype=torch.uint8, device=self.device) for n in self.ws_bytes]
+        self.ws_ptr = [(w.data_ptr() + 255) // 256 * 256 for w in self.ws]
 
     def _stream(self, stream):
         return torch.cuda.current_stream(self.device).cuda_stream if stream is None else stream
@@ -233,13 +234,13 @@ class OutputLayer:
     def weight_gradient(self, grads, stream=None):
         assert tuple(grads.shape) == (self.T, self.B, self.A) and grads.dtype == self.logits.dtype and grads.is_contiguous()
         layer.weight_gradient_i8(grads.data_ptr(), self.q.data_ptr(), self.scales.data_ptr(), self.frames.data_ptr(), self.rows,
-                                 self.H, self.A, self.dtype, self.dweight.data_ptr(), self.dbias.data_ptr(), self.ws_ptr,
+                                 self.H, self.A, self.dtype, self.dweight.data_ptr(), self.dbias.data_ptr(), self.ws_ptr[0],
                                  self.ws_bytes[0], self._stream(stream))
         return self.dweight, self.dbias
 
     def norm_backward(self, dy, dresidual=None, stream=None):
         layer.rms_norm_backward(self._states(dy), self.sum.data_ptr(), self.norm_weight.data_ptr(), self.eps,
                                 None if dresidual is None else self._states(dresidual), self.frames.data_ptr(), self.rows, self.H,
-                                self.dtype, self.dsum.data_ptr(), self.dnorm_weight.data_ptr(), self.ws_ptr, self.ws_bytes[1],
+                                self.dtype, self.dsum.data_ptr(), self.dnorm_weight.data_ptr(), self.ws_ptr[1], self.ws_bytes[1],
                                 self._stream(stream))
         return self.dsum, self.dnorm_weight

@@ -49,3 +49,27 @@ def test_weights_are_set_on_the_stream_that_is_given(handle):
     torch.cuda.synchronize()
     assert torch.equal(got, want) and want.any()
     assert torch.equal(layers[1].bias, bias) and torch.equal(layers[1].norm_weight, norm)
+
+
+def test_gradients_on_two_streams():
+    """The weights' and the norm's gradient need nothing of each other: neither writes where the other does."""
+    rng = np.random.default_rng(2)
+    T, B, H, A = 300, 30, 700, 29
+    out = harness.OutputLayer(T, B, H, A, BF16)
+    out.set_lengths(torch.from_numpy(rng.integers(100, T + 1, B).astype(np.int32)).cuda())
+    out.set_weights(random(rng, A, H))
+    out.forward(random(rng, T, B, H, dtype=torch.bfloat16))
+    grads, dy = random(rng, T, B, A, dtype=torch.bfloat16), random(rng, T, B, H, dtype=torch.bfloat16)
+    want = [t.clone() for t in (*out.weight_gradient(grads), *out.norm_backward(dy))]
+    (a, b), (n, m) = out.ws_ptr, out.ws_bytes
+    assert a + n <= b or b + m <= a
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        out.dweight.zero_(), out.dbias.zero_(), out.dnorm_weight.zero_()
+        torch.cuda.synchronize()
+        for _ in range(3):
+            out.weight_gradient(grads, stream=streams[0].cuda_stream)
+            out.norm_backward(dy, stream=streams[1].cuda_stream)
+        torch.cuda.synchronize()
+        assert all(torch.equal(g, w) for g, w in zip((out.dweight, out.dbias, out.dsum, out.dnorm_weight), want))
