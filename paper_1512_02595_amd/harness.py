@@ -239,8 +239,15 @@ class OutputLayer:
         return self.dweight, self.dbias
 
     def norm_backward(self, dy, dresidual=None, stream=None):
-        layer.rms_norm_backward(self._states(dy), self.sum.data_ptr(), self.norm_weight.data_ptr(), self.eps,
-                                None if dresidual is None else self._states(dresidual), self.frames.data_ptr(), self.rows, self.H,
-                                self.dtype, self.dsum.data_ptr(), self.dnorm_weight.data_ptr(), self.ws_ptr[1], self.ws_bytes[1],
-                                self._stream(stream))
+        """(gradient of the norm's input [T, B, H], of its weight); frames behind an utterance's end get zeros, as in CTC's gradient."""
+        given = [None if t is None else self._states(t) for t in (dy, dresidual)]
+        with self._on(stream):
+            # The library leaves such rows as they were, which may be the last minibatch's.  (An input in `dsum`'s own place is read afterwards.)
+            if self.dsum.data_ptr() in given:
+                aside = self.dsum.clone()
+                given = [aside.data_ptr() if at == self.dsum.data_ptr() else at for at in given]
+            self.dsum.zero_()
+        layer.rms_norm_backward(given[0], self.sum.data_ptr(), self.norm_weight.data_ptr(), self.eps, given[1],
+                                self.frames.data_ptr(), self.rows, self.H, self.dtype, self.dsum.data_ptr(),
+                                self.dnorm_weight.data_ptr(), self.ws_ptr[1], self.ws_bytes[1], self._stream(stream))
         return self.dsum, self.dnorm_weight

@@ -73,3 +73,61 @@ def test_gradients_on_two_streams():
             out.norm_backward(dy, stream=streams[1].cuda_stream)
         torch.cuda.synchronize()
         assert all(torch.equal(g, w) for g, w in zip((out.dweight, out.dbias, out.dsum, out.dnorm_weight), want))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("given_twice", [None, "dy", "dresidual"])
+def test_gradients_behind_an_utterances_end_are_zeros_in_every_minibatch(given_twice, dtype):
+    """Utterances get shorter: what the minibatch before left behind their new ends is gone.  So with an input in the result's place."""
+    rng = np.random.default_rng(3)
+    T, B, H, A, t = 9, 4, 130, 29, ref.torch_type(dtype)
+    out = harness.OutputLayer(T, B, H, A, dtype)
+    norm = random(rng, H)
+    out.set_weights(random(rng, A, H), norm_weight=norm)
+    for ends in ((9, 9, 7, 8), (3, 0, 7, 1), (9, 1, 0, 4)):
+        x, dy, dresidual = (random(rng, T, B, H, dtype=t) for _ in range(3))
+        out.set_lengths(lengths(*ends))
+        out.forward(x)
+        keep = torch.arange(T)[:, None] < torch.tensor(ends)[None, :]
+        want, dweight, bound, terms = ref.norm_backward(dy.cpu()[keep].double(), x.cpu()[keep].double(), norm.cpu().double(),
+                                                        float(np.float32(out.eps)), dresidual.cpu()[keep].double())
+        if given_twice:
+            out.dsum.copy_(dy if given_twice == "dy" else dresidual)
+        dsum, dnorm = out.norm_backward(out.dsum if given_twice == "dy" else dy, out.dsum if given_twice == "dresidual" else dresidual)
+        got = dsum.cpu()
+        assert not got[~keep].any()
+        assert ((got[keep].double() - want).abs() <= 1.001 * bound + ref.half_step(dtype) * (want.abs() + bound) + 1e-40).all()
+        assert ((dnorm.cpu().double() - dweight).abs() <= ref.HALF * (int(keep.sum()) + 8) * terms + 1e-40).all()
+
+
+def test_a_captured_norms_gradient_clears_what_the_replay_before_left():
+    rng = np.random.default_rng(4)
+    T, B, H, A = 12, 5, 300, 29
+    out = harness.OutputLayer(T, B, H, A)
+    out.set_weights(random(rng, A, H))
+    x, dy, ends = torch.zeros((T, B, H), device="cuda"), torch.zeros((T, B, H), device="cuda"), lengths(*[T] * B)
+
+    def step():
+        out.set_lengths(ends)
+        out.forward(x)
+        out.norm_backward(dy)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    for _ in range(4):
+        x.copy_(random(rng, T, B, H)), dy.copy_(random(rng, T, B, H))
+        ends.copy_(torch.from_numpy(rng.integers(0, T + 1, B).astype(np.int32)))
+        step()
+        torch.cuda.synchronize()
+        want = out.dsum.clone(), out.dnorm_weight.clone()
+        out.dsum.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out.dsum, want[0]) and torch.equal(out.dnorm_weight, want[1]) and want[0].any()
+        assert not out.dsum[torch.arange(T, device="cuda")[:, None] >= ends[None, :]].any()
