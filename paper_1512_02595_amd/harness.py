@@ -178,7 +178,9 @@ class OutputLayer:
             return torch.zeros(shape, dtype=dtype, device=self.device)
 
         pitch = layer.row_pitch(H)
-        self.frames = zeros(1 + self.rows, dtype=torch.int32)
+        # (the number of rows, then their indices: all of them, until set_lengths says otherwise)
+        self.frames = torch.cat((torch.tensor([self.rows], dtype=torch.int32, device=self.device),
+                                 torch.arange(self.rows, dtype=torch.int32, device=self.device)))
         self.norm_weight, self.bias = torch.ones(H, device=self.device), zeros(A)
         self.weight_q, self.weight_scales = zeros(A, pitch, dtype=torch.int8), zeros(A)
         self.sum, self.dsum = zeros(T, B, H, dtype=tdtype), zeros(T, B, H, dtype=tdtype)
@@ -217,7 +219,7 @@ class OutputLayer:
                 self.norm_weight.copy_(norm_weight)
 
     def set_lengths(self, input_lengths, stream=None):
-        """int32 [B] on the GPU: the frames of this minibatch, for all calls until the next one's."""
+        """int32 [B] on the GPU: the frames of this minibatch, for all calls until the next one's (before the first: all)."""
         assert tuple(input_lengths.shape) == (self.B,) and input_lengths.dtype == torch.int32 and input_lengths.is_contiguous()
         layer.pack_frames(input_lengths.data_ptr(), self.T, self.B, self.frames.data_ptr(), self._stream(stream))
 

@@ -131,3 +131,17 @@ def test_a_captured_norms_gradient_clears_what_the_replay_before_left():
         torch.cuda.synchronize()
         assert torch.equal(out.dsum, want[0]) and torch.equal(out.dnorm_weight, want[1]) and want[0].any()
         assert not out.dsum[torch.arange(T, device="cuda")[:, None] >= ends[None, :]].any()
+
+
+def test_all_frames_count_until_lengths_are_set():
+    rng = np.random.default_rng(5)
+    T, B, H, A = 7, 3, 140, 29
+    weight, x, grads, dy = random(rng, A, H), random(rng, T, B, H), random(rng, T, B, A), random(rng, T, B, H)
+    results = []
+    for said in (True, False):
+        out = harness.OutputLayer(T, B, H, A)
+        out.set_weights(weight)
+        if said:
+            out.set_lengths(lengths(*[T] * B))
+        results.append([t.clone() for t in (out.forward(x), *out.weight_gradient(grads), *out.norm_backward(dy))])
+    assert all(torch.equal(a, b) and a.any() for a, b in zip(*results))
