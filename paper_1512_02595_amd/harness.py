@@ -186,7 +186,7 @@ class OutputLayer:
         self.sum, self.dsum = zeros(T, B, H, dtype=tdtype), zeros(T, B, H, dtype=tdtype)
         self.q, self.scales = zeros(self.rows, pitch, dtype=torch.int8), zeros(self.rows)
         self.logits = zeros(T, B, A, dtype=tdtype) if logits is None else logits
-        assert tuple(self.logits.shape) == (T, B, A) and self.logits.dtype == tdtype and self.logits.is_contiguous()
+        assert tuple(self.logits.shape) == (T, B, A) and self.logits.dtype == tdtype and self._here(self.logits)
         self.dweight, self.dbias, self.dnorm_weight = zeros(A, H), zeros(A), zeros(H)
         self.ws_bytes = layer.weight_gradient_workspace_size(self.rows, H, A), layer.rms_norm_workspace_size(self.rows, H)
         # (the two gradients need nothing of each other and may be on two streams: a workspace each)
@@ -203,13 +203,17 @@ class OutputLayer:
             return contextlib.nullcontext()
         return torch.cuda.stream(torch.cuda.ExternalStream(s, device=self.device))
 
+    def _here(self, t):
+        """Whether the library may be given the tensor's address."""
+        return t.device == self.frames.device and t.is_contiguous()
+
     def _states(self, t):
-        assert t.numel() == self.rows * self.H and t.dtype == self.sum.dtype and t.is_contiguous()
+        assert t.numel() == self.rows * self.H and t.dtype == self.sum.dtype and self._here(t)
         return t.data_ptr()
 
     def set_weights(self, weight, bias=None, norm_weight=None, stream=None):
         """fp32 weights [A, H] to 8 bits, and copies of the others: once per step of the optimiser."""
-        assert tuple(weight.shape) == (self.A, self.H) and weight.dtype == torch.float32 and weight.is_contiguous()
+        assert tuple(weight.shape) == (self.A, self.H) and weight.dtype == torch.float32 and self._here(weight)
         layer.quantize_rows(weight.data_ptr(), None, self.A, self.H, ctc.DTYPE_F32, self.weight_q.data_ptr(),
                             self.weight_scales.data_ptr(), self._stream(stream))
         with self._on(stream):
@@ -220,7 +224,7 @@ class OutputLayer:
 
     def set_lengths(self, input_lengths, stream=None):
         """int32 [B] on the GPU: the frames of this minibatch, for all calls until the next one's (before the first: all)."""
-        assert tuple(input_lengths.shape) == (self.B,) and input_lengths.dtype == torch.int32 and input_lengths.is_contiguous()
+        assert tuple(input_lengths.shape) == (self.B,) and input_lengths.dtype == torch.int32 and self._here(input_lengths)
         layer.pack_frames(input_lengths.data_ptr(), self.T, self.B, self.frames.data_ptr(), self._stream(stream))
 
     def forward(self, x, residual=None, stream=None):
@@ -234,7 +238,7 @@ class OutputLayer:
         return self.logits
 
     def weight_gradient(self, grads, stream=None):
-        assert tuple(grads.shape) == (self.T, self.B, self.A) and grads.dtype == self.logits.dtype and grads.is_contiguous()
+        assert tuple(grads.shape) == (self.T, self.B, self.A) and grads.dtype == self.logits.dtype and self._here(grads)
         layer.weight_gradient_i8(grads.data_ptr(), self.q.data_ptr(), self.scales.data_ptr(), self.frames.data_ptr(), self.rows,
                                  self.H, self.A, self.dtype, self.dweight.data_ptr(), self.dbias.data_ptr(), self.ws_ptr[0],
                                  self.ws_bytes[0], self._stream(stream))
