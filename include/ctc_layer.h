@@ -68,7 +68,8 @@ int ctc_row_pitch(int H);
  *
  *   input_lengths (device) [B]; below 0 counts as 0, above T as T
  *   frames        (device) [1 + T*B]: receives the number n of frames and the n rows t * B + b with
- *                 t < input_lengths[b], utterance by utterance; what lies behind them stays.
+ *                 t < input_lengths[b], ascending: frame by frame, a frame's in the order of the
+ *                 utterances; what lies behind them stays.
  *   B is at most 65535 (as for ctc_loss_and_grad), T * B at most 2^30
  */
 ctc_status_t ctc_pack_frames(const int32_t *input_lengths, int T, int B, int32_t *frames, hipStream_t stream);

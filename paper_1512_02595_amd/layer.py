@@ -95,7 +95,7 @@ def pack_frames_status(input_lengths_ptr, T, B, frames_ptr, stream=0) -> int:
 
 
 def pack_frames(input_lengths_ptr, T, B, frames_ptr, stream=0) -> None:
-    """The list of a minibatch's frames, int32 [1 + T * B], from its input lengths on the GPU."""
+    """The list of a minibatch's frames, int32 [1 + T * B], from its input lengths on the GPU: their number, then their rows in ascending order."""
     st = (_native or _module()).pack_frames(input_lengths_ptr, T, B, frames_ptr, stream)
     if st:
         _check(st, "ctc_pack_frames")
