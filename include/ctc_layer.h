@@ -165,6 +165,9 @@ ctc_status_t ctc_linear_i8(const int8_t *q, const float *scales, const int8_t *w
  *   dweight    (device) [A, H] float.  Zeros if no row is listed.
  *   dbias      (device) [A] float, or NULL
  *   workspace  (device) 256-byte aligned, ctc_weight_gradient_workspace_size bytes
+ *
+ * A workspace made for the largest minibatch serves all: the size never shrinks as rows grow, and a call takes
+ * one of the size for its own rows or for more (so too for ctc_rms_norm_workspace_size).
  */
 ctc_status_t ctc_weight_gradient_workspace_size(int rows, int H, int A, size_t *bytes_out);
 ctc_status_t ctc_weight_gradient_i8(const void *grads, const int8_t *q, const float *scales,

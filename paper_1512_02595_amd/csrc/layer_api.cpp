@@ -60,7 +60,6 @@ size_t list_bytes(int rows) { return (static_cast<size_t>(rows) + 1) * 4; }
 size_t round_up(size_t v) { return (v + 255) / 256 * 256; }
 
 size_t norm_workspace(int rows, int H) { return round_up(static_cast<size_t>(norm_partials(rows, H)) * H * 4); }
-size_t gradient_workspace(int rows, int H, int A) { return round_up(gradient_plan(rows, H, A).bytes); }
 
 }  // namespace
 }  // namespace layer
@@ -181,7 +180,7 @@ ctc_status_t ctc_weight_gradient_workspace_size(int rows, int H, int A, size_t* 
 {
     if (!bytes_out) return CTC_STATUS_INVALID_VALUE;
     const ctc_status_t st = sizes_in_range(rows, H, A, CTC_DTYPE_F32);
-    if (st == CTC_STATUS_SUCCESS) *bytes_out = gradient_workspace(rows, H, A);
+    if (st == CTC_STATUS_SUCCESS) *bytes_out = round_up(gradient_bytes(rows, H, A));
     return st;
 }
 
@@ -191,7 +190,7 @@ ctc_status_t ctc_weight_gradient_i8(const void* grads, const int8_t* q, const fl
 {
     const ctc_status_t st = sizes_in_range(rows, H, A, dtype);
     if (st != CTC_STATUS_SUCCESS) return st;
-    const size_t e = element(dtype), needed = gradient_workspace(rows, H, A);
+    const size_t e = element(dtype), needed = round_up(gradient_plan(rows, H, A).bytes);
     if (!buffers_in_order({{grads, matrix(rows, A, e), false, true, e},
                            {q, matrix(rows, pitch_of(H), 1), false, true, 16},
                            {scales, matrix(rows, 1, 4), false},

@@ -36,44 +36,115 @@ struct GradientPlan {
     int bias_slabs;
     size_t bias_at, largest_at, wide_at, bytes; // places in the workspace, in floats; all of it, in bytes
 };
-inline GradientPlan gradient_plan(int rows, int H, int A)
-{
-    const long steps = (rows + 31L) / 32;
-    const auto plan = [&](int symbols) {
+
+// One kind of tile for A symbols of H columns, and the time (us) that so many slabs of them take for so many steps of 32 rows: as many rounds of
+// workgroups as the 256 compute units take (two workgroups each where tiles are narrow), each of its share of the steps and a few to begin and
+// end with; every slab's sums written and read once more.
+struct GradientTiles {
+    int H, A, symbols, columns;
+    bool wide;
+    long tiles, at_once;
+    double step, slab_cost;
+    GradientTiles(int H_, int A_, int symbols_) : H(H_), A(A_), symbols(symbols_), columns(symbols_ == 128 ? 512 : 256), wide(symbols_ == 128)
+    {
+        tiles = ((A + symbols - 1L) / symbols) * ((H + columns - 1L) / columns);
+        at_once = wide ? 256 : 512;
+        step = wide ? 1.7 : 1.5;
+        slab_cost = 8.0 * A * H / 5.0e6;
+    }
+    double rounds(long s) const { return static_cast<double>((tiles * s + at_once - 1) / at_once); }
+    double sums(long s) const { return s > 1 ? s * slab_cost + 6.0 * step : 0.0; }
+    double time(long steps, long s) const { return rounds(s) * (static_cast<double>((steps + s - 1) / s) + 6.0) * step + sums(s); }
+    static long most_slabs(long steps) { return (steps + 3) / 4 < 256 ? (steps + 3) / 4 : 256; }
+
+    GradientPlan plan(long steps, long s) const
+    {
         GradientPlan p{};
-        const bool wide = symbols == 128;
         p.symbols = symbols;
-        p.columns = wide ? 512 : 256;
-        const long tiles = ((A + symbols - 1L) / symbols) * ((H + p.columns - 1L) / p.columns);
-        // Time (us): as many rounds of workgroups as the 256 compute units take (two workgroups each where tiles are narrow), each of its share of the
-        // steps of 32 rows and a few to begin and end with; every slab's sums written and read once more.
-        const long at_once = wide ? 256 : 512;
-        const double step = wide ? 1.7 : 1.5, slab_cost = 8.0 * A * H / 5.0e6;
-        for (long s = 1; s <= 256 && s <= (steps + 3) / 4; ++s) {
-            const long rounds = (tiles * s + at_once - 1) / at_once;
-            const double time = static_cast<double>(rounds) * (static_cast<double>((steps + s - 1) / s) + 6.0) * step + (s > 1 ? s * slab_cost + 6.0 * step : 0.0);
-            if (s == 1 || time < p.time) {
-                p.time = time;
-                p.slabs = static_cast<int>(s);
+        p.columns = columns;
+        p.slabs = static_cast<int>(s);
+        p.time = time(steps, s);
+        p.bias_slabs = wide ? kColumnSlabs : p.slabs;
+        p.bias_at = s > 1 ? static_cast<size_t>(s) * A * H : 0;
+        p.largest_at = p.bias_at + static_cast<size_t>(p.bias_slabs) * A;
+        p.wide_at = (p.largest_at + (wide ? static_cast<size_t>(kColumnSlabs) * A : 0) + 63) / 64 * 64;
+        p.bytes = (p.wide_at + (wide ? static_cast<size_t>(steps) * pitch_of(H) * 16 : 0)) * 4;
+        return p;
+    }
+    GradientPlan quickest(long steps) const
+    {
+        long best = 1;
+        double least = time(steps, 1);
+        for (long s = 2; s <= most_slabs(steps); ++s) {
+            const double t = time(steps, s);
+            if (t < least) {
+                least = t;
+                best = s;
             }
         }
-        return p;
-    };
-    GradientPlan p = plan(A <= 32 ? 32 : 64);
-    if (A > 64) {
-        // Wide tiles need a launch before theirs (the columns' largest, the rows' numbers as fp16) and are a fourth as many, each of which takes a
-        // third fewer products.  (Narrow and wide, us, fp32: 514 rows, 2048 wide, 172 symbols 15 and 27, 6000 symbols 59 and 52; 4000 rows,
-        // 1000 symbols 70 and 70; 12000 rows, 172 symbols 46 and 69, 1000 symbols 178 and 139, 6000 symbols 1035 and 662.)
-        const GradientPlan wide = plan(128);
-        if (wide.time + 20.0 <= 1.1 * p.time) p = wide;
+        return plan(steps, best);
     }
-    const bool wide = p.symbols == 128;
-    p.bias_slabs = wide ? kColumnSlabs : p.slabs;
-    p.bias_at = p.slabs > 1 ? static_cast<size_t>(p.slabs) * A * H : 0;
-    p.largest_at = p.bias_at + static_cast<size_t>(p.bias_slabs) * A;
-    p.wide_at = (p.largest_at + (wide ? static_cast<size_t>(kColumnSlabs) * A : 0) + 63) / 64 * 64;
-    p.bytes = (p.wide_at + (wide ? static_cast<size_t>(steps) * pitch_of(H) * 16 : 0)) * 4;
-    return p;
+};
+
+// Wide tiles need a launch before theirs (the columns' largest, the rows' numbers as fp16) and are a fourth as many, each of which takes a
+// third fewer products.  (Narrow and wide, us, fp32: 514 rows, 2048 wide, 172 symbols 15 and 27, 6000 symbols 59 and 52; 4000 rows,
+// 1000 symbols 70 and 70; 12000 rows, 172 symbols 46 and 69, 1000 symbols 178 and 139, 6000 symbols 1035 and 662.)
+constexpr double kWideLaunch = 20.0, kWideFavour = 1.1;
+
+inline int narrow_symbols(int A) { return A <= 32 ? 32 : 64; }
+
+inline GradientPlan gradient_plan_of_steps(long steps, int H, int A)
+{
+    const GradientPlan narrow = GradientTiles(H, A, narrow_symbols(A)).quickest(steps);
+    if (A <= 64) return narrow;
+    const GradientPlan wide = GradientTiles(H, A, 128).quickest(steps);
+    return wide.time + kWideLaunch <= kWideFavour * narrow.time ? wide : narrow;
+}
+inline GradientPlan gradient_plan(int rows, int H, int A) { return gradient_plan_of_steps((rows + 31L) / 32, H, A); }
+
+// The most slabs of `mine` that are chosen for any number of steps in [from, to], or a few more; 0: none ever are.  A number of slabs is chosen only
+// where its time, taken low (shares of steps not rounded up), is at most that of each smaller number, taken high, and, where there are `others` (the
+// tiles of the other width), `weight` times it and `extra` at most `others_weight` times theirs: each a straight line over another, which leaves an interval of steps.
+inline long most_slabs_chosen(const GradientTiles& mine, long from, long to, const GradientTiles* others, double weight, double extra, double others_weight)
+{
+    for (long s = GradientTiles::most_slabs(to); s >= 1; --s) {
+        double low = from > 4 * s - 3 ? from : 4 * s - 3, high = to;
+        const double slope = mine.rounds(s) * mine.step / s, base = mine.rounds(s) * 6.0 * mine.step + mine.sums(s);
+        const auto at_most = [&](const GradientTiles& t, long u, double w, double more, double v) {       // w (slope x + base) + more <= v (time of u)
+            const double a = w * slope - v * t.rounds(u) * t.step / u, top = v * (t.rounds(u) * t.step * ((u - 1.0) / u + 6.0) + t.sums(u));
+            const double b = top - w * base - more + 1e-9 * (top + w * base + more);                      // (a little more than rounding takes)
+            if (a > 0)
+                high = b / a < high ? b / a : high;
+            else if (a < 0)
+                low = b / a > low ? b / a : low;
+            else if (b < 0)
+                high = 0;
+        };
+        for (long u = s - 1; u >= 1 && low <= high + 1; --u) at_most(mine, u, 1.0, 0.0, 1.0);
+        if (others)
+            for (long u = 1; u <= s && low <= high + 1; ++u) at_most(*others, u, weight, extra, others_weight);
+        if (low <= high + 1e-6 * (high + 1)) return s;
+    }
+    return 0;
+}
+
+// Bytes of workspace that are enough for `rows` rows and for any fewer, so that one made for the largest minibatch serves all: slabs, and the kind of
+// tile, do not always grow with the rows.  Up to 64 steps each number's plan is looked at, beyond them the most slabs of either kind.
+inline size_t gradient_bytes(int rows, int H, int A)
+{
+    constexpr long kLookedAt = 64;
+    const long steps = (rows + 31L) / 32;
+    size_t most = 0;
+    const auto count = [&](size_t bytes) { most = bytes > most ? bytes : most; };
+    for (long x = 1; x <= steps && x <= kLookedAt; ++x) count(gradient_plan_of_steps(x, H, A).bytes);
+    if (steps <= kLookedAt) return most;
+    const GradientTiles narrow(H, A, narrow_symbols(A)), wide(H, A, 128);
+    const bool both = A > 64;
+    const long n = most_slabs_chosen(narrow, kLookedAt + 1, steps, both ? &wide : nullptr, kWideFavour, -kWideLaunch, 1.0);
+    const long w = both ? most_slabs_chosen(wide, kLookedAt + 1, steps, &narrow, 1.0, kWideLaunch, kWideFavour) : 0;
+    if (n) count(narrow.plan(steps, n).bytes);
+    if (w) count(wide.plan(steps, w).bytes);
+    return most;
 }
 
 // Every launch returns a hipError_t.

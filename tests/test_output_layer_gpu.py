@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import layer_reference as ref
-from paper_1512_02595_amd import ctc, harness
+from paper_1512_02595_amd import ctc, harness, layer
 
 pytestmark = pytest.mark.gpu
 F32, BF16 = ctc.DTYPE_F32, ctc.DTYPE_BF16
@@ -144,4 +144,23 @@ def test_all_frames_count_until_lengths_are_set():
         if said:
             out.set_lengths(lengths(*[T] * B))
         results.append([t.clone() for t in (out.forward(x), *out.weight_gradient(grads), *out.norm_backward(dy))])
+    assert all(torch.equal(a, b) and a.any() for a, b in zip(*results))
+
+
+def test_a_workspace_of_the_largest_minibatch_serves_a_smaller_one():
+    """32768 rows take wide tiles and six times the workspace of 32800 rows, which take narrow ones."""
+    rng = np.random.default_rng(6)
+    most, rows, H, A = 32800, 32768, 2048, 172
+    size = layer.weight_gradient_workspace_size(most, H, A)
+    grads, scales = random(rng, rows, A), random(rng, rows)
+    q = torch.from_numpy(rng.integers(-127, 128, (rows, H)).astype(np.int8)).cuda()
+    results = []
+    for n in (size, layer.weight_gradient_workspace_size(rows, H, A)):
+        work, dweight, dbias = ref.Guarded((n,), torch.uint8), torch.zeros((A, H), device="cuda"), torch.zeros(A, device="cuda")
+        assert work.t.data_ptr() % 256 == 0
+        layer.weight_gradient_i8(grads.data_ptr(), q.data_ptr(), scales.data_ptr(), None, rows, H, A, F32, dweight.data_ptr(), dbias.data_ptr(),
+                                 work.t.data_ptr(), n, ref.stream())
+        torch.cuda.synchronize()
+        assert work.intact()
+        results.append((dweight, dbias))
     assert all(torch.equal(a, b) and a.any() for a, b in zip(*results))
