@@ -190,7 +190,8 @@ ctc_status_t ctc_weight_gradient_i8(const void* grads, const int8_t* q, const fl
 {
     const ctc_status_t st = sizes_in_range(rows, H, A, dtype);
     if (st != CTC_STATUS_SUCCESS) return st;
-    const size_t e = element(dtype), needed = round_up(gradient_plan(rows, H, A).bytes);
+    const GradientPlan plan = gradient_plan(rows, H, A);
+    const size_t e = element(dtype), needed = round_up(plan.bytes);
     if (!buffers_in_order({{grads, matrix(rows, A, e), false, true, e},
                            {q, matrix(rows, pitch_of(H), 1), false, true, 16},
                            {scales, matrix(rows, 1, 4), false},
@@ -200,7 +201,7 @@ ctc_status_t ctc_weight_gradient_i8(const void* grads, const int8_t* q, const fl
                            {workspace, needed, true, true, 256}}))
         return CTC_STATUS_INVALID_VALUE;
     if (workspace_bytes < needed) return CTC_STATUS_WORKSPACE_TOO_SMALL;
-    return launched(launch_weight_gradient(grads, q, scales, frames, rows, H, A, dtype == CTC_DTYPE_BF16, dweight, dbias,
+    return launched(launch_weight_gradient(grads, q, scales, frames, rows, H, A, dtype == CTC_DTYPE_BF16, plan, dweight, dbias,
                                            static_cast<float*>(workspace), stream));
 }
 

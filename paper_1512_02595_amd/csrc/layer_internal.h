@@ -160,7 +160,7 @@ int launch_norm_backward(const void* dy, const void* sum, const float* weight, f
 int launch_linear(const int8_t* q, const float* scales, const int8_t* weight_q, const float* weight_scales, const float* bias,
                   const int32_t* frames, int rows, int H, int A, bool bf16, void* logits, void* stream);
 int launch_weight_gradient(const void* grads, const int8_t* q, const float* scales, const int32_t* frames, int rows, int H,
-                           int A, bool bf16, float* dweight, float* dbias, float* partials, void* stream);
+                           int A, bool bf16, const GradientPlan& plan, float* dweight, float* dbias, float* workspace, void* stream);
 
 }  // namespace layer
 

@@ -1443,24 +1443,23 @@ int launch_linear(const int8_t* q, const float* scales, const int8_t* weight_q, 
 }
 
 int launch_weight_gradient(const void* grads, const int8_t* q, const float* scales, const int32_t* frames, int rows, int H,
-                           int A, bool bf16, float* dweight, float* dbias, float* partials, void* stream)
+                           int A, bool bf16, const GradientPlan& plan, float* dweight, float* dbias, float* workspace, void* stream)
 {
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const GradientPlan plan = gradient_plan(rows, H, A);
     const int64_t weights = static_cast<int64_t>(A) * H;
-    float* const bias = partials + plan.bias_at;
+    float* const bias = workspace + plan.bias_at;
     const GradientArgs p = {grads, q, scales, frames, rows, H, A, pitch_of(H), plan.slabs,
-                            plan.slabs > 1 ? partials : dweight, dbias ? bias : nullptr,
-                            reinterpret_cast<const uint32_t*>(partials + plan.largest_at)};
+                            plan.slabs > 1 ? workspace : dweight, dbias ? bias : nullptr,
+                            reinterpret_cast<const uint32_t*>(workspace + plan.largest_at)};
     if (bf16)
-        launch_gradient<bf16_t>(p, plan, partials, s);
+        launch_gradient<bf16_t>(p, plan, workspace, s);
     else
-        launch_gradient<float>(p, plan, partials, s);
+        launch_gradient<float>(p, plan, workspace, s);
     const int err = last_error();
     if (err) return err;
     const unsigned weight_blocks = plan.slabs > 1 ? blocks(weights, 1024) : 0, bias_blocks = dbias ? blocks(A, 256) : 0;
     if (weight_blocks + bias_blocks == 0) return 0;
-    hipLaunchKernelGGL(ctc_sum_slabs_kernel, dim3(weight_blocks + bias_blocks), dim3(256), 0, s, partials, plan.slabs, weights, dweight, weight_blocks,
+    hipLaunchKernelGGL(ctc_sum_slabs_kernel, dim3(weight_blocks + bias_blocks), dim3(256), 0, s, workspace, plan.slabs, weights, dweight, weight_blocks,
                        bias, plan.bias_slabs, A, dbias);
     return last_error();
 }
