@@ -26,6 +26,49 @@ inline int norm_partials(int rows, int H)
     return groups < 1024 ? groups : 1024;
 }
 
+// Rows to 8 bits: so many wavefronts to a row, so many elements to a lane.  16 elements a lane, and so wavefronts by the width: more elements leave
+// too few wavefronts to a compute unit for what memory takes (the norm's 27200 rows of 2048 fp32 by one wavefront with 32 a lane 137 us, by two with
+// 16 125; 6000 of 3500 by two with 32 50 us, by four with 16 46).  Where rows are few, 8 a lane, for the time that one row takes (one row of 2048 bf16
+// 4.1 us with 16, 3.4 with 8; 1500 rows 6.9 and 6.0; 27200 rows to 8 bits 31.3 and 35.3).
+struct RowShape {
+    int waves, elements;
+};
+inline RowShape row_shape(int rows, int H)
+{
+    const int pitch = pitch_of(H);
+    const bool few = rows <= 2048;
+    if (pitch <= 512) return {1, 8};
+    if (few && pitch <= 1024) return {2, 8};
+    if (few && pitch <= 2048) return {4, 8};
+    if (few && pitch <= 4096) return {8, 8};
+    if (pitch <= 1024) return {1, 16};
+    if (pitch <= 2048) return {2, 16};
+    if (pitch <= 4096) return {4, 16};
+    if (pitch <= 8192) return {8, 16};
+    return {8, 32};                                     // (16 wavefronts with 16 a lane: the norm's 1500 rows of 12000 bf16 38 us, eight with 32 31)
+}
+
+// Activations: rows and symbols to a workgroup; 16 by 16 is the kernel without tiles in LDS.
+struct ProductTile {
+    int rows, symbols;
+};
+inline ProductTile product_tile(int all_rows, int H, int A, bool list)
+{
+    // Of a list's rows, five in eight are taken to count (how many do, only the GPU knows).
+    const int64_t rows = list ? (static_cast<int64_t>(all_rows) * 5 + 7) / 8 : all_rows;
+    const auto tiles = [&](int m, int n) { return (rows + m - 1) / m * ((A + n - 1) / n); };
+    // Tiles of 256 by 256 read the least of memory and LDS, those of 128 by 128, two of which share a compute unit, begin and end sooner: the times
+    // of a round of each (us), from K = 512 and 2048 at 3000 and 19200 rows by 6000 symbols (28.7 and 389 against 40 and 326; 5560 x 4733, K = 1152:
+    // 73 against 60).
+    const double steps = pitch_of(H) / 64;
+    const double large = static_cast<double>((tiles(256, 256) + 255) / 256) * (13.5 + 0.85 * steps);
+    const double small = static_cast<double>((tiles(128, 128) + 511) / 512) * (7.0 + 0.65 * steps);
+    if (tiles(16, 16) <= 400) return {16, 16};                          // 1 x 6000 4.5 us against 6.0 in tiles of 64 by 64, 16 x 6000 5.9 and 6.1, 32 x 6000 7.8 and 6.3
+    if (A <= 64 && tiles(64, 64) > 400) return {128, 64};               // 27200 x 60 14.7 us against 15.6; 5000 x 60 8.4 against 6.8
+    if (tiles(64, 64) <= 600) return {64, 64};                          // 300 x 6000 10.9 us against 13.7 in 128 by 128; 1500 x 2000 (768 tiles) 11.1 and 10.8
+    return small < large ? ProductTile{128, 128} : ProductTile{256, 256};
+}
+
 // The weights' gradient: symbols and columns in tiles, the listed rows dealt out to so many slabs, each summed by workgroups
 // of its own.
 constexpr int kColumnSlabs = 64;                // workgroups that look at one symbol's gradients first

@@ -1268,36 +1268,19 @@ dim3 spread(unsigned groups)
     return groups <= kAcross ? dim3(groups) : dim3(kAcross, (groups + kAcross - 1) / kAcross);
 }
 
-template <typename T, bool NORM, int WAVES, int E> void launch_rows(const NormArgs& p, hipStream_t s)
+template <typename T, bool NORM, int WAVES, int E> bool launch_rows(const NormArgs& p, RowShape shape, hipStream_t s)
 {
+    if (shape.waves != WAVES || shape.elements != E) return false;
     const unsigned groups = WAVES == 1 ? blocks(p.rows, 4) : static_cast<unsigned>(p.rows);
     hipLaunchKernelGGL((ctc_rows_to_8_bits_kernel<T, WAVES, E, NORM>), spread(groups), dim3(WAVES == 1 ? 256 : WAVES * kWave), 0, s, p);
+    return true;
 }
 template <typename T, bool NORM> void launch_to_8_bits(const NormArgs& p, hipStream_t s)
 {
-    // 16 elements a lane, and so wavefronts by the width: more elements leave too few wavefronts to a compute unit for what memory takes (the
-    // norm's 27200 rows of 2048 fp32 by one wavefront with 32 a lane 137 us, by two with 16 125; 6000 of 3500 by
-    // two with 32 50 us, by four with 16 46).  Where rows are few, 8 a lane, for the time that one row takes (one row of 2048 bf16 4.1 us with 16, 3.4 with 8; 1500 rows 6.9
-    // and 6.0; 27200 rows to 8 bits 31.3 and 35.3).
-    const bool few = p.rows <= 2048;
-    if (p.pitch <= 512)
-        launch_rows<T, NORM, 1, 8>(p, s);
-    else if (few && p.pitch <= 1024)
-        launch_rows<T, NORM, 2, 8>(p, s);
-    else if (few && p.pitch <= 2048)
-        launch_rows<T, NORM, 4, 8>(p, s);
-    else if (few && p.pitch <= 4096)
-        launch_rows<T, NORM, 8, 8>(p, s);
-    else if (p.pitch <= 1024)
-        launch_rows<T, NORM, 1, 16>(p, s);
-    else if (p.pitch <= 2048)
-        launch_rows<T, NORM, 2, 16>(p, s);
-    else if (p.pitch <= 4096)
-        launch_rows<T, NORM, 4, 16>(p, s);
-    else if (p.pitch <= 8192)
-        launch_rows<T, NORM, 8, 16>(p, s);
-    else                                                // (16 wavefronts with 16 a lane: the norm's 1500 rows of 12000 bf16 38 us, eight with 32 31)
-        launch_rows<T, NORM, 8, 32>(p, s);
+    const RowShape shape = row_shape(p.rows, p.H);
+    (void)(launch_rows<T, NORM, 1, 8>(p, shape, s) || launch_rows<T, NORM, 2, 8>(p, shape, s) || launch_rows<T, NORM, 4, 8>(p, shape, s) ||
+           launch_rows<T, NORM, 8, 8>(p, shape, s) || launch_rows<T, NORM, 1, 16>(p, shape, s) || launch_rows<T, NORM, 2, 16>(p, shape, s) ||
+           launch_rows<T, NORM, 4, 16>(p, shape, s) || launch_rows<T, NORM, 8, 16>(p, shape, s) || launch_rows<T, NORM, 8, 32>(p, shape, s));
 }
 
 template <typename T> void launch_backward(const NormBackArgs& p, unsigned groups, hipStream_t s)
@@ -1330,24 +1313,15 @@ template <typename T> void launch_direct(const LinearArgs& p, hipStream_t s)
 {
     hipLaunchKernelGGL(ctc_linear_direct_kernel<T>, dim3(blocks(p.rows, 16) * blocks(p.A, 16)), dim3(256), 0, s, p);
 }
-template <typename T> void launch_product(const LinearArgs& p, hipStream_t s)
+template <typename T> void launch_product(const LinearArgs& p, ProductTile tile, hipStream_t s)
 {
-    // Of a list's rows, five in eight are taken to count (how many do, only the GPU knows).
-    const int64_t rows = p.frames ? (static_cast<int64_t>(p.rows) * 5 + 7) / 8 : p.rows;
-    const auto tiles = [&](int m, int n) { return (rows + m - 1) / m * ((p.A + n - 1) / n); };
-    // Tiles of 256 by 256 read the least of memory and LDS, those of 128 by 128, two of which share a compute unit, begin and end sooner: the times
-    // of a round of each (us), from K = 512 and 2048 at 3000 and 19200 rows by 6000 symbols (28.7 and 389 against 40 and 326; 5560 x 4733, K = 1152:
-    // 73 against 60).
-    const double steps = p.pitch / 64;
-    const double large = static_cast<double>((tiles(256, 256) + 255) / 256) * (13.5 + 0.85 * steps);
-    const double small = static_cast<double>((tiles(128, 128) + 511) / 512) * (7.0 + 0.65 * steps);
-    if (tiles(16, 16) <= 400)                           // 1 x 6000 4.5 us against 6.0 in tiles of 64 by 64, 16 x 6000 5.9 and 6.1, 32 x 6000 7.8 and 6.3
+    if (tile.rows == 16)
         launch_direct<T>(p, s);
-    else if (p.A <= 64 && tiles(64, 64) > 400)          // 27200 x 60 14.7 us against 15.6; 5000 x 60 8.4 against 6.8
+    else if (tile.symbols == 64 && tile.rows == 128)
         launch_tiles<T, 2, 1>(p, s);
-    else if (tiles(64, 64) <= 600)                      // 300 x 6000 10.9 us against 13.7 in 128 by 128; 1500 x 2000 (768 tiles) 11.1 and 10.8
+    else if (tile.symbols == 64)
         launch_tiles<T, 1, 1>(p, s);
-    else if (small < large)
+    else if (tile.symbols == 128)
         launch_tiles<T, 2, 2>(p, s);
     else
         launch_tiles<T, 4, 4>(p, s);
@@ -1435,10 +1409,11 @@ int launch_linear(const int8_t* q, const float* scales, const int8_t* weight_q, 
                   const int32_t* frames, int rows, int H, int A, bool bf16, void* logits, void* stream)
 {
     const LinearArgs p = {q, scales, weight_q, weight_scales, bias, frames, rows, A, pitch_of(H), logits};
+    const ProductTile tile = product_tile(rows, H, A, frames != nullptr);
     if (bf16)
-        launch_product<bf16_t>(p, static_cast<hipStream_t>(stream));
+        launch_product<bf16_t>(p, tile, static_cast<hipStream_t>(stream));
     else
-        launch_product<float>(p, static_cast<hipStream_t>(stream));
+        launch_product<float>(p, tile, static_cast<hipStream_t>(stream));
     return last_error();
 }
 
