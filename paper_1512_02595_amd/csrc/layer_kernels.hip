@@ -2,6 +2,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <tuple>
 #include <type_traits>
 
 #include "layer_internal.h"
@@ -1257,8 +1258,6 @@ __global__ __launch_bounds__(256) void ctc_sum_slabs_kernel(const float* __restr
     }
 }
 
-int last_error() { return static_cast<int>(hipGetLastError()); }
-
 unsigned blocks(int64_t items, int per_block) { return static_cast<unsigned>((items + per_block - 1) / per_block); }
 
 // A grid of `groups` workgroups and some: a dimension has fewer than 2^32 threads, rows may be 2^30.
@@ -1268,123 +1267,109 @@ dim3 spread(unsigned groups)
     return groups <= kAcross ? dim3(groups) : dim3(kAcross, (groups + kAcross - 1) / kAcross);
 }
 
-template <typename T, bool NORM, int WAVES, int E> bool launch_rows(const NormArgs& p, RowShape shape, hipStream_t s)
+// Enqueues a kernel and returns this launch's own error: hipGetLastError's could be one that the caller has met and dealt with long ago.
+template <typename... P, typename... Args> int launch(void (*kernel)(P...), dim3 grid, int threads, hipStream_t s, const Args&... args)
 {
-    if (shape.waves != WAVES || shape.elements != E) return false;
-    const unsigned groups = WAVES == 1 ? blocks(p.rows, 4) : static_cast<unsigned>(p.rows);
-    hipLaunchKernelGGL((ctc_rows_to_8_bits_kernel<T, WAVES, E, NORM>), spread(groups), dim3(WAVES == 1 ? 256 : WAVES * kWave), 0, s, p);
-    return true;
-}
-template <typename T, bool NORM> void launch_to_8_bits(const NormArgs& p, hipStream_t s)
-{
-    const RowShape shape = row_shape(p.rows, p.H);
-    (void)(launch_rows<T, NORM, 1, 8>(p, shape, s) || launch_rows<T, NORM, 2, 8>(p, shape, s) || launch_rows<T, NORM, 4, 8>(p, shape, s) ||
-           launch_rows<T, NORM, 8, 8>(p, shape, s) || launch_rows<T, NORM, 1, 16>(p, shape, s) || launch_rows<T, NORM, 2, 16>(p, shape, s) ||
-           launch_rows<T, NORM, 4, 16>(p, shape, s) || launch_rows<T, NORM, 8, 16>(p, shape, s) || launch_rows<T, NORM, 8, 32>(p, shape, s));
+    std::tuple<P...> held(args...);
+    const hipError_t err = std::apply([&](auto&... p) {
+        void* at[] = {const_cast<void*>(static_cast<const void*>(&p))...};
+        return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, dim3(threads), at, 0, s);
+    }, held);
+    if (err != hipSuccess) (void)hipGetLastError();     // (told by status, and by nothing else)
+    return static_cast<int>(err);
 }
 
-template <typename T> void launch_backward(const NormBackArgs& p, unsigned groups, hipStream_t s)
+template <typename T, bool NORM, int WAVES, int E> int launch_rows(const NormArgs& p, hipStream_t s)
+{
+    const unsigned groups = WAVES == 1 ? blocks(p.rows, 4) : static_cast<unsigned>(p.rows);
+    return launch(ctc_rows_to_8_bits_kernel<T, WAVES, E, NORM>, spread(groups), WAVES == 1 ? 256 : WAVES * kWave, s, p);
+}
+template <typename T, bool NORM> int launch_to_8_bits(const NormArgs& p, hipStream_t s)
+{
+    const RowShape shape = row_shape(p.rows, p.H);
+    switch (shape.waves) {
+    case 1: return shape.elements == 8 ? launch_rows<T, NORM, 1, 8>(p, s) : launch_rows<T, NORM, 1, 16>(p, s);
+    case 2: return shape.elements == 8 ? launch_rows<T, NORM, 2, 8>(p, s) : launch_rows<T, NORM, 2, 16>(p, s);
+    case 4: return shape.elements == 8 ? launch_rows<T, NORM, 4, 8>(p, s) : launch_rows<T, NORM, 4, 16>(p, s);
+    default:
+        return shape.elements == 8    ? launch_rows<T, NORM, 8, 8>(p, s)
+               : shape.elements == 16 ? launch_rows<T, NORM, 8, 16>(p, s)
+                                      : launch_rows<T, NORM, 8, 32>(p, s);
+    }
+}
+
+template <typename T> int launch_backward(const NormBackArgs& p, unsigned groups, hipStream_t s)
 {
     const dim3 grid(groups);
     // As few wavefronts to a row as hold it in registers, for each wavefront more is one more to wait for in the row's sums (27200 rows
     // of 1024 bf16: one wavefront with 16 a lane 39 us, two with 8 50, four with 8 67; 5556 of 3204 fp32: four with 16 54.7, eight with 8 58.6),
     // until registers are what a compute unit runs out of (5600 of 1999 fp32: two with 16 37.3, four with 8 35.1; 4000 of 5000: eight with
     // 16 66, sixteen with 8 62).
-    if (p.H <= 512)
-        hipLaunchKernelGGL((ctc_norm_backward_kernel<T, 1, 8>), grid, dim3(256), 0, s, p);
-    else if (p.H <= 1024)
-        hipLaunchKernelGGL((ctc_norm_backward_kernel<T, 1, 16>), grid, dim3(256), 0, s, p);
-    else if (p.H <= 2048)
-        hipLaunchKernelGGL((ctc_norm_backward_kernel<T, 4, 8>), grid, dim3(256), 0, s, p);
-    else if (p.H <= 4096)
-        hipLaunchKernelGGL((ctc_norm_backward_kernel<T, 4, 16>), grid, dim3(256), 0, s, p);
-    else if (p.H <= 8192)
-        hipLaunchKernelGGL((ctc_norm_backward_kernel<T, 16, 8>), grid, dim3(1024), 0, s, p);
-    else
-        hipLaunchKernelGGL((ctc_norm_backward_kernel<T, 8, 32>), grid, dim3(512), 0, s, p);
+    if (p.H <= 512) return launch(ctc_norm_backward_kernel<T, 1, 8>, grid, 256, s, p);
+    if (p.H <= 1024) return launch(ctc_norm_backward_kernel<T, 1, 16>, grid, 256, s, p);
+    if (p.H <= 2048) return launch(ctc_norm_backward_kernel<T, 4, 8>, grid, 256, s, p);
+    if (p.H <= 4096) return launch(ctc_norm_backward_kernel<T, 4, 16>, grid, 256, s, p);
+    if (p.H <= 8192) return launch(ctc_norm_backward_kernel<T, 16, 8>, grid, 1024, s, p);
+    return launch(ctc_norm_backward_kernel<T, 8, 32>, grid, 512, s, p);
 }
 
-template <typename T, int WM, int WN> void launch_tiles(const LinearArgs& p, hipStream_t s)
+template <typename T, int WM, int WN> int launch_tiles(const LinearArgs& p, hipStream_t s)
 {
     const int64_t tiles = static_cast<int64_t>(blocks(p.rows, 64 * WM)) * blocks(p.A, 64 * WN);
-    hipLaunchKernelGGL((ctc_linear_tiles_kernel<T, WM, WN>), dim3(blocks(tiles, 8) * 8), dim3(256), 0, s, p);
+    return launch(ctc_linear_tiles_kernel<T, WM, WN>, dim3(blocks(tiles, 8) * 8), 256, s, p);
 }
-template <typename T> void launch_direct(const LinearArgs& p, hipStream_t s)
+template <typename T> int launch_direct(const LinearArgs& p, hipStream_t s)
 {
-    hipLaunchKernelGGL(ctc_linear_direct_kernel<T>, dim3(blocks(p.rows, 16) * blocks(p.A, 16)), dim3(256), 0, s, p);
+    return launch(ctc_linear_direct_kernel<T>, dim3(blocks(p.rows, 16) * blocks(p.A, 16)), 256, s, p);
 }
-template <typename T> void launch_product(const LinearArgs& p, ProductTile tile, hipStream_t s)
+template <typename T> int launch_product(const LinearArgs& p, ProductTile tile, hipStream_t s)
 {
-    if (tile.rows == 16)
-        launch_direct<T>(p, s);
-    else if (tile.symbols == 64 && tile.rows == 128)
-        launch_tiles<T, 2, 1>(p, s);
-    else if (tile.symbols == 64)
-        launch_tiles<T, 1, 1>(p, s);
-    else if (tile.symbols == 128)
-        launch_tiles<T, 2, 2>(p, s);
-    else
-        launch_tiles<T, 4, 4>(p, s);
+    if (tile.rows == 16) return launch_direct<T>(p, s);
+    if (tile.symbols == 64) return tile.rows == 128 ? launch_tiles<T, 2, 1>(p, s) : launch_tiles<T, 1, 1>(p, s);
+    return tile.symbols == 128 ? launch_tiles<T, 2, 2>(p, s) : launch_tiles<T, 4, 4>(p, s);
 }
 
-template <typename T> void launch_gradient(const GradientArgs& p, const GradientPlan& plan, float* workspace, hipStream_t s)
+template <typename T> int launch_gradient(const GradientArgs& p, const GradientPlan& plan, float* workspace, hipStream_t s)
 {
     const dim3 grid(blocks(p.A, plan.symbols), blocks(p.H, plan.columns), static_cast<unsigned>(p.slabs));
-    if (plan.symbols == 32) {
-        hipLaunchKernelGGL((ctc_weight_gradient_narrow_kernel<T, 1>), grid, dim3(512), 0, s, p);
-    } else if (plan.symbols == 64) {
-        hipLaunchKernelGGL((ctc_weight_gradient_narrow_kernel<T, 2>), grid, dim3(512), 0, s, p);
-    } else {
-        uint16_t* const wide = reinterpret_cast<uint16_t*>(workspace + plan.wide_at);
-        const unsigned columns = blocks(p.A, 2 * kWave);
-        hipLaunchKernelGGL(ctc_gradient_prepare_kernel<T>, spread(columns * kColumnSlabs + blocks(p.rows, 32) * blocks(p.pitch, 256)), dim3(256), 0, s, p,
+    if (plan.symbols == 32) return launch(ctc_weight_gradient_narrow_kernel<T, 1>, grid, 512, s, p);
+    if (plan.symbols == 64) return launch(ctc_weight_gradient_narrow_kernel<T, 2>, grid, 512, s, p);
+    uint16_t* const wide = reinterpret_cast<uint16_t*>(workspace + plan.wide_at);
+    const unsigned columns = blocks(p.A, 2 * kWave);
+    const int err = launch(ctc_gradient_prepare_kernel<T>, spread(columns * kColumnSlabs + blocks(p.rows, 32) * blocks(p.pitch, 256)), 256, s, p,
                            reinterpret_cast<uint32_t*>(workspace + plan.largest_at), wide, columns);
-        hipLaunchKernelGGL(ctc_weight_gradient_wide_kernel<T>, grid, dim3(512), 0, s, p, wide);
-    }
+    return err ? err : launch(ctc_weight_gradient_wide_kernel<T>, grid, 512, s, p, wide);
 }
 
 }  // namespace
 
 int launch_pack_frames(const int32_t* lengths, int T, int B, int32_t* frames, void* stream)
 {
-    hipLaunchKernelGGL(ctc_pack_frames_kernel, spread(blocks(T, 4)), dim3(256), 0, static_cast<hipStream_t>(stream), lengths, T, B,
-                       frames);
-    return last_error();
+    return launch(ctc_pack_frames_kernel, spread(blocks(T, 4)), 256, static_cast<hipStream_t>(stream), lengths, T, B, frames);
 }
 
 int launch_quantize(const void* x, const int32_t* frames, int rows, int H, bool bf16, int8_t* q, float* scales, void* stream)
 {
     const NormArgs p = {x, nullptr, nullptr, 0.0f, frames, rows, H, pitch_of(H), nullptr, q, scales};
-    if (bf16)
-        launch_to_8_bits<bf16_t, false>(p, static_cast<hipStream_t>(stream));
-    else
-        launch_to_8_bits<float, false>(p, static_cast<hipStream_t>(stream));
-    return last_error();
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return bf16 ? launch_to_8_bits<bf16_t, false>(p, s) : launch_to_8_bits<float, false>(p, s);
 }
 
 int launch_norm(const void* x, const void* residual, const float* weight, float eps, const int32_t* frames, int rows, int H,
                 bool bf16, void* sum, int8_t* q, float* scales, void* stream)
 {
     const NormArgs p = {x, residual, weight, eps, frames, rows, H, pitch_of(H), sum, q, scales};
-    if (bf16)
-        launch_to_8_bits<bf16_t, true>(p, static_cast<hipStream_t>(stream));
-    else
-        launch_to_8_bits<float, true>(p, static_cast<hipStream_t>(stream));
-    return last_error();
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return bf16 ? launch_to_8_bits<bf16_t, true>(p, s) : launch_to_8_bits<float, true>(p, s);
 }
 
 int launch_dequantize(const int8_t* q, const float* scales, const int32_t* frames, int rows, int H, bool bf16, void* out,
                       void* stream)
 {
-    const dim3 grid = spread(blocks(rows, 4)), block(256);
+    const dim3 grid = spread(blocks(rows, 4));
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (bf16)
-        hipLaunchKernelGGL(ctc_rows_from_8_bits_kernel<bf16_t>, grid, block, 0, s, q, scales, frames, rows, H, pitch_of(H),
-                           static_cast<bf16_t*>(out));
-    else
-        hipLaunchKernelGGL(ctc_rows_from_8_bits_kernel<float>, grid, block, 0, s, q, scales, frames, rows, H, pitch_of(H),
-                           static_cast<float*>(out));
-    return last_error();
+    if (bf16) return launch(ctc_rows_from_8_bits_kernel<bf16_t>, grid, 256, s, q, scales, frames, rows, H, pitch_of(H), static_cast<bf16_t*>(out));
+    return launch(ctc_rows_from_8_bits_kernel<float>, grid, 256, s, q, scales, frames, rows, H, pitch_of(H), static_cast<float*>(out));
 }
 
 int launch_norm_backward(const void* dy, const void* sum, const float* weight, float eps, const void* dresidual,
@@ -1394,15 +1379,9 @@ int launch_norm_backward(const void* dy, const void* sum, const float* weight, f
     hipStream_t s = static_cast<hipStream_t>(stream);
     const int groups = norm_partials(rows, H);
     const NormBackArgs p = {dy, sum, weight, eps, dresidual, frames, rows, H, dsum, dweight ? partials : nullptr};
-    if (bf16)
-        launch_backward<bf16_t>(p, static_cast<unsigned>(groups), s);
-    else
-        launch_backward<float>(p, static_cast<unsigned>(groups), s);
-    const int err = last_error();
+    const int err = bf16 ? launch_backward<bf16_t>(p, static_cast<unsigned>(groups), s) : launch_backward<float>(p, static_cast<unsigned>(groups), s);
     if (err || !dweight) return err;
-    hipLaunchKernelGGL(ctc_sum_partials_kernel, dim3(blocks(H, 16)), dim3(1024), 0, s, partials, groups,
-                       static_cast<int64_t>(H), static_cast<int64_t>(H), dweight);
-    return last_error();
+    return launch(ctc_sum_partials_kernel, dim3(blocks(H, 16)), 1024, s, partials, groups, static_cast<int64_t>(H), static_cast<int64_t>(H), dweight);
 }
 
 int launch_linear(const int8_t* q, const float* scales, const int8_t* weight_q, const float* weight_scales, const float* bias,
@@ -1410,11 +1389,8 @@ int launch_linear(const int8_t* q, const float* scales, const int8_t* weight_q, 
 {
     const LinearArgs p = {q, scales, weight_q, weight_scales, bias, frames, rows, A, pitch_of(H), logits};
     const ProductTile tile = product_tile(rows, H, A, frames != nullptr);
-    if (bf16)
-        launch_product<bf16_t>(p, tile, static_cast<hipStream_t>(stream));
-    else
-        launch_product<float>(p, tile, static_cast<hipStream_t>(stream));
-    return last_error();
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return bf16 ? launch_product<bf16_t>(p, tile, s) : launch_product<float>(p, tile, s);
 }
 
 int launch_weight_gradient(const void* grads, const int8_t* q, const float* scales, const int32_t* frames, int rows, int H,
@@ -1426,17 +1402,11 @@ int launch_weight_gradient(const void* grads, const int8_t* q, const float* scal
     const GradientArgs p = {grads, q, scales, frames, rows, H, A, pitch_of(H), plan.slabs,
                             plan.slabs > 1 ? workspace : dweight, dbias ? bias : nullptr,
                             reinterpret_cast<const uint32_t*>(workspace + plan.largest_at)};
-    if (bf16)
-        launch_gradient<bf16_t>(p, plan, workspace, s);
-    else
-        launch_gradient<float>(p, plan, workspace, s);
-    const int err = last_error();
-    if (err) return err;
+    const int err = bf16 ? launch_gradient<bf16_t>(p, plan, workspace, s) : launch_gradient<float>(p, plan, workspace, s);
     const unsigned weight_blocks = plan.slabs > 1 ? blocks(weights, 1024) : 0, bias_blocks = dbias ? blocks(A, 256) : 0;
-    if (weight_blocks + bias_blocks == 0) return 0;
-    hipLaunchKernelGGL(ctc_sum_slabs_kernel, dim3(weight_blocks + bias_blocks), dim3(256), 0, s, workspace, plan.slabs, weights, dweight, weight_blocks,
-                       bias, plan.bias_slabs, A, dbias);
-    return last_error();
+    if (err || weight_blocks + bias_blocks == 0) return err;
+    return launch(ctc_sum_slabs_kernel, dim3(weight_blocks + bias_blocks), 256, s, workspace, plan.slabs, weights, dweight, weight_blocks, bias,
+                  plan.bias_slabs, A, dbias);
 }
 
 }  // namespace layer
