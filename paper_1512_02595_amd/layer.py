@@ -8,6 +8,7 @@ fallback.
 from __future__ import annotations
 
 import ctypes
+import operator
 
 from . import ctc
 
@@ -49,9 +50,17 @@ def last_hip_error() -> int:
     return int(load().ctc_layer_last_hip_error())
 
 
+def _size(v) -> int:
+    """A whole number that a C int holds, as the native module takes one (ctypes would drop what does not fit)."""
+    v = operator.index(v)
+    if not -2 ** 31 <= v < 2 ** 31:
+        raise OverflowError("a size is out of a 32-bit integer's range")
+    return v
+
+
 def row_pitch(H) -> int:
     """Bytes from one row in 8 bits to the next; 0 for a width that is refused."""
-    return int(load().ctc_row_pitch(int(H)))
+    return int(load().ctc_row_pitch(_size(H)))
 
 
 def _check(status: int, where: str) -> None:
@@ -69,7 +78,7 @@ def _module():
 def rms_norm_workspace_size_status(rows, H):
     """(status, bytes), without raising."""
     out = ctypes.c_size_t(0)
-    return int(load().ctc_rms_norm_workspace_size(int(rows), int(H), ctypes.byref(out))), int(out.value)
+    return int(load().ctc_rms_norm_workspace_size(_size(rows), _size(H), ctypes.byref(out))), int(out.value)
 
 
 def rms_norm_workspace_size(rows, H) -> int:
@@ -81,7 +90,8 @@ def rms_norm_workspace_size(rows, H) -> int:
 def weight_gradient_workspace_size_status(rows, H, A):
     """(status, bytes), without raising."""
     out = ctypes.c_size_t(0)
-    return int(load().ctc_weight_gradient_workspace_size(int(rows), int(H), int(A), ctypes.byref(out))), int(out.value)
+    st = load().ctc_weight_gradient_workspace_size(_size(rows), _size(H), _size(A), ctypes.byref(out))
+    return int(st), int(out.value)
 
 
 def weight_gradient_workspace_size(rows, H, A) -> int:
