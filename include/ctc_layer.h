@@ -84,7 +84,7 @@ ctc_status_t ctc_pack_frames(const int32_t *input_lengths, int T, int B, int32_t
 ctc_status_t ctc_quantize_rows(const void *x, const int32_t *frames, int rows, int H, ctc_dtype_t dtype,
                                int8_t *q, float *scales, hipStream_t stream);
 
-/* And back: out (device) [rows, H] of type dtype = q * scales, rounded once. */
+/* And back: out (device) [rows, H] of type dtype = q * scales, a product in fp32, rounded to dtype. */
 ctc_status_t ctc_dequantize_rows(const int8_t *q, const float *scales, const int32_t *frames, int rows, int H,
                                  ctc_dtype_t dtype, void *out, hipStream_t stream);
 
@@ -136,8 +136,8 @@ ctc_status_t ctc_rms_norm_backward(const void *dy, const void *sum, const float 
  *
  *     logits[r][a] = scales[r] * weight_scales[a] * sum_k q[r][k] * weight_q[a][k]  + bias[a]
  *
- * The sums are exact; the products with the scales and the sum with the bias are in fp32, rounded to
- * dtype once.  Rows that are not listed are never read by ctc_loss_and_grad either.
+ * The sums are exact; from there on all is in fp32 (the sum as such a number, the product of the scales, its product
+ * with the sum and the bias added in one step), rounded to dtype at last.  Rows that are not listed are never read by ctc_loss_and_grad either.
  *
  *   q, scales                (device) [rows, ctc_row_pitch(H)], [rows]
  *   weight_q, weight_scales  (device) [A, ctc_row_pitch(H)] (16-byte aligned), [A]: the weights as
@@ -156,8 +156,8 @@ ctc_status_t ctc_linear_i8(const int8_t *q, const float *scales, const int8_t *w
  *     dbias[a]      = sum over the listed rows of  grads[r][a]
  *
  * grads[r][a] * scales[r] is rounded to fp32 and enters the matrix cores in parts of 16 bits that hold it to
- * within 2^-23 of itself (where symbols, states and rows are many: or 2^-38 of its symbol's largest, if that is
- * more); sums are in fp32, in an order that the sizes and the list fix.  A product that is an infinity or a NaN gives
+ * within 2^-23 of itself or 2^-133, if that is more (where symbols, states and rows are many: 2^-38 of its symbol's
+ * largest, if that is more); sums are in fp32, in an order that the sizes and the list fix.  A product that is an infinity or a NaN gives
  * its symbol's row of dweight NaNs.
  *
  *   grads      (device) [rows, A] of type dtype, as ctc_loss_and_grad writes them

@@ -705,8 +705,8 @@ __global__ __launch_bounds__(256) void ctc_linear_tiles_kernel(LinearArgs p)
 // gradients take their scale and are split, and whole numbers become floats, and are laid down in LDS with the rows innermost.
 //
 // A product of gradient and scale, an fp32 number c, enters the matrix cores
-//   as three bf16 numbers, the leading 8 bits, the next 8 and the last (exact at any size): narrow tiles, whose gradients' work is done as
-//   they come, or
+//   as three bf16 numbers, the leading 8 bits, the next 8 and the last (exact from 2^-110 on; below, bits under 2^-133, where bf16 ends, are
+//   lost): narrow tiles, whose gradients' work is done as they come, or
 //   as two fp16 numbers, each rounded to nearest (22 bits and a sign; c is off by at most half its last bit or 2^-39 of its column's
 //   largest), after a power of two that puts the column's largest in [2^14, 2^15): wide tiles, which the matrix cores bind.  The columns' largest
 //   take one more reading of the gradients, a launch of its own, which also forms the bias's gradient.

@@ -157,3 +157,27 @@ def test_norm_gradients_of_many_rows(rows, H, dtype, kind):
                                  rows, H, 1e-5, frames)
     base.check_backward(out, dweight, dy, z, w, dres, dtype, rows, H, 1e-5, names)
     assert out.untouched(others(rows, names)) and out.intact()
+
+
+@pytest.mark.parametrize("top", [60, 0, -100, -110, -120, -126, -130])
+@pytest.mark.parametrize("rows, H, A, symbols", [(3000, 120, 29, 32), (3000, 120, 60, 64), (12000, 640, 172, 64), (9000, 700, 2001, 128)])
+def test_the_smallest_products_of_the_weights_gradient(rows, H, A, symbols, top):
+    """Each element is one product; a symbol's are of sizes from 2^top down to 2^-25 of it, so down to and below what fp32 and bf16 hold."""
+    print("smallest products", rows, H, A, top, flush=True)
+    assert rules.gradient_tile(rows, H, A)[0] == symbols
+    rng = np.random.default_rng(rows + A)
+    q = torch.from_numpy(rng.integers(1, 128, (rows, H)) * rng.choice([-1, 1], (rows, H)))
+    q = torch.where(torch.arange(H)[None, :] % EACH == torch.arange(rows)[:, None] % EACH, q, 0)
+    where = torch.from_numpy(rng.integers(0, rows // EACH, (A, EACH)) * EACH + np.arange(EACH))
+    c = torch.from_numpy((1 + rng.random((A, EACH))) * 2.0 ** (top - 5 * np.arange(EACH))[None, :] * rng.choice([-1, 1], (A, EACH))).float()
+    grads = torch.zeros(rows, A)
+    grads[where, torch.arange(A)[:, None]] = c
+    dweight, _ = base.weight_gradient(grads, q, torch.ones(rows), F32)
+    column = torch.arange(H) % EACH
+    size = c.double()[:, column]
+    levels = q[where].double().sum(1)                    # (the one row of a symbol's that is not 0 there)
+    # two half steps by the parts, at most three of which are added; bf16 ends at 2^-133, and the parts of wide tiles at 2^-38 of the largest; the result
+    # is an fp32 number, of which there are none between multiples of 2^-149
+    least = torch.full((A, 1), 2.0 ** -133, dtype=torch.float64) if symbols < 128 else 2.0 ** -38 * c.double().abs().amax(1, keepdim=True)
+    bound = levels.abs() * (HALF * (2 + 3) * 1.001 * size.abs() + least) + 2.0 ** -149
+    assert ((dweight.t.cpu().double() - size * levels).abs() <= bound).all()
