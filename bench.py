@@ -10,7 +10,8 @@ per-GPU minibatch (config index 1: B=64, A=29, T<=750).  Prints one JSON line.
 --mode loss times the cost-only call (grads == NULL), --mode align the most probable
 alignment (ctc_best_path); the default, grad, is the headline metric.  --mode layer times the
 output layer around it as well: states of --width to activations to cost and gradient to the
-weights' gradient, with states and weights in 8 bits.
+weights' gradient, with states and weights in 8 bits (and not what lies below: the states'
+gradient, which the library does not compute, and the norm's, which follows from it).
 """
 from __future__ import annotations
 
@@ -292,10 +293,15 @@ def main():
 
     B = batches[0].B
     frames = float(np.mean([b.frames for b in batches]))
+    layer_bytes = 0
+    if args.mode == "layer":
+        layer_bytes = sum(t.numel() * t.element_size() for out, *given in layers.values()
+                          for t in (*given, out.sum, out.q, out.scales, out.weight_q, out.dweight, *out.ws))
     if args.mode in ("grad", "layer"):
         compulsory = float(np.mean([b.compulsory_bytes(elem) for b in batches]))
-        if args.mode == "layer":    # states and residual once, their sum written, rows in 8 bits written and read twice, weights read, their gradient written
-            compulsory += frames * args.width * (3 * elem + 3) + batches[0].A * args.width * 5
+        if args.mode == "layer":    # states and residual once, their sum written, rows in 8 bits written and read twice, weights read, their gradient written,
+            #                         activations written and their gradient read
+            compulsory += frames * args.width * (3 * elem + 3) + batches[0].A * args.width * 5 + 2 * frames * batches[0].A * elem
     else:       # the valid activations once; the alignment also writes one int32 per frame of the tensor
         compulsory = float(np.mean([b.frames * b.A * elem for b in batches]))
         if args.mode == "align":
@@ -366,9 +372,10 @@ def main():
         "ms_per_call_median": round(float(np.median(per_call)), 5),
         "ms_per_call_min": round(float(per_call.min()), 5),
         "ms_per_step_cache_warm": round(warm_ms, 5),
-        "rotating_bytes": int(sum(d.x.numel() * d.x.element_size() * 2 + d.ws_bytes for d in dbs)),
+        "rotating_bytes": int(sum(d.x.numel() * d.x.element_size() * 2 + d.ws_bytes for d in dbs)) + layer_bytes,
         "higher_is_better": True, "scaling": "weak", "vs_baseline": None,
-        "dtype": "f64 lattice state (probabilities with a per-lane exponent), %s activations" % args.dtype,
+        "dtype": "f64 lattice state (probabilities with a per-lane exponent), %s activations" % args.dtype
+                 + (", states and weights of the output layer in 8 bits, its sums in 32" if args.mode == "layer" else ""),
         "data": "synthetic",
         "gradient_beside_chains": bool(beside),
         "config": {"workload": "config[%d] %s: B=%d A=%d T=%d, %d rotating minibatches"
@@ -384,7 +391,7 @@ def main():
         "paper_context": PAPER_CONTEXT,
     }
 
-    if not args.no_cpu_baseline:
+    if not args.no_cpu_baseline and args.mode != "layer":          # (the oracle has no output layer)
         from oracle import ctc_oracle as orc
         b = batches[0]
         x64 = b.logits.astype(np.float64) if dtype == ctc.DTYPE_F32 else workloads.to_bf16_grid(b.logits).astype(np.float64)
