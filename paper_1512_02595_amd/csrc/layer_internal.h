@@ -54,7 +54,8 @@ struct ProductTile {
 };
 inline ProductTile product_tile(int all_rows, int H, int A, bool list)
 {
-    // Of a list's rows, five in eight are taken to count (how many do, only the GPU knows).
+    // Of a list's rows, five in eight are taken to count (how many do, only the GPU knows; the workspaces' sizes above and below are for all rows, since
+    // they are told without a list).
     const int64_t rows = list ? (static_cast<int64_t>(all_rows) * 5 + 7) / 8 : all_rows;
     const auto tiles = [&](int m, int n) { return (rows + m - 1) / m * ((A + n - 1) / n); };
     // Tiles of 256 by 256 read the least of memory and LDS, those of 128 by 128, two of which share a compute unit, begin and end sooner: the times
@@ -63,7 +64,9 @@ inline ProductTile product_tile(int all_rows, int H, int A, bool list)
     const double steps = pitch_of(H) / 64;
     const double large = static_cast<double>((tiles(256, 256) + 255) / 256) * (13.5 + 0.85 * steps);
     const double small = static_cast<double>((tiles(128, 128) + 511) / 512) * (7.0 + 0.65 * steps);
-    if (tiles(16, 16) <= 400) return {16, 16};                          // 1 x 6000 4.5 us against 6.0 in tiles of 64 by 64, 16 x 6000 5.9 and 6.1, 32 x 6000 7.8 and 6.3
+    // (By tiles alone, whatever the rows: 1 x 6000 4.5 us against 6.0 in tiles of 64 by 64, 16 x 6000 5.9 and 6.1, 32 x 6000 7.8 and 6.3.  Few rows by
+    // more than 6400 symbols have not been measured.)
+    if (tiles(16, 16) <= 400) return {16, 16};
     if (A <= 64 && tiles(64, 64) > 400) return {128, 64};               // 27200 x 60 14.7 us against 15.6; 5000 x 60 8.4 against 6.8
     if (tiles(64, 64) <= 600) return {64, 64};                          // 300 x 6000 10.9 us against 13.7 in 128 by 128; 1500 x 2000 (768 tiles) 11.1 and 10.8
     return small < large ? ProductTile{128, 128} : ProductTile{256, 256};

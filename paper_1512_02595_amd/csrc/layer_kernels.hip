@@ -28,7 +28,8 @@ template <> __device__ __forceinline__ bf16_t narrow<bf16_t>(float v)
 }
 
 // Bytes of rows that nobody reads soon are written past the caches: they would take the place of what is being read, and a cache that has to let
-// go of old lines to take new ones slows both.  28 900 of 48 000 rows of 2048 bf16: from 8 bits 43 us -> 27.5, the norm 91 -> 80.
+// go of old lines to take new ones slows both.  28 900 of 48 000 rows of 2048 bf16: from 8 bits 43 us -> 27.5, the norm 91 -> 80.  (The partial sums
+// of the norm's gradient take the same way, though the launch behind reads them at once; kept in the caches they have not been measured.)
 template <int BYTES> __device__ __forceinline__ void store_past(void* to, const void* from)
 {
     typedef uint32_t words_t __attribute__((ext_vector_type(BYTES / 4), aligned(2)));

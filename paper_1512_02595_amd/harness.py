@@ -248,7 +248,8 @@ class OutputLayer:
         """(gradient of the norm's input [T, B, H], of its weight); frames behind an utterance's end get zeros, as in CTC's gradient."""
         given = [None if t is None else self._states(t) for t in (dy, dresidual)]
         with self._on(stream):
-            # The library leaves such rows as they were, which may be the last minibatch's.  (An input in `dsum`'s own place is read afterwards.)
+            # The library leaves such rows as they were, which may be the last minibatch's.  (A fill: 28900 of 48000 rows of 2048 fp32 133 us -> 225, bf16
+            # 90 -> 118; which rows they are only the GPU knows.  An input in `dsum`'s own place is read afterwards.)
             if self.dsum.data_ptr() in given:
                 aside = self.dsum.clone()
                 given = [aside.data_ptr() if at == self.dsum.data_ptr() else at for at in given]
