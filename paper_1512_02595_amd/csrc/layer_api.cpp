@@ -2,49 +2,14 @@
 // kernels are enqueued.  Nothing is allocated, waited for or kept.
 
 #include <cmath>
-#include <initializer_list>
 
+#include "layer_checks.h"
 #include "layer_internal.h"
 
 namespace layer {
 namespace {
 
 thread_local int g_last_hip_error = 0;
-
-ctc_status_t launched(int err)
-{
-    if (err == 0) return CTC_STATUS_SUCCESS;
-    g_last_hip_error = err;
-    return CTC_STATUS_HIP_ERROR;
-}
-
-// A buffer of the call.  An output may not overlap any other buffer, unless it is `alias`-ed to it: the same
-// address and, by the caller's word, the same shape.
-struct Buffer {
-    const void* at;
-    size_t bytes;
-    bool output;
-    bool required = true;
-    size_t align = 4;
-    bool alias = false;              // this input may be the output that `may_alias` is set for
-    bool may_alias = false;
-};
-
-bool buffers_in_order(std::initializer_list<Buffer> list)
-{
-    for (const Buffer& b : list) {
-        if (!b.at && b.required) return false;
-        if (reinterpret_cast<uintptr_t>(b.at) % b.align) return false;
-    }
-    for (const Buffer* a = list.begin(); a != list.end(); ++a)
-        for (const Buffer* b = a + 1; b != list.end(); ++b) {
-            if (!(a->output || b->output) || !a->at || !b->at) continue;
-            if (a->at == b->at && ((a->alias && b->may_alias) || (b->alias && a->may_alias))) continue;
-            const uintptr_t i = reinterpret_cast<uintptr_t>(a->at), j = reinterpret_cast<uintptr_t>(b->at);
-            if (i < j + b->bytes && j < i + a->bytes) return false;
-        }
-    return true;
-}
 
 ctc_status_t sizes_in_range(int rows, int H, int A, ctc_dtype_t dtype)
 {
@@ -54,14 +19,17 @@ ctc_status_t sizes_in_range(int rows, int H, int A, ctc_dtype_t dtype)
     return CTC_STATUS_SUCCESS;
 }
 
-size_t element(ctc_dtype_t dtype) { return dtype == CTC_DTYPE_F32 ? 4 : 2; }
-size_t matrix(int rows, int width, size_t elem) { return static_cast<size_t>(rows) * width * elem; }
-size_t list_bytes(int rows) { return (static_cast<size_t>(rows) + 1) * 4; }
-size_t round_up(size_t v) { return (v + 255) / 256 * 256; }
-
 size_t norm_workspace(int rows, int H) { return round_up(static_cast<size_t>(norm_partials(rows, H)) * H * 4); }
 
 }  // namespace
+
+ctc_status_t launched(int err)
+{
+    if (err == 0) return CTC_STATUS_SUCCESS;
+    g_last_hip_error = err;
+    return CTC_STATUS_HIP_ERROR;
+}
+
 }  // namespace layer
 
 using namespace layer;

@@ -4,14 +4,7 @@
 // The functions take positional arguments only, in the order of the C functions, addresses as integers or None, and
 // return the status.  `bind` is given the addresses of the library's functions.
 
-#define PY_SSIZE_T_CLEAN
-#include <Python.h>
-
-#include <cstdint>
-#include <tuple>
-#include <utility>
-
-#include "ctc_layer.h"
+#include "layer_binding_calls.h"
 
 namespace {
 
@@ -23,67 +16,6 @@ decltype(&ctc_rms_norm_backward) g_rms_norm_backward;
 decltype(&ctc_linear_i8) g_linear_i8;
 decltype(&ctc_weight_gradient_i8) g_weight_gradient_i8;
 
-// One argument of a call, taken as the C type that the function has there.
-bool take(PyObject* o, int* out)
-{
-    PyObject* index = PyNumber_Index(o);
-    if (!index) return false;
-    const long v = PyLong_AsLong(index);
-    Py_DECREF(index);
-    if (v == -1 && PyErr_Occurred()) return false;
-    if (v < INT32_MIN || v > INT32_MAX) {
-        PyErr_SetString(PyExc_OverflowError, "a size is out of a 32-bit integer's range");
-        return false;
-    }
-    *out = static_cast<int>(v);
-    return true;
-}
-bool take(PyObject* o, ctc_dtype_t* out)
-{
-    int v;
-    if (!take(o, &v)) return false;
-    *out = static_cast<ctc_dtype_t>(v);
-    return true;
-}
-bool take(PyObject* o, float* out)
-{
-    const double v = PyFloat_AsDouble(o);
-    if (v == -1.0 && PyErr_Occurred()) return false;
-    *out = static_cast<float>(v);
-    return true;
-}
-bool take(PyObject* o, size_t* out)
-{
-    *out = PyLong_AsSize_t(o);
-    return *out != static_cast<size_t>(-1) || !PyErr_Occurred();
-}
-template <typename T> bool take(PyObject* o, T** out)                       // (None is the null pointer)
-{
-    void* p = o == Py_None ? nullptr : PyLong_AsVoidPtr(o);
-    *out = static_cast<T*>(p);
-    return p || !PyErr_Occurred();
-}
-
-template <typename... Args, size_t... I>
-PyObject* call_with(ctc_status_t (*f)(Args...), PyObject* const* a, Py_ssize_t n, std::index_sequence<I...>)
-{
-    if (n != static_cast<Py_ssize_t>(sizeof...(Args))) {
-        PyErr_Format(PyExc_TypeError, "expected %zu arguments, got %zd", sizeof...(Args), n);
-        return nullptr;
-    }
-    std::tuple<Args...> args;
-    if (!(take(a[I], &std::get<I>(args)) && ...)) return nullptr;
-    ctc_status_t st;
-    Py_BEGIN_ALLOW_THREADS
-    st = f(std::get<I>(args)...);
-    Py_END_ALLOW_THREADS
-    return PyLong_FromLong(st);
-}
-template <typename... Args> PyObject* call(ctc_status_t (*f)(Args...), PyObject* const* a, Py_ssize_t n)
-{
-    return call_with(f, a, n, std::index_sequence_for<Args...>());
-}
-
 PyObject* pack_frames(PyObject*, PyObject* const* a, Py_ssize_t n) { return call(g_pack_frames, a, n); }
 PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n) { return call(g_quantize_rows, a, n); }
 PyObject* dequantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n) { return call(g_dequantize_rows, a, n); }
@@ -91,13 +23,6 @@ PyObject* rms_norm_i8(PyObject*, PyObject* const* a, Py_ssize_t n) { return call
 PyObject* rms_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) { return call(g_rms_norm_backward, a, n); }
 PyObject* linear_i8(PyObject*, PyObject* const* a, Py_ssize_t n) { return call(g_linear_i8, a, n); }
 PyObject* weight_gradient_i8(PyObject*, PyObject* const* a, Py_ssize_t n) { return call(g_weight_gradient_i8, a, n); }
-
-template <typename F> bool address(PyObject* o, F* out)
-{
-    void* p = PyLong_AsVoidPtr(o);
-    *out = reinterpret_cast<F>(p);
-    return p != nullptr || !PyErr_Occurred();
-}
 
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
@@ -111,9 +36,6 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n)
         return nullptr;
     Py_RETURN_NONE;
 }
-
-using Fast = PyObject* (*)(PyObject*, PyObject* const*, Py_ssize_t);
-PyCFunction method(Fast f) { return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)); }
 
 PyMethodDef g_methods[] = {
     {"bind", method(bind), METH_FASTCALL, "Addresses of the library's functions, in the order of this module's."},
