@@ -1,0 +1,190 @@
+/*
+ * ctc_block.h -- a recurrent block under the output layer (gfx950).
+ *
+ * The network under the output layer is a stack of recurrent layers (Section 3 of the paper; bidirectional
+ * ones run over an utterance both ways, streaming ones forward only, Section 3.7).  The calls below are what a
+ * block of such a stack needs beside its matrix products: a gated linear recurrence over the frames, and the
+ * norm of what it makes, gated, scaled and added to the residual stream, with the norm before the next block.
+ * For streaming, where a few frames at a time meet all weights, there is the product with weights in 4 bits.
+ *
+ *   forward    ctc_recurrence              states of all frames from gates and candidates
+ *              ctc_block_norm              norm after a block, gate, scale, residual, norm before the next
+ *   backward   ctc_recurrence_backward     gradient of gates, candidates and initial states
+ *              ctc_block_norm_backward     gradient of its inputs and of its weights
+ *   streaming  ctc_quantize_weights_i4     weights to 4 bits with a scale per group of columns
+ *              ctc_dequantize_weights_i4   and back
+ *              ctc_linear_i4               activations from rows in 8 bits and weights in 4
+ *
+ * Same library, same manner as ctc_layer.h: plain C ABI, every buffer is the caller's, all work is enqueued on the
+ * given stream, nothing waits, nothing is allocated, errors are reported by status only, and on an error found during
+ * validation nothing has been enqueued.  No call reads host memory or keeps anything between calls, so all of them
+ * may be recorded into a HIP graph.  Results are bitwise repeatable from run to run on one device.  Calls that may
+ * overlap in time need outputs and workspaces of their own.  `stream` and all buffers belong to the calling
+ * thread's current device.  ctc_layer_last_hip_error tells these calls' HIP failures too.  Rows, lists of frames and
+ * rows in 8 bits are those of ctc_layer.h.
+ *
+ * Pitches.  Gates and candidates are columns of a projection, one product for all of a block's: a row of theirs lies
+ * `pitch` elements behind the one before.  What lies between a call's columns and the next row is neither read nor written.
+ *
+ * Limits.  T, B, rows, H, A >= 1, B <= 65535, T * B and rows <= 2^30, H <= CTC_MAX_STATE_WIDTH, A <= 2^20, pitches
+ * <= 2^20: more is refused with CTC_STATUS_UNSUPPORTED.  Pointers are aligned to their element type unless more is said; a
+ * misaligned one, a null pointer not marked as allowed, a pitch that is less than a row's columns, and an output that
+ * overlaps another buffer of the call (unless marked "may be") are refused with CTC_STATUS_INVALID_VALUE.
+ */
+#ifndef CTC_BLOCK_H
+#define CTC_BLOCK_H
+
+#include "ctc_layer.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/*
+ * Gated linear recurrence.  For each utterance and channel, over the utterance's frames in the channel's direction,
+ *
+ *     z = 1 / (1 + exp(-gate)),     h = h' + z (candidate - h')
+ *
+ * with h' the state of the frame before, or the initial state.  Channels below forward_channels run from the first
+ * frame to the last, the others from the last to the first.  States are carried in fp64 within a call and rounded once, to
+ * dtype where they are stored and to fp32 in `final_states`.
+ *
+ *   inputs            (device) [T*B rows, pitch] of type dtype: in each row H gates, then H candidates
+ *   input_pitch       elements from one row to the next, >= 2 H
+ *   input_lengths     (device) [B] int32; below 0 counts as 0, above T as T; NULL: all T
+ *   initial           (device) [B, H] float, or NULL: zeros
+ *   forward_channels  0..H; H: all run forward
+ *   states            (device) [T, B, H] of type dtype: receives h; rows behind an utterance's end stay
+ *   final_states      (device) [B, H] float: receives the state behind each channel's last frame (the initial one if
+ *                     there is none), or NULL; may be `initial` itself
+ *   workspace         (device) 256-byte aligned, ctc_recurrence_workspace_size bytes; NULL allowed if that is 0
+ *
+ * A workspace made for the longest and largest minibatch serves all: the size never shrinks as T, B or H grows.
+ */
+ctc_status_t ctc_recurrence_workspace_size(int T, int B, int H, size_t *bytes_out);
+ctc_status_t ctc_recurrence(const void *inputs, int input_pitch, const int32_t *input_lengths, const float *initial,
+                            int T, int B, int H, int forward_channels, ctc_dtype_t dtype, void *states,
+                            float *final_states, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Its gradient.  With D the whole gradient of a state h, from `dstates` and from the frame behind it,
+ *
+ *     D = dstates + (1 - z'') D''   ('': the frame behind; at a channel's last one, dfinal instead of the product)
+ *     dcandidate = z D,     dgate = z (1 - z) (candidate - h') D,     dinitial = (1 - z) D of a channel's first frame
+ *
+ *   dstates    (device) [T, B, H] of type dtype: gradient of the stored states; rows behind an utterance's end are not read
+ *   dfinal     (device) [B, H] float: gradient of final_states, or NULL: zeros
+ *   inputs, input_pitch, input_lengths, initial, forward_channels: as in the forward call
+ *   states     (device) [T, B, H] of type dtype, as the forward call stored them
+ *   dinputs    (device) [T*B rows, pitch] of type dtype, with the inputs' pitch: receives H dgates and H dcandidates a row;
+ *              rows behind an utterance's end stay
+ *   dinitial   (device) [B, H] float (dfinal for an utterance without frames), or NULL; may be `dfinal` itself
+ *   workspace  as in the forward call, of the same size
+ */
+ctc_status_t ctc_recurrence_backward(const void *dstates, const float *dfinal, const void *inputs, int input_pitch,
+                                     const void *states, const int32_t *input_lengths, const float *initial,
+                                     int T, int B, int H, int forward_channels, ctc_dtype_t dtype, void *dinputs,
+                                     float *dinitial, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Norm after a block, gate, residual scale, residual, norm before the next block.  For each row
+ *
+ *     n = x * weight_after / sqrt(mean_k x_k^2 + eps)
+ *     z = residual + scale * gate / (1 + exp(-gate)) * n,  rounded to dtype
+ *     y = z * weight_before / sqrt(mean_k z_k^2 + eps)
+ *
+ *   x              (device) [rows, H] of type dtype: what the block made
+ *   gate           (device) [rows, gate_pitch] of type dtype, H columns of each row, or NULL: no gate (a factor of 1)
+ *   gate_pitch     >= H; without a gate of no consequence
+ *   residual       (device) [rows, H] of type dtype, or NULL: zeros
+ *   weight_after, scale, weight_before  (device) [H] float, or NULL: ones
+ *   eps            finite and > 0
+ *   sum            (device) [rows, H] of type dtype: receives z, for the next block's residual and for
+ *                  ctc_block_norm_backward; may be x or residual itself; NULL: not written
+ *   normed         (device) [rows, H] of type dtype: receives y; may be x or residual itself; NULL: not written.
+ *                  One of the two is needed.
+ *   The last block's z goes to ctc_rms_norm_i8 instead, as its x.
+ */
+ctc_status_t ctc_block_norm(const void *x, const void *gate, int gate_pitch, const void *residual,
+                            const float *weight_after, const float *scale, const float *weight_before, float eps,
+                            const int32_t *frames, int rows, int H, ctc_dtype_t dtype, void *sum, void *normed,
+                            hipStream_t stream);
+
+/*
+ * Its gradient.  With r = 1 / sqrt(mean x^2 + eps), s = 1 / sqrt(mean z^2 + eps), a = gate / (1 + exp(-gate)) and sums
+ * over the listed rows,
+ *
+ *     D         = dsum + s (dnormed weight_before - z s^2 mean_k(dnormed weight_before z))
+ *     dresidual = D
+ *     dgate     = D scale weight_after x r a'
+ *     dx        = r (E - x r^2 mean_k(E x)),  E = D scale a weight_after
+ *     dweight_after = scale Q,  dscale = weight_after Q,  Q_k = sum of D a x r
+ *     dweight_before_k = sum of dnormed z s
+ *
+ *   dnormed    (device) [rows, H] of type dtype: gradient of y, or NULL: zeros (y was not used)
+ *   dsum       (device) the same: the gradient that reaches z by other ways, or NULL: zeros.  One of the two is needed.
+ *   x, gate, gate_pitch, weight_after, scale, weight_before, eps, frames: as in the forward call
+ *   sum        (device) [rows, H] of type dtype: the z that the forward call stored; NULL allowed without dnormed
+ *   dx         (device) [rows, H] of type dtype
+ *   dgate      (device) [rows, gate_pitch] of type dtype, H columns of each row; NULL without a gate, and only then
+ *   dresidual  (device) [rows, H] of type dtype, or NULL: not written
+ *              (dx and dresidual each may be x, sum, dnormed or dsum itself)
+ *   dweight_after, dscale, dweight_before  (device) [H] float each, or NULL: not computed.  Zeros if no row is listed.
+ *   workspace  (device) 256-byte aligned, ctc_block_norm_workspace_size bytes; NULL allowed without these three
+ *
+ * A workspace made for the largest minibatch serves all: the size never shrinks as rows grow.
+ */
+ctc_status_t ctc_block_norm_workspace_size(int rows, int H, size_t *bytes_out);
+ctc_status_t ctc_block_norm_backward(const void *dnormed, const void *dsum, const void *x, const void *gate, int gate_pitch,
+                                     const void *sum, const float *weight_after, const float *scale,
+                                     const float *weight_before, float eps, const int32_t *frames, int rows, int H,
+                                     ctc_dtype_t dtype, void *dx, void *dgate, void *dresidual, float *dweight_after,
+                                     float *dscale, float *dweight_before, void *workspace, size_t workspace_bytes,
+                                     hipStream_t stream);
+
+/*
+ * Weights in 4 bits.  A row's columns [i group, (i + 1) group) share a scale; with m the largest |value| of these, each is
+ * rounded to the whole number q in -7..7 nearest to 7 value / m in real arithmetic (of two equally near ones the even one),
+ * and the scale is m / 7 (0 for a group of zeros; a group that holds an infinity or a NaN gets zeros and the scale NaN).
+ *
+ *   group          64, or a multiple of 128 up to CTC_MAX_STATE_WIDTH
+ *   weight_q       (device, 16-byte aligned): for each 16 rows and each 128 columns 1024 bytes; of row r and byte i (0..63) there,
+ *                  byte 256 (i / 16) + 16 r + i % 16, whose low four bits hold column i and whose high four column 64 + i, as two's
+ *                  complements.  Rows and columns behind the last hold zeros.
+ *   weight_scales  (device, 16-byte aligned) float: for each 16 rows and each group 16 scales, row by row
+ *
+ * ctc_weights_i4_sizes tells the bytes of both.  Host computation; refuses what the other calls refuse.
+ */
+ctc_status_t ctc_weights_i4_sizes(int A, int H, int group, size_t *weight_bytes_out, size_t *scale_bytes_out);
+
+/*   weights  (device) [A, H] of type dtype */
+ctc_status_t ctc_quantize_weights_i4(const void *weights, int A, int H, int group, ctc_dtype_t dtype, uint8_t *weight_q,
+                                     float *weight_scales, hipStream_t stream);
+
+/* And back: out (device) [A, H] of type dtype = q * scale, a product in fp32, rounded to dtype. */
+ctc_status_t ctc_dequantize_weights_i4(const uint8_t *weight_q, const float *weight_scales, int A, int H, int group,
+                                       ctc_dtype_t dtype, void *out, hipStream_t stream);
+
+/*
+ * Activations from rows in 8 bits and weights in 4:
+ *
+ *     logits[r][a] = scales[r] * sum_i ( weight_scales[a][i] * sum over group i of q[r][k] weight_q[a][k] ) + bias[a]
+ *
+ * Sums over 64 columns are exact (over 128 where the group is not 64); from there on all is in fp32, in an order that the sizes
+ * fix, rounded to dtype at last.
+ *
+ *   q, scales                (device) [rows, ctc_row_pitch(H)], [rows], as ctc_rms_norm_i8 or ctc_quantize_rows wrote them
+ *   weight_q, weight_scales  as ctc_quantize_weights_i4 wrote them
+ *   bias                     (device) [A] float, or NULL
+ *   frames                   the rows that count, or NULL: all
+ *   logits                   (device) [rows, A] of type dtype
+ */
+ctc_status_t ctc_linear_i4(const int8_t *q, const float *scales, const uint8_t *weight_q, const float *weight_scales, int group,
+                           const float *bias, const int32_t *frames, int rows, int H, int A, ctc_dtype_t dtype,
+                           void *logits, hipStream_t stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* CTC_BLOCK_H */

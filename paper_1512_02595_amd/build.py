@@ -3,7 +3,7 @@
     python -m paper_1512_02595_amd.build
 
 hipcc cross-compiles without a GPU.  Packed-fp32 code generation is switched off
-for all device code.  The CTC path and the output layer's calls are compiled apart
+for all device code.  The CTC path and the layers' calls are compiled apart
 (the former takes it that no NaN arises) and linked into one library.
 """
 from __future__ import annotations
@@ -20,8 +20,10 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libctc_mi355x.so")
 SOURCES = ["ctc_kernels.hip", "ctc_api.cpp"]
 LAYER_SOURCES = ["layer_kernels.hip", "layer_api.cpp"]
+BLOCK_SOURCES = ["layer_recurrence_kernels.hip", "layer_block_kernels.hip", "layer_i4_kernels.hip", "layer_block_api.cpp"]
 BINDING = os.path.join(HERE, "_binding.so")
 LAYER_BINDING = os.path.join(HERE, "_layer_binding.so")
+BLOCK_BINDING = os.path.join(HERE, "_block_binding.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 
@@ -35,7 +37,7 @@ def _hipcc(more: list[str], out: str) -> list[str]:
 
 def object_command(source: str, out: str) -> list[str]:
     """One source to an object.  No NaN ever enters the CTC path's arithmetic (log 0 is a finite sentinel): that lets
-    max/min skip the quieting of their operands.  The output layer's calls pass NaNs on."""
+    max/min skip the quieting of their operands.  The layers' calls pass NaNs on."""
     flags = ["-fno-honor-nans"] if source in SOURCES else []
     return _hipcc([*flags, "-x", "hip", "-c", os.path.join(CSRC, source)], out)
 
@@ -65,12 +67,13 @@ def _compile(cmd: list[str], tmp: str, target: str, verbose: bool) -> None:
 
 
 def build(verbose: bool = False) -> str:
-    for target, source in ((BINDING, "binding.cpp"), (LAYER_BINDING, "layer_binding.cpp")):
+    for target, source in ((BINDING, "binding.cpp"), (LAYER_BINDING, "layer_binding.cpp"),
+                           (BLOCK_BINDING, "layer_block_binding.cpp")):
         tmp = target + f".tmp{os.getpid()}"
         _compile(binding_command(source, tmp), tmp, target, verbose)
     with tempfile.TemporaryDirectory() as folder:
         objects = []
-        for source in SOURCES + LAYER_SOURCES:
+        for source in SOURCES + LAYER_SOURCES + BLOCK_SOURCES:
             objects.append(os.path.join(folder, source + ".o"))
             _compile(object_command(source, objects[-1]), objects[-1], objects[-1], verbose)
         tmp = LIB + f".tmp{os.getpid()}"

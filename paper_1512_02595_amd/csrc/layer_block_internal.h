@@ -1,0 +1,120 @@
+// What the host side of the recurrent block's calls (layer_block_api.cpp) and their kernels (layer_recurrence_kernels.hip,
+// layer_block_kernels.hip, layer_i4_kernels.hip) share.
+#ifndef LAYER_BLOCK_INTERNAL_H
+#define LAYER_BLOCK_INTERNAL_H
+
+#include <cstddef>
+#include <cstdint>
+
+#include "ctc_block.h"
+#include "layer_internal.h"
+
+namespace layer {
+
+constexpr int kMaxUtterances = 65535;
+constexpr int kMaxPitch = 1 << 20;
+
+// ---- the recurrence ----
+
+struct RecurrenceArgs {
+    const void* inputs;
+    int64_t pitch;
+    const int32_t* lengths;
+    const float* initial;
+    int T, B, H, forward;
+    const void* states_in;          // backward: the forward call's
+    const void* dstates;
+    const float* dfinal;
+    void* out;                      // states, or dinputs
+    float* last;                    // final_states, or dinitial
+    double* workspace;
+};
+
+// Bytes of workspace: two numbers in fp64 for each channel of each stretch of frames, and the initial states; of more than one stretch only
+// where there are few channels, so that kMostCarried is never exceeded.
+constexpr int kShortestStretch = 128;
+constexpr int64_t kMostCarried = 3 * 1024 * 256;
+inline size_t recurrence_bytes(int T, int B, int H)
+{
+    if (T <= kShortestStretch) return 0;
+    const int64_t stretches = (static_cast<int64_t>(T) + kShortestStretch - 1) / kShortestStretch, all = (stretches + 1) * B * H;
+    return static_cast<size_t>(all < kMostCarried ? all : kMostCarried) * 16;
+}
+
+int launch_recurrence(const RecurrenceArgs& p, bool bf16, bool backward, void* stream);
+
+// ---- norms around a block ----
+
+struct BlockNormArgs {
+    const void* x;
+    const void* gate;
+    int64_t gate_pitch;
+    const void* residual;
+    const float* weight_after;
+    const float* scale;
+    const float* weight_before;
+    float eps;
+    const int32_t* frames;
+    int rows, H;
+    void* sum;
+    void* normed;
+};
+struct BlockNormBackArgs {
+    const void* dnormed;
+    const void* dsum;
+    const void* x;
+    const void* gate;
+    int64_t gate_pitch;
+    const void* sum;
+    const float* weight_after;
+    const float* scale;
+    const float* weight_before;
+    float eps;
+    const int32_t* frames;
+    int rows, H;
+    void* dx;
+    void* dgate;
+    void* dresidual;
+    float* partials;                // [groups][2][H]: sums for dweight_before, and Q; or null
+};
+
+// Workgroups of the backward pass, each of which leaves its partial sums.
+inline int block_norm_groups(int rows, int H)
+{
+    const int per_group = H <= 1024 ? 4 : 2;
+    const int groups = (rows + per_group - 1) / per_group;
+    return groups < 1024 ? groups : 1024;
+}
+
+int launch_block_norm(const BlockNormArgs& p, bool bf16, void* stream);
+int launch_block_norm_backward(const BlockNormBackArgs& p, bool bf16, float* dweight_after, float* dscale, float* dweight_before,
+                               void* stream);
+
+// ---- weights in 4 bits ----
+
+constexpr int kTileRows = 16, kTileColumns = 128, kTileBytes = 1024;
+
+inline bool group_in_order(int group) { return group == 64 || (group >= 128 && group % 128 == 0 && group <= kMaxWidth); }
+inline int groups_of(int H, int group) { return (H + group - 1) / group; }
+inline size_t weights_i4_bytes(int A, int H) { return static_cast<size_t>((A + 15) / 16) * (pitch_of(H) / kTileColumns) * kTileBytes; }
+inline size_t scales_i4_bytes(int A, int H, int group) { return static_cast<size_t>((A + 15) / 16) * groups_of(H, group) * 64; }
+
+struct LinearI4Args {
+    const int8_t* q;
+    const float* scales;
+    const uint8_t* weight_q;
+    const float* weight_scales;
+    int group, groups;
+    const float* bias;
+    const int32_t* frames;
+    int rows, A, pitch;
+    void* logits;
+};
+
+int launch_quantize_i4(const void* weights, int A, int H, int group, bool bf16, uint8_t* weight_q, float* weight_scales, void* stream);
+int launch_dequantize_i4(const uint8_t* weight_q, const float* weight_scales, int A, int H, int group, bool bf16, void* out, void* stream);
+int launch_linear_i4(const LinearI4Args& p, bool bf16, void* stream);
+
+}  // namespace layer
+
+#endif  // LAYER_BLOCK_INTERNAL_H
