@@ -1,4 +1,14 @@
 // Kernels of the gated linear recurrence (ctc_block.h).
+//
+// A step h = h' + z (c - h') is a map h' -> P h' + S with P = 1 - z, and so is any run of steps: the state behind it is P times the state before it, plus
+// the state that it ends in from zero.  So the frames of an utterance are dealt out in runs of kRun to the wavefronts of a workgroup, whose
+// lanes have channels: each finds its run's P and S from what it has brought into registers, the runs' are exchanged through LDS, and each wavefront
+// goes through its run once more from the state that the runs before it lead to, and writes.  The gradient is the same with the frames the other
+// way round: what reaches frame t from behind is P D'' with D'' = dstates'' + what reaches the frame behind, see ctc_block.h.  Every tensor is read and
+// written once, and the time of a workgroup does not depend on how long a chain of frames is, only on the bytes.
+//
+// Where channels and utterances are few, an utterance's frames are dealt out in stretches to several workgroups too: a first launch finds the P and S
+// of the stretches and leaves them in the workspace.
 
 #include <hip/hip_runtime.h>
 
@@ -16,42 +26,303 @@ __device__ __forceinline__ int length_of(const int32_t* lengths, int b, int T)
     return n < 0 ? 0 : n > T ? T : n;
 }
 
-// A channel of an utterance to a thread, frame after frame.
-template <typename T> __global__ __launch_bounds__(256) void ctc_recurrence_kernel(RecurrenceArgs p)
+// V neighbouring channels of a lane, of any alignment.
+template <typename T, int V> struct Some {
+    T v[V];
+};
+template <typename T, int V> __device__ __forceinline__ Some<T, V> load_some(const T* p)
 {
-    const int64_t i = group_number() * 256 + threadIdx.x;
-    if (i >= static_cast<int64_t>(p.B) * p.H) return;
-    const int b = static_cast<int>(i / p.H), k = static_cast<int>(i % p.H), n = length_of(p.lengths, b, p.T);
-    double h = p.initial ? static_cast<double>(p.initial[i]) : 0.0;
-    for (int s = 0; s < n; ++s) {
-        const int64_t row = static_cast<int64_t>(k < p.forward ? s : n - 1 - s) * p.B + b;
-        const T* in = static_cast<const T*>(p.inputs) + row * p.pitch + k;
-        h = fma(static_cast<double>(gate_of(widen(in[0])).z), static_cast<double>(widen(in[p.H])) - h, h);
-        static_cast<T*>(p.out)[row * p.H + k] = narrow<T>(static_cast<float>(h));
-    }
-    if (p.last) p.last[i] = static_cast<float>(h);
+    Some<T, V> r;
+    __builtin_memcpy(&r, p, sizeof(r));
+    return r;
+}
+template <typename T, int V> __device__ __forceinline__ void store_some(T* p, const Some<T, V>& r)
+{
+    if constexpr (sizeof(r) % 4 == 0)
+        store_past<sizeof(r)>(p, &r);
+    else
+        __builtin_memcpy(p, &r, sizeof(r));
 }
 
-template <typename T> __global__ __launch_bounds__(256) void ctc_recurrence_backward_kernel(RecurrenceArgs p)
+// A run's map, in fp64: P is the product of hundreds of numbers that may all be nearly one.
+struct Map {
+    double keep, add;
+};
+
+// The number itself, of which nothing worked out before is known any more: it is converted again where it is used again, in place of being kept
+// in fp64 over a barrier in twice the registers.
+__device__ __forceinline__ void forget(float& v) { asm("" : "+v"(v)); }
+
+enum class Part { kWhole, kSummary, kStretch };
+
+// What of the grid a workgroup is: a tile of channels of one direction, an utterance, a stretch of its frames.  Workgroups are dealt out to the eight dies
+// in turn; each die's take neighbouring tiles of all utterances, so that lines of memory that two tiles share are in one die's cache, and
+// each die has its share of the long utterances.
+struct Place {
+    int b, k, stretch, steps;           // k: this lane's first channel; steps of the utterance
+    bool backwards, mine;               // in time; whether the lane has channels that no lane before it has
+};
+template <int V> __device__ __forceinline__ bool place_of(const RecurrenceArgs& p, int64_t groups, Place& at)
 {
-    const int64_t i = group_number() * 256 + threadIdx.x;
-    if (i >= static_cast<int64_t>(p.B) * p.H) return;
-    const int b = static_cast<int>(i / p.H), k = static_cast<int>(i % p.H), n = length_of(p.lengths, b, p.T);
-    double d = p.dfinal ? static_cast<double>(p.dfinal[i]) : 0.0;
-    for (int s = n - 1; s >= 0; --s) {
-        const int64_t row = static_cast<int64_t>(k < p.forward ? s : n - 1 - s) * p.B + b;
-        const int64_t before = row + (k < p.forward ? -p.B : p.B);
-        const T* in = static_cast<const T*>(p.inputs) + row * p.pitch + k;
-        const Gate g = gate_of(widen(in[0]));
-        const float h = s ? widen(static_cast<const T*>(p.states_in)[before * p.H + k]) : p.initial ? p.initial[i] : 0.0f;
-        d += static_cast<double>(widen(static_cast<const T*>(p.dstates)[row * p.H + k]));
-        const float whole = static_cast<float>(d);
-        T* out = static_cast<T*>(p.out) + row * p.pitch + k;
-        out[0] = narrow<T>(whole * (widen(in[p.H]) - h) * (g.z * g.stays));
-        out[p.H] = narrow<T>(whole * g.z);
-        d *= 1.0 - static_cast<double>(g.z);
+    constexpr int kTile = kWave * V;
+    const int64_t per_die = (groups + 7) / 8, number = group_number();
+    if (number / 8 >= per_die) return false;
+    const int64_t i = number % 8 * per_die + number / 8;
+    if (i >= groups) return false;
+    const int tiles_forward = (p.forward + kTile - 1) / kTile;
+    at.b = static_cast<int>(i % p.B);
+    const int64_t rest = i / p.B;
+    at.stretch = static_cast<int>(rest % p.stretches);
+    int tile = static_cast<int>(rest / p.stretches);
+    at.backwards = tile >= tiles_forward;
+    if (at.backwards) tile -= tiles_forward;
+    const int first = at.backwards ? p.forward : 0, end = at.backwards ? p.H : p.forward;
+    const int k = first + tile * kTile + static_cast<int>(threadIdx.x % kWave) * V;
+    at.mine = k < end;
+    at.k = k + V <= end ? k : end - V;          // (a direction's channels are at least V: a lane at its end takes some that another lane has too)
+    at.steps = length_of(p.lengths, at.b, p.T);
+    return true;
+}
+
+// The maps of this workgroup's wavefronts in order, applied to the state before them all: `before` becomes that before this wavefront's, `carry` that behind
+// the last.  Two buffers by turns: who writes one again has passed the barrier that its readers of the round before came to.
+template <int V, int WAVES>
+__device__ __forceinline__ void through_waves(Map (*s_map)[V][kWave], const Map (&mine)[V], int lane, int wave, double (&carry)[V], double (&before)[V])
+{
+    if constexpr (WAVES == 1) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            before[v] = carry[v];
+            carry[v] = fma(mine[v].keep, carry[v], mine[v].add);
+        }
+        return;
     }
-    if (p.last) p.last[i] = static_cast<float>(d);
+#pragma unroll
+    for (int v = 0; v < V; ++v) s_map[wave][v][lane] = mine[v];
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            if (w == wave) before[v] = carry[v];
+            const Map m = s_map[w][v][lane];
+            carry[v] = fma(m.keep, carry[v], m.add);
+        }
+    }
+}
+
+// The state before this stretch: the initial one through the maps of the stretches before, a share of which each wavefront puts together.
+template <int V, int WAVES>
+__device__ __forceinline__ void through_stretches(const RecurrenceArgs& p, const Place& at, Map (*s_map)[V][kWave], int lane, int wave, double (&carry)[V])
+{
+    const int64_t channels = static_cast<int64_t>(p.B) * p.H, here = static_cast<int64_t>(at.b) * p.H + at.k;
+    const Map* const maps = reinterpret_cast<const Map*>(p.workspace);
+    const int share = (at.stretch + WAVES - 1) / WAVES, first = wave * share, last = first + share < at.stretch ? first + share : at.stretch;
+    Map m[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        m[v] = {1.0, 0.0};
+        carry[v] = maps[here + v].add;
+    }
+#pragma unroll 4
+    for (int j = first; j < last; ++j)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const Map o = maps[(1 + j) * channels + here + v];
+            m[v].add = fma(o.keep, m[v].add, o.add);
+            m[v].keep *= o.keep;
+        }
+    double before[V];
+    through_waves<V, WAVES>(s_map, m, lane, wave, carry, before);
+    if constexpr (WAVES > 1) __syncthreads();                   // (the rounds begin with the same buffer)
+}
+
+template <int V> __device__ __forceinline__ void carry_from(const float* initial, int64_t at, double (&carry)[V])
+{
+#pragma unroll
+    for (int v = 0; v < V; ++v) carry[v] = initial ? static_cast<double>(initial[at + v]) : 0.0;
+}
+
+// What a summary leaves: the stretch's map, and (the first stretch's) the initial state, which the last's `last` may overwrite.
+template <int V> __device__ __forceinline__ void leave_map(const RecurrenceArgs& p, const Place& at, const float* initial, const Map (&m)[V])
+{
+    const int64_t channels = static_cast<int64_t>(p.B) * p.H, here = static_cast<int64_t>(at.b) * p.H + at.k;
+    Map* const maps = reinterpret_cast<Map*>(p.workspace);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        maps[(1 + at.stretch) * channels + here + v] = m[v];
+        if (at.stretch == 0) maps[here + v] = {0.0, initial ? static_cast<double>(initial[here + v]) : 0.0};
+    }
+}
+
+// Rounds of WAVES runs of RUN frames.  BACK: the gradient, whose steps are an utterance's in the other order.
+template <typename T, int V, int RUN, int WAVES, Part PART, bool BACK>
+__global__ __launch_bounds__(WAVES * kWave) void ctc_recurrence_kernel(RecurrenceArgs p, int64_t groups)
+{
+    __shared__ Map s_map[WAVES > 1 ? 2 : 1][WAVES][V][kWave];
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    Place at;
+    if (!place_of<V>(p, groups, at)) return;
+    const int64_t channel = static_cast<int64_t>(at.b) * p.H + at.k;
+    const float* const before_all = BACK ? p.dfinal : p.initial;
+    const int begin = PART == Part::kWhole ? 0 : static_cast<int>(static_cast<int64_t>(at.stretch) * p.stretch_steps < at.steps ? at.stretch * p.stretch_steps : at.steps);
+    const int end = PART == Part::kWhole ? at.steps : at.steps - begin < p.stretch_steps ? at.steps : begin + p.stretch_steps;
+    double carry[V], before[V];
+    float initial[V];
+    if constexpr (BACK && PART != Part::kSummary) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) initial[v] = p.initial ? p.initial[channel + v] : 0.0f;
+    }
+    Map all[V];
+    if constexpr (PART == Part::kStretch)
+        through_stretches<V, WAVES>(p, at, s_map[0], lane, wave, carry);
+    else if constexpr (PART == Part::kWhole)
+        carry_from<V>(before_all, channel, carry);
+    else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            carry[v] = 0.0;
+            all[v] = {1.0, 0.0};
+        }
+    }
+    int turn = 0;
+    for (int round = begin; round < end; round += WAVES * RUN) {
+        const int first = round + wave * RUN;
+        Some<T, V> g[RUN], c[RUN], d[RUN], h[RUN];
+#pragma unroll
+        for (int i = 0; i < RUN; ++i) {
+            // (steps behind the end: the last one again, with a gate that leaves all as it was)
+            int s = first + i < end ? first + i : end - 1;
+            if (BACK) s = at.steps - 1 - s;                                       // in the channel's own order
+            const int64_t t = at.backwards ? at.steps - 1 - s : s, row = t * p.B + at.b;
+            const T* const in = static_cast<const T*>(p.inputs) + row * p.pitch;
+            g[i] = load_some<T, V>(in + at.k);
+            if constexpr (!BACK || PART != Part::kSummary) c[i] = load_some<T, V>(in + p.H + at.k);
+            if constexpr (BACK) {
+                d[i] = load_some<T, V>(static_cast<const T*>(p.dstates) + row * p.H + at.k);
+                if constexpr (PART != Part::kSummary) {
+                    const int64_t ahead = s == 0 ? 0 : at.backwards ? p.B : -p.B;
+                    h[i] = load_some<T, V>(static_cast<const T*>(p.states_in) + (row + ahead) * p.H + at.k);
+                }
+            }
+        }
+        float z[RUN][V], slope[RUN][V];
+        Map run[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) run[v] = {1.0, 0.0};
+#pragma unroll
+        for (int i = 0; i < RUN; ++i)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const Gate gate = gate_of(widen(g[i].v[v]));
+                z[i][v] = first + i < end ? gate.z : 0.0f;
+                if constexpr (BACK && PART != Part::kSummary) {
+                    const float was = BACK && at.steps - 1 - (first + i) == 0 ? initial[v] : widen(h[i].v[v]);
+                    slope[i][v] = (widen(c[i].v[v]) - was) * (gate.z * gate.stays);
+                }
+                const double zd = static_cast<double>(z[i][v]);
+                if constexpr (BACK) {
+                    const double whole = run[v].add + static_cast<double>(first + i < end ? widen(d[i].v[v]) : 0.0f);
+                    run[v].add = fma(-zd, whole, whole);
+                } else {
+                    run[v].add = fma(zd, static_cast<double>(widen(c[i].v[v])) - run[v].add, run[v].add);
+                }
+                run[v].keep = fma(-zd, run[v].keep, run[v].keep);
+            }
+        through_waves<V, WAVES>(s_map[turn], run, lane, wave, carry, before);
+        if constexpr (WAVES > 1) turn ^= 1;
+        if constexpr (PART == Part::kSummary) {
+            // (the carry of a summary begins with zero; the product is every wavefront's own to keep)
+#pragma unroll
+            for (int v = 0; v < V; ++v) all[v].keep *= run[v].keep;
+            continue;
+        }
+#pragma unroll
+        for (int i = 0; i < RUN; ++i) {
+            if (first + i >= end) break;
+            int s = first + i;
+            if (BACK) s = at.steps - 1 - s;
+            const int64_t t = at.backwards ? at.steps - 1 - s : s, row = t * p.B + at.b;
+            Some<T, V> out, more;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                forget(z[i][v]);
+                const double zd = static_cast<double>(z[i][v]);
+                if constexpr (BACK) {
+                    float here = widen(d[i].v[v]);
+                    forget(here);
+                    const double whole = before[v] + static_cast<double>(here);
+                    const float w = static_cast<float>(whole);
+                    out.v[v] = narrow<T>(w * slope[i][v]);
+                    more.v[v] = narrow<T>(w * z[i][v]);
+                    before[v] = fma(-zd, whole, whole);
+                } else {
+                    float here = widen(c[i].v[v]);
+                    forget(here);
+                    before[v] = fma(zd, static_cast<double>(here) - before[v], before[v]);
+                    out.v[v] = narrow<T>(static_cast<float>(before[v]));
+                }
+            }
+            if (!at.mine) continue;
+            if constexpr (BACK) {
+                T* const to = static_cast<T*>(p.out) + row * p.pitch + at.k;
+                store_some<T, V>(to, out);
+                store_some<T, V>(to + p.H, more);
+            } else {
+                store_some<T, V>(static_cast<T*>(p.out) + row * p.H + at.k, out);
+            }
+        }
+    }
+    if constexpr (PART == Part::kSummary) {
+        // The stretch's product: the wavefronts' own, multiplied.
+        if constexpr (WAVES > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int v = 0; v < V; ++v) s_map[0][wave][v][lane] = all[v];
+            __syncthreads();
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                all[v].keep = 1.0;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) all[v].keep *= s_map[0][w][v][lane].keep;
+            }
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) all[v].add = carry[v];
+        if (wave == 0) leave_map<V>(p, at, before_all, all);
+        return;
+    }
+    if (wave == 0 && p.last && at.mine && (PART == Part::kWhole || at.stretch == p.stretches - 1)) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) p.last[channel + v] = static_cast<float>(carry[v]);
+    }
+}
+
+template <typename T, int V, int RUN, int WAVES, Part PART, bool BACK> int launch_part(RecurrenceArgs p, int64_t tiles, hipStream_t s)
+{
+    if (PART == Part::kSummary) --p.stretches;                  // (nobody asks for the last one's)
+    const int64_t groups = tiles * p.B * p.stretches;
+    return launch(ctc_recurrence_kernel<T, V, RUN, WAVES, PART, BACK>, spread(blocks(groups, 8) * 8), WAVES * kWave, s, p, groups);
+}
+
+template <typename T, int V, bool BACK> int launch_channels(RecurrenceArgs p, hipStream_t s)
+{
+    constexpr int kTile = kWave * V, kFrames = BACK ? kRunBack : kRun;
+    const int64_t tiles = (p.forward + kTile - 1) / kTile + (p.H - p.forward + kTile - 1) / kTile;
+    const RecurrencePlan plan = recurrence_plan(p.T, tiles * p.B, kFrames);
+    p.stretches = plan.stretches;
+    p.stretch_steps = plan.steps;
+    if (plan.waves == 1) return launch_part<T, V, kFrames, 1, Part::kWhole, BACK>(p, tiles, s);
+    if (plan.stretches == 1) return launch_part<T, V, kFrames, kRecurrenceWaves, Part::kWhole, BACK>(p, tiles, s);
+    const int err = launch_part<T, V, kFrames, kRecurrenceWaves, Part::kSummary, BACK>(p, tiles, s);
+    return err ? err : launch_part<T, V, kFrames, kRecurrenceWaves, Part::kStretch, BACK>(p, tiles, s);
+}
+
+template <typename T, bool BACK> int launch_of(const RecurrenceArgs& p, hipStream_t s)
+{
+    const int back = p.H - p.forward;
+    const bool two = (p.forward == 0 || p.forward >= 2) && (back == 0 || back >= 2);
+    return two ? launch_channels<T, 2, BACK>(p, s) : launch_channels<T, 1, BACK>(p, s);
 }
 
 }  // namespace
@@ -59,9 +330,8 @@ template <typename T> __global__ __launch_bounds__(256) void ctc_recurrence_back
 int launch_recurrence(const RecurrenceArgs& p, bool bf16, bool backward, void* stream)
 {
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const dim3 grid = spread(blocks(static_cast<int64_t>(p.B) * p.H, 256));
-    if (backward) return bf16 ? launch(ctc_recurrence_backward_kernel<bf16_t>, grid, 256, s, p) : launch(ctc_recurrence_backward_kernel<float>, grid, 256, s, p);
-    return bf16 ? launch(ctc_recurrence_kernel<bf16_t>, grid, 256, s, p) : launch(ctc_recurrence_kernel<float>, grid, 256, s, p);
+    if (backward) return bf16 ? launch_of<bf16_t, true>(p, s) : launch_of<float, true>(p, s);
+    return bf16 ? launch_of<bf16_t, false>(p, s) : launch_of<float, false>(p, s);
 }
 
 }  // namespace layer
