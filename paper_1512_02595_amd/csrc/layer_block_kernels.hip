@@ -84,7 +84,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void ctc_block_no
             float y = widen(x[k / kE].v[k % kE]) * f * after[k];
             if (p.gate) {
                 const float gate = widen(g[k / kE].v[k % kE]);
-                y *= gate * gate_of(gate).z;
+                y *= gate * share_of<sizeof(T) == 4>(gate);
             }
             const T rounded = narrow<T>(y + widen(z[k / kE].v[k % kE]));
             z[k / kE].v[k % kE] = rounded;
@@ -171,7 +171,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void ctc_block_no
             const float normed = xk * f1;
             if (p.gate) {
                 const float gate = widen(g[k / kE].v[k % kE]);
-                const Gate s = gate_of(gate);
+                const Gate s = gate_of<sizeof(T) == 4>(gate);
                 a = gate * s.z;
                 g[k / kE].v[k % kE] = narrow<T>(d * after[k] * normed * (s.z + a * s.stays));
             }
@@ -300,7 +300,7 @@ template <typename T> __global__ __launch_bounds__(1024) void ctc_block_norm_bac
                         const float normed = xk * f1;
                         if (p.gate) {
                             const float gate = widen(g.v[v + j]);
-                            const Gate s = gate_of(gate);
+                            const Gate s = gate_of<sizeof(T) == 4>(gate);
                             a = gate * s.z;
                             g.v[v + j] = narrow<T>(d * after * normed * (s.z + a * s.stays));
                         }

@@ -7,23 +7,33 @@
 namespace layer {
 namespace {
 
-// z = 1 / (1 + exp(-g)) and 1 - z, each to a few units of its own last place: from exp(-|g|), which does not overflow, both
-// are a quotient without a difference.  The exponent is a product in two parts, so that it is good to a last place of the
-// result, not of itself.  An infinite g gives 0 and 1, a NaN NaNs.
+// z = 1 / (1 + exp(-g)), 1 - z and their product, each to a few units of its own last place: from t = exp(-|g|), which does not overflow, all are
+// quotients without a difference.  An infinite g gives 0 and 1, a NaN NaNs.  The exponent is a product; its rounding would be an error of |g| half
+// steps of t, so for FINE, where results are in 32 bits, the rest that the product leaves is made good (five operations more).
 struct Gate {
-    float z, stays;
+    float z, stays, both;
 };
-__device__ __forceinline__ Gate gate_of(float g)
+constexpr float kLog2e = 0x1.715476p+0f, kLog2eRest = 0x1.4ae0cp-26f, kLn2 = 0x1.62e430p-1f;
+template <bool FINE> __device__ __forceinline__ float exp_of_minus(float a)             // a >= 0, or a NaN
 {
-    constexpr float kLog2e = 0x1.715476p+0f, kRest = 0x1.4ae0cp-26f, kLn2 = 0x1.62e430p-1f;
-    float a = fabsf(g);
+    if constexpr (!FINE) return __builtin_amdgcn_exp2f(-a * kLog2e);
     a = a > 150.0f ? 150.0f : a;                                        // (exp(-150) is 0 here; an infinity would make the rest a NaN)
-    const float whole = -a * kLog2e, rest = fmaf(-a, kLog2e, -whole) - a * kRest;
+    const float whole = -a * kLog2e, rest = fmaf(-a, kLog2eRest, fmaf(-a, kLog2e, -whole));
     const float power = __builtin_amdgcn_exp2f(whole);
-    const float t = fmaf(power, rest * kLn2, power);                    // exp(-|g|)
+    return fmaf(power, rest * kLn2, power);
+}
+template <bool FINE> __device__ __forceinline__ Gate gate_of(float g)
+{
+    const float t = exp_of_minus<FINE>(fabsf(g));
     const float large = __builtin_amdgcn_rcpf(1.0f + t), small = t * large;
     const bool up = g >= 0.0f;
-    return {up ? large : small, up ? small : large};
+    return {up ? large : small, up ? small : large, large * small};
+}
+// z alone.
+template <bool FINE> __device__ __forceinline__ float share_of(float g)
+{
+    if constexpr (FINE) return gate_of<true>(g).z;
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-g * kLog2e));
 }
 
 }  // namespace

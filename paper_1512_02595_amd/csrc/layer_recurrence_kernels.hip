@@ -30,18 +30,18 @@ __device__ __forceinline__ int length_of(const int32_t* lengths, int b, int T)
 template <typename T, int V> struct Some {
     T v[V];
 };
-template <typename T, int V> __device__ __forceinline__ Some<T, V> load_some(const T* p)
+template <typename T, int V> __device__ __forceinline__ Some<T, V> load_some(const char* row, uint32_t at)
 {
     Some<T, V> r;
-    __builtin_memcpy(&r, p, sizeof(r));
+    __builtin_memcpy(&r, row + at, sizeof(r));
     return r;
 }
-template <typename T, int V> __device__ __forceinline__ void store_some(T* p, const Some<T, V>& r)
+template <typename T, int V> __device__ __forceinline__ void store_some(char* row, uint32_t at, const Some<T, V>& r)
 {
     if constexpr (sizeof(r) % 4 == 0)
-        store_past<sizeof(r)>(p, &r);
+        store_past<sizeof(r)>(row + at, &r);
     else
-        __builtin_memcpy(p, &r, sizeof(r));
+        __builtin_memcpy(row + at, &r, sizeof(r));
 }
 
 // A run's map, in fp64: P is the product of hundreds of numbers that may all be nearly one.
@@ -53,6 +53,15 @@ struct Map {
 // in fp64 over a barrier in twice the registers.
 __device__ __forceinline__ void forget(float& v) { asm("" : "+v"(v)); }
 
+// To fp32, and from there on a number in fp32: the compiler would take this rounding and the one to bf16 behind it for one, which it works out in eight
+// operations more.
+__device__ __forceinline__ float once(double v)
+{
+    float f = static_cast<float>(v);
+    forget(f);
+    return f;
+}
+
 enum class Part { kWhole, kSummary, kStretch };
 
 // What of the grid a workgroup is: a tile of channels of one direction, an utterance, a stretch of its frames.  Workgroups are dealt out to the eight dies
@@ -61,26 +70,28 @@ enum class Part { kWhole, kSummary, kStretch };
 struct Place {
     int b, k, stretch, steps;           // k: this lane's first channel; steps of the utterance
     bool backwards, mine;               // in time; whether the lane has channels that no lane before it has
+
+    __device__ __forceinline__ int64_t row(int step, int B) const { return static_cast<int64_t>(backwards ? steps - 1 - step : step) * B + b; }
 };
-template <int V> __device__ __forceinline__ bool place_of(const RecurrenceArgs& p, int64_t groups, Place& at)
+template <int V> __device__ __forceinline__ bool place_of(const RecurrenceArgs& p, unsigned groups, Place& at)
 {
     constexpr int kTile = kWave * V;
-    const int64_t per_die = (groups + 7) / 8, number = group_number();
+    const unsigned per_die = (groups + 7) / 8, number = static_cast<unsigned>(group_number());
     if (number / 8 >= per_die) return false;
-    const int64_t i = number % 8 * per_die + number / 8;
+    const unsigned i = number % 8 * per_die + number / 8;
     if (i >= groups) return false;
     const int tiles_forward = (p.forward + kTile - 1) / kTile;
-    at.b = static_cast<int>(i % p.B);
-    const int64_t rest = i / p.B;
-    at.stretch = static_cast<int>(rest % p.stretches);
-    int tile = static_cast<int>(rest / p.stretches);
+    const unsigned B = static_cast<unsigned>(p.B), stretches = static_cast<unsigned>(p.stretches), rest = i / B;
+    at.b = static_cast<int>(i % B);
+    at.stretch = static_cast<int>(rest % stretches);
+    int tile = static_cast<int>(rest / stretches);
     at.backwards = tile >= tiles_forward;
     if (at.backwards) tile -= tiles_forward;
     const int first = at.backwards ? p.forward : 0, end = at.backwards ? p.H : p.forward;
     const int k = first + tile * kTile + static_cast<int>(threadIdx.x % kWave) * V;
     at.mine = k < end;
     at.k = k + V <= end ? k : end - V;          // (a direction's channels are at least V: a lane at its end takes some that another lane has too)
-    at.steps = length_of(p.lengths, at.b, p.T);
+    at.steps = __builtin_amdgcn_readfirstlane(length_of(p.lengths, at.b, p.T));
     return true;
 }
 
@@ -157,7 +168,7 @@ template <int V> __device__ __forceinline__ void leave_map(const RecurrenceArgs&
 
 // Rounds of WAVES runs of RUN frames.  BACK: the gradient, whose steps are an utterance's in the other order.
 template <typename T, int V, int RUN, int WAVES, Part PART, bool BACK>
-__global__ __launch_bounds__(WAVES * kWave) void ctc_recurrence_kernel(RecurrenceArgs p, int64_t groups)
+__global__ __launch_bounds__(WAVES * kWave) void ctc_recurrence_kernel(RecurrenceArgs p, unsigned groups)
 {
     __shared__ Map s_map[WAVES > 1 ? 2 : 1][WAVES][V][kWave];
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -185,27 +196,50 @@ __global__ __launch_bounds__(WAVES * kWave) void ctc_recurrence_kernel(Recurrenc
             all[v] = {1.0, 0.0};
         }
     }
+    // Bytes from a step's row to that of the kernel's next step, rows of the inputs and of states; a row's begin is the same for all lanes.
+    constexpr bool kFine = sizeof(T) == 4;
+    const int64_t row_bytes = p.pitch * static_cast<int64_t>(sizeof(T)), state_bytes = static_cast<int64_t>(p.H) * sizeof(T);
+    const int64_t hop_rows = at.backwards != BACK ? -p.B : p.B, hop = hop_rows * row_bytes, hop_states = hop_rows * state_bytes;
+    const uint32_t at_gate = static_cast<uint32_t>(at.k) * sizeof(T), at_candidate = static_cast<uint32_t>(p.H + at.k) * sizeof(T);
     int turn = 0;
     for (int round = begin; round < end; round += WAVES * RUN) {
         const int first = round + wave * RUN;
         Some<T, V> g[RUN], c[RUN], d[RUN], h[RUN];
+        const bool full = first + RUN <= end && (!BACK || first + RUN < at.steps);
+        const int64_t row = at.row(BACK ? at.steps - 1 - (first < end ? first : end - 1) : first < end ? first : end - 1, p.B);
+        const char* in = static_cast<const char*>(p.inputs) + row * row_bytes;
+        const char* grad = static_cast<const char*>(p.dstates) + row * state_bytes;
+        const char* held = static_cast<const char*>(p.states_in) + row * state_bytes;
+        const auto bring = [&](int i) {
+            g[i] = load_some<T, V>(in, at_gate);
+            if constexpr (!BACK || PART != Part::kSummary) c[i] = load_some<T, V>(in, at_candidate);
+            if constexpr (BACK) d[i] = load_some<T, V>(grad, at_gate);
+            if constexpr (BACK && PART != Part::kSummary) h[i] = load_some<T, V>(held, at_gate);
+        };
+        if (full) {
+            held += hop_states;
 #pragma unroll
-        for (int i = 0; i < RUN; ++i) {
-            // (steps behind the end: the last one again, with a gate that leaves all as it was)
-            int s = first + i < end ? first + i : end - 1;
-            if (BACK) s = at.steps - 1 - s;                                       // in the channel's own order
-            const int64_t t = at.backwards ? at.steps - 1 - s : s, row = t * p.B + at.b;
-            const T* const in = static_cast<const T*>(p.inputs) + row * p.pitch;
-            g[i] = load_some<T, V>(in + at.k);
-            if constexpr (!BACK || PART != Part::kSummary) c[i] = load_some<T, V>(in + p.H + at.k);
-            if constexpr (BACK) {
-                d[i] = load_some<T, V>(static_cast<const T*>(p.dstates) + row * p.H + at.k);
-                if constexpr (PART != Part::kSummary) {
-                    const int64_t ahead = s == 0 ? 0 : at.backwards ? p.B : -p.B;
-                    h[i] = load_some<T, V>(static_cast<const T*>(p.states_in) + (row + ahead) * p.H + at.k);
-                }
+            for (int i = 0; i < RUN; ++i) {
+                bring(i);
+                in += hop;
+                grad += hop_states;
+                held += hop_states;
+            }
+        } else {
+            // Steps behind the end: the last one again, with a gate that leaves all as it was.  (The gradient's last step has no frame before it; what is
+            // read in its place is not used.)
+            held += first + 1 < at.steps ? hop_states : 0;
+#pragma unroll
+            for (int i = 0; i < RUN; ++i) {
+                bring(i);
+                in += first + i + 1 < end ? hop : 0;
+                grad += first + i + 1 < end ? hop_states : 0;
+                held += first + i + 1 < end && first + i + 2 < at.steps ? hop_states : 0;
             }
         }
+        // All of a run is asked for before any of it is waited for.
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
         float z[RUN][V], slope[RUN][V];
         Map run[V];
 #pragma unroll
@@ -214,12 +248,14 @@ __global__ __launch_bounds__(WAVES * kWave) void ctc_recurrence_kernel(Recurrenc
         for (int i = 0; i < RUN; ++i)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const Gate gate = gate_of(widen(g[i].v[v]));
-                z[i][v] = first + i < end ? gate.z : 0.0f;
                 if constexpr (BACK && PART != Part::kSummary) {
-                    const float was = BACK && at.steps - 1 - (first + i) == 0 ? initial[v] : widen(h[i].v[v]);
-                    slope[i][v] = (widen(c[i].v[v]) - was) * (gate.z * gate.stays);
+                    const Gate gate = gate_of<kFine>(widen(g[i].v[v]));
+                    z[i][v] = gate.z;
+                    slope[i][v] = (widen(c[i].v[v]) - (first + i < at.steps - 1 ? widen(h[i].v[v]) : initial[v])) * gate.both;
+                } else {
+                    z[i][v] = share_of<kFine>(widen(g[i].v[v]));
                 }
+                if (first + i >= end) z[i][v] = 0.0f;
                 const double zd = static_cast<double>(z[i][v]);
                 if constexpr (BACK) {
                     const double whole = run[v].add + static_cast<double>(first + i < end ? widen(d[i].v[v]) : 0.0f);
@@ -238,39 +274,38 @@ __global__ __launch_bounds__(WAVES * kWave) void ctc_recurrence_kernel(Recurrenc
             continue;
         }
 #pragma unroll
-        for (int i = 0; i < RUN; ++i) {
-            if (first + i >= end) break;
-            int s = first + i;
-            if (BACK) s = at.steps - 1 - s;
-            const int64_t t = at.backwards ? at.steps - 1 - s : s, row = t * p.B + at.b;
-            Some<T, V> out, more;
+        for (int i = 0; i < RUN; ++i)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 forget(z[i][v]);
                 const double zd = static_cast<double>(z[i][v]);
+                float here = widen(BACK ? d[i].v[v] : c[i].v[v]);
+                forget(here);
                 if constexpr (BACK) {
-                    float here = widen(d[i].v[v]);
-                    forget(here);
                     const double whole = before[v] + static_cast<double>(here);
-                    const float w = static_cast<float>(whole);
-                    out.v[v] = narrow<T>(w * slope[i][v]);
-                    more.v[v] = narrow<T>(w * z[i][v]);
+                    const float w = once(whole);
+                    g[i].v[v] = narrow<T>(w * slope[i][v]);
+                    c[i].v[v] = narrow<T>(w * z[i][v]);
                     before[v] = fma(-zd, whole, whole);
                 } else {
-                    float here = widen(c[i].v[v]);
-                    forget(here);
                     before[v] = fma(zd, static_cast<double>(here) - before[v], before[v]);
-                    out.v[v] = narrow<T>(static_cast<float>(before[v]));
+                    g[i].v[v] = narrow<T>(once(before[v]));
                 }
             }
-            if (!at.mine) continue;
-            if constexpr (BACK) {
-                T* const to = static_cast<T*>(p.out) + row * p.pitch + at.k;
-                store_some<T, V>(to, out);
-                store_some<T, V>(to + p.H, more);
-            } else {
-                store_some<T, V>(static_cast<T*>(p.out) + row * p.H + at.k, out);
-            }
+        char* to = static_cast<char*>(p.out) + row * (BACK ? row_bytes : state_bytes);
+        const auto write = [&](int i) {
+            store_some<T, V>(to, at_gate, g[i]);
+            if constexpr (BACK) store_some<T, V>(to, at_candidate, c[i]);
+            to += BACK ? hop : hop_states;
+        };
+        if (!at.mine) {
+        } else if (full) {
+#pragma unroll
+            for (int i = 0; i < RUN; ++i) write(i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < RUN; ++i)
+                if (first + i < end) write(i);
         }
     }
     if constexpr (PART == Part::kSummary) {
@@ -301,7 +336,7 @@ __global__ __launch_bounds__(WAVES * kWave) void ctc_recurrence_kernel(Recurrenc
 template <typename T, int V, int RUN, int WAVES, Part PART, bool BACK> int launch_part(RecurrenceArgs p, int64_t tiles, hipStream_t s)
 {
     if (PART == Part::kSummary) --p.stretches;                  // (nobody asks for the last one's)
-    const int64_t groups = tiles * p.B * p.stretches;
+    const unsigned groups = static_cast<unsigned>(tiles * p.B * p.stretches);         // (at most 257 tiles by 65535 utterances: stretches come where places are few)
     return launch(ctc_recurrence_kernel<T, V, RUN, WAVES, PART, BACK>, spread(blocks(groups, 8) * 8), WAVES * kWave, s, p, groups);
 }
 

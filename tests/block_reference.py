@@ -8,9 +8,14 @@ import torch
 
 from layer_reference import HALF
 
-# z and 1 - z: an exponential good to a unit in the last place (two half steps) and a half for each of two operations that correct
+# z, 1 - z and their product: an exponential good to a unit in the last place (two half steps) and a half for each of two operations that correct
 # it, a sum, a reciprocal good to a unit, a product, and the exponent's second part (1.5 half steps at most).
+# Where results are in 16 bits the exponent's second part is left out: the product's rounding is an error of |g| half steps.
 GATE = 9 * HALF
+
+
+def gate_error(g, fine):
+    return GATE + (0.0 if fine else HALF) * g.double().abs()
 
 
 def sigmoid(g):
@@ -28,13 +33,14 @@ def turned(x, lengths, forward):
     return out
 
 
-def recurrence(gates, candidates, initial, lengths, forward):
+def recurrence(gates, candidates, initial, lengths, forward, fine):
     """(states [T, B, H], final [B, H], bound on either's error but for the rounding that stores it)."""
     T, B, H = gates.shape
+    slack = gate_error(gates, fine).amax(0)
     z, _ = sigmoid(turned(gates.double(), lengths, forward))
     c = turned(candidates.double(), lengths, forward)
     h = torch.zeros(B, H, dtype=torch.float64) if initial is None else initial.double()
-    # |dh| <= sum_s |dz_s| |c_s - h_(s-1)| prod (1 - z) <= GATE max |c - h|: the weights z_s prod (1 - z) are at most 1 in sum
+    # |dh| <= sum_s |dz_s| |c_s - h_(s-1)| prod (1 - z) <= slack max |c - h| (slack: the largest gate's): the weights z_s prod (1 - z) are at most 1 in sum
     most = h.abs()
     for b, n in enumerate(lengths):
         if n:
@@ -46,12 +52,13 @@ def recurrence(gates, candidates, initial, lengths, forward):
         states[s] = h
     final = h
     # (2^-50: what thousands of steps in fp64 add)
-    return turned(states, lengths, forward), final, (2 * GATE + 2.0 ** -40) * most
+    return turned(states, lengths, forward), final, (2 * slack + 2.0 ** -40) * most
 
 
-def recurrence_backward(dstates, dfinal, gates, candidates, states, initial, lengths, forward):
+def recurrence_backward(dstates, dfinal, gates, candidates, states, initial, lengths, forward, fine):
     """(dgates, dcandidates, dinitial), and a bound on the error of each but for the rounding that stores it."""
     T, B, H = gates.shape
+    slack = gate_error(gates, fine).amax(0)
     z, stays = sigmoid(turned(gates.double(), lengths, forward))
     c, h, dh = (turned(t.double(), lengths, forward) for t in (candidates, states, dstates))
     begin = torch.zeros(B, H, dtype=torch.float64) if initial is None else initial.double()
@@ -67,12 +74,12 @@ def recurrence_backward(dstates, dfinal, gates, candidates, states, initial, len
         whole[s] = torch.where(there, D.abs(), 0.0)
         most = torch.where(there, torch.maximum(most, D.abs()), most)
         d = torch.where(there, D * stays[s], d)
-    # |dD| <= sum_s |dz_s| |D_s| prod (1 - z) <= GATE max |D|, then D and the factors are rounded
-    slip = GATE * most + 2.0 ** -40 * most
+    # |dD| <= sum_s |dz_s| |D_s| prod (1 - z) <= slack max |D|, then D and the factors are rounded
+    slip = slack * most + 2.0 ** -40 * most
     before = torch.cat((begin[None], h[:-1]))
-    bound_c = z * (slip + (GATE + 2 * HALF) * whole)
-    bound_g = (c - before).abs() * z * stays * (slip + (2 * GATE + 6 * HALF) * whole)
-    bound_d = slip + GATE * most
+    bound_c = z * (slip + (slack + 2 * HALF) * whole)
+    bound_g = (c - before).abs() * z * stays * (slip + (2 * slack + 6 * HALF) * whole)
+    bound_d = slip + slack * most
     return tuple(turned(t, lengths, forward) for t in (dg, dc)) + (d,) + tuple(turned(t, lengths, forward) for t in (bound_g, bound_c)) + (bound_d,)
 
 
@@ -81,7 +88,7 @@ def silu(p):
     return p * z, z + p * z * stays, z + (p * z * stays).abs()
 
 
-def block_norm(x, gate, residual, after, scale, eps):
+def block_norm(x, gate, residual, after, scale, eps, fine):
     """(z before it is rounded, bound)."""
     x = x.double()
     r = 1.0 / torch.sqrt((x * x).mean(1, keepdim=True) + eps)
@@ -89,7 +96,8 @@ def block_norm(x, gate, residual, after, scale, eps):
     term = x * r * after.double() * scale.double() * a
     res = torch.zeros_like(x) if residual is None else residual.double()
     z = term + res
-    return z, (GATE + 8 * HALF) * term.abs() + HALF * z.abs()
+    error = 0.0 if gate is None else gate_error(gate, fine)
+    return z, (error + 8 * HALF) * term.abs() + HALF * z.abs()
 
 
 def normed(z, before, eps):
@@ -99,7 +107,7 @@ def normed(z, before, eps):
     return y, 4 * HALF * y.abs()
 
 
-def block_norm_backward(dnormed, dsum, x, gate, z, after, scale, before, eps, per_group):
+def block_norm_backward(dnormed, dsum, x, gate, z, after, scale, before, eps, per_group, fine):
     """dict of gradients, and one of bounds.  `per_group`: how many rows' shares are added up in fp32."""
     zero = torch.zeros_like(x, dtype=torch.float64)
     x = x.double()
@@ -118,14 +126,15 @@ def block_norm_backward(dnormed, dsum, x, gate, z, after, scale, before, eps, pe
     c1, c1_abs = (e * x).mean(1, keepdim=True) / v1, (e_abs * x.abs()).mean(1, keepdim=True) / v1
     factor = after * scale * x * f1
     out = {"dresidual": d, "dx": (e - x * c1) * f1, "dgate": d * factor * slope}
-    D, E = 8 * HALF, GATE + 12 * HALF
-    bound = {"dresidual": D * d_abs, "dx": (E + 6 * HALF) * (e_abs + x.abs() * c1_abs) * f1,
-             "dgate": (D + 2 * GATE + 8 * HALF) * d_abs * factor.abs() * slope_abs}
+    error = 0.0 if gate is None else gate_error(gate, fine)
+    D, E = 8 * HALF, error + 12 * HALF
+    bound = {"dresidual": D * d_abs, "dx": (E + 6 * HALF) * e_abs * f1 + x.abs() * f1 * (((E + 6 * HALF) * e_abs * x.abs()).mean(1, keepdim=True) / v1 + 6 * HALF * c1_abs),
+             "dgate": (D + 2 * error + 8 * HALF) * d_abs * factor.abs() * slope_abs}
     q, q_abs = d * a * x * f1, d_abs * (a * x * f1).abs()
     w = dy * z * f2
     sums = per_group * HALF
     out.update(dweight_after=(q * scale).sum(0), dscale=(q * after).sum(0), dweight_before=w.sum(0))
-    bound.update(dweight_after=(E + 4 * HALF + sums) * (q_abs * scale.abs()).sum(0), dscale=(E + 4 * HALF + sums) * (q_abs * after.abs()).sum(0),
+    bound.update(dweight_after=((E + 4 * HALF + sums) * q_abs * scale.abs()).sum(0), dscale=((E + 4 * HALF + sums) * q_abs * after.abs()).sum(0),
                  dweight_before=(5 * HALF + sums) * w.abs().sum(0))
     return out, bound
 

@@ -73,7 +73,7 @@ def forward(c, sum_at=None, normed_at=None, want_sum=True, want_normed=True):
     block.block_norm(at(x), at(gate), c.pitch, at(residual), *map(at, c.w_dev), EPS, pointer(c.frames), c.rows, c.H, c.dtype, at(total), at(out), stream())
     torch.cuda.synchronize()
     eps = float(np.float32(EPS))
-    want, bound = ref.block_norm(c.listed(c.x), c.listed(c.gate), c.listed(c.residual), c.ones[0], c.ones[1], eps)
+    want, bound = ref.block_norm(c.listed(c.x), c.listed(c.gate), c.listed(c.residual), c.ones[0], c.ones[1], eps, c.dtype == F32)
     rest = others(c.rows, c.names)
     z = None
     if total:
@@ -139,7 +139,7 @@ def backward(c, dx_at=None, dres_at=None, use_dy=True, use_dz=True, sums=(True, 
     # (the partial sums: each workgroup's rows, and what four wavefronts add)
     per_group = -(-c.rows // min(1024, -(-c.rows // (4 if c.H <= 1024 else 2)))) + 8
     want, bound = ref.block_norm_backward(c.listed(c.dy) if use_dy else None, c.listed(c.dz) if use_dz else None, c.listed(c.x), c.listed(c.gate),
-                                          c.listed(c.z) if use_dy else None, *c.ones, float(np.float32(EPS)), per_group)
+                                          c.listed(c.z) if use_dy else None, *c.ones, float(np.float32(EPS)), per_group, c.dtype == F32)
     rest, H = others(c.rows, c.names), c.H
     outs = [("dx", dx, dx_at), ("dresidual", dres, dres_at), ("dgate", dgate, None)]
     for name, g, place in outs:

@@ -74,7 +74,7 @@ class Call:
 
     def check_forward(self):
         torch.cuda.synchronize()
-        want, final, bound = ref.recurrence(self.gates, self.candidates, self.initial, self.n, self.forward)
+        want, final, bound = ref.recurrence(self.gates, self.candidates, self.initial, self.n, self.forward, self.dtype == F32)
         got = self.states.t.cpu().double()
         tolerance = bound[None] + (HALF + half_step(self.dtype)) * (want.abs() + bound[None])
         off = ((got - want).abs() / tolerance)[self.counts]
@@ -100,7 +100,7 @@ class Call:
     def check_backward(self):
         torch.cuda.synchronize()
         dg, dc, d0, bg, bc, b0 = ref.recurrence_backward(self.dstates, self.dfinal, self.gates, self.candidates, self.states_in, self.initial,
-                                                         self.n, self.forward)
+                                                         self.n, self.forward, self.dtype == F32)
         H, got = self.H, self.dinputs.t.cpu().double()
         for name, here, want, bound in (("dgates", got[:, :, :H], dg, bg), ("dcandidates", got[:, :, H:2 * H], dc, bc)):
             tolerance = bound + (HALF + half_step(self.dtype)) * (want.abs() + bound) + 2.0 ** -140
