@@ -31,8 +31,8 @@ struct RecurrenceArgs {
     int stretches = 1, stretch_steps = 0;   // set by the launch code
 };
 
-// Frames that a wavefront has in registers at once (of the gradient, which has twice the tensors, half as many), and wavefronts that share an utterance's.
-constexpr int kRun = 16, kRunBack = 8, kRecurrenceWaves = 8;
+// Frames that a wavefront has in registers at once (of the gradient, which has twice the tensors and a slope to keep, four), and wavefronts that share an utterance's.
+constexpr int kRun = 16, kRunBack = 4, kRecurrenceWaves = 8;
 
 // How an utterance's T frames are dealt out in runs, where `places` workgroups would have one tile of channels of one utterance each: one wavefront has
 // few of them; many go in rounds to eight; and where that leaves compute units without work, they go in stretches of whole rounds to several workgroups.
@@ -43,17 +43,17 @@ inline RecurrencePlan recurrence_plan(int T, int64_t places, int run)
 {
     if (T <= run) return {1, 1, T};
     const int round = run * kRecurrenceWaves, rounds = (T - 1) / round + 1;
-    if (places >= 512 || rounds == 1) return {kRecurrenceWaves, 1, T};
-    const int64_t wanted = (1024 + places - 1) / places, most = wanted < rounds ? wanted : rounds;
+    if (places > 256 || rounds == 1) return {kRecurrenceWaves, 1, T};
+    const int64_t wanted = 512 / places, most = wanted < rounds ? wanted : rounds;
     const int each = static_cast<int>((rounds + most - 1) / most);
     return {kRecurrenceWaves, (rounds + each - 1) / each, each * round};
 }
 
 // Bytes of workspace: two numbers in fp64 for each channel of each stretch of frames, and the initial states; of more than one stretch only
-// where there are few places (at most 512 by recurrence_plan, of at most 128 channels each, and then not more than 1024 + places stretches in all), so that
-// kMostCarried is never exceeded.
+// where there are few places (by recurrence_plan at most 256, of at most 128 channels each, and then at most 512 stretches in all), so that kMostCarried is never
+// exceeded.
 constexpr int kShortestStretch = kRunBack * kRecurrenceWaves;
-constexpr int64_t kMostCarried = 3 * 1024 * 256;
+constexpr int64_t kMostCarried = (512 + 256) * 128;
 inline size_t recurrence_bytes(int T, int B, int H)
 {
     if (T <= kShortestStretch) return 0;
