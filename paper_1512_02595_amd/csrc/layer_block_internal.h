@@ -103,7 +103,7 @@ inline int block_norm_groups(int rows, int H)
 {
     const int per_group = H <= 1024 ? 4 : 2;
     const int groups = (rows + per_group - 1) / per_group;
-    return groups < 1024 ? groups : 1024;
+    return groups < 768 ? groups : 768;
 }
 
 int launch_block_norm(const BlockNormArgs& p, bool bf16, void* stream);

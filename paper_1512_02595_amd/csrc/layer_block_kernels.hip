@@ -16,12 +16,37 @@ __device__ __forceinline__ Vector<float> weights_at(const float* w, int col, int
     return {{1.0f, 1.0f, 1.0f, 1.0f}};
 }
 
+// A wavefront's sum in every lane, without LDS: lanes one and two apart, the other four of eight, the other eight of sixteen, the neighbouring sixteen, the
+// other half.  (The swap of sixteens, or halves, of a number with itself leaves the one in the first result, the other in the second.)
+template <int CONTROL> __device__ __forceinline__ double from_lane(double v)
+{
+    const uint64_t bits = __builtin_bit_cast(uint64_t, v);
+    const int low = __builtin_amdgcn_mov_dpp(static_cast<int>(bits), CONTROL, 0xf, 0xf, true);
+    const int high = __builtin_amdgcn_mov_dpp(static_cast<int>(bits >> 32), CONTROL, 0xf, 0xf, true);
+    return __builtin_bit_cast(double, static_cast<uint64_t>(static_cast<uint32_t>(high)) << 32 | static_cast<uint32_t>(low));
+}
+template <typename F> __device__ __forceinline__ double both_of(double v, F swap)
+{
+    const uint64_t bits = __builtin_bit_cast(uint64_t, v);
+    const auto low = swap(static_cast<uint32_t>(bits)), high = swap(static_cast<uint32_t>(bits >> 32));
+    return __builtin_bit_cast(double, static_cast<uint64_t>(high[0]) << 32 | low[0]) + __builtin_bit_cast(double, static_cast<uint64_t>(high[1]) << 32 | low[1]);
+}
+__device__ __forceinline__ double lanes_sum(double v)
+{
+    v += from_lane<0xB1>(v);                        // quad_perm 1 0 3 2
+    v += from_lane<0x4E>(v);                        // quad_perm 2 3 0 1
+    v += from_lane<0x141>(v);                       // row_half_mirror
+    v += from_lane<0x140>(v);                       // row_mirror
+    v = both_of(v, [](uint32_t w) { return __builtin_amdgcn_permlane16_swap(w, w, false, false); });
+    return both_of(v, [](uint32_t w) { return __builtin_amdgcn_permlane32_swap(w, w, false, false); });
+}
+
 // Sums over a row's threads: a wavefront's, or those of all wavefronts of the workgroup through LDS.  `s_sums` is one of two buffers that a row's
 // reductions take by turns, so that one barrier each is enough: who writes a buffer again has passed the barrier that its readers came to.
 template <int WAVES, int N> __device__ __forceinline__ void row_sums(double (&v)[N], double (*s_sums)[WAVES], int lane, int wave)
 {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
+    for (int i = 0; i < N; ++i) v[i] = lanes_sum(v[i]);
     if constexpr (WAVES > 1) {
         if (lane == 0)
 #pragma unroll
@@ -364,7 +389,7 @@ template <typename T> int launch_norm_of(const BlockNormArgs& p, hipStream_t s)
 {
     const int per_group = p.H <= 1024 ? 4 : 1;
     const int64_t groups = (static_cast<int64_t>(p.rows) + per_group - 1) / per_group;
-    const dim3 grid(static_cast<unsigned>(groups < 2048 ? groups : 2048));
+    const dim3 grid(static_cast<unsigned>(groups < 8192 ? groups : 8192));
     if (p.H <= 512) return launch(ctc_block_norm_kernel<T, 1, 8>, grid, 256, s, p);
     if (p.H <= 1024) return launch(ctc_block_norm_kernel<T, 1, 16>, grid, 256, s, p);
     if (p.H <= 2048) return launch(ctc_block_norm_kernel<T, 4, 8>, grid, 256, s, p);
