@@ -2,12 +2,33 @@
 
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "layer_block_internal.h"
 #include "layer_gate.h"
 #include "layer_rows.h"
 
 namespace layer {
 namespace {
+
+// load_vector, but that a row's last lane waits for no more than the others: where a vector reaches over the row's end it is the row's last one, shifted.  (Its
+// elements one by one: 10000 x 2500 bf16 97 us, backward 199.)
+template <typename T> __device__ __forceinline__ Vector<T> load_row(const T* row, int col, int H)
+{
+    constexpr int kE = Vector<T>::kElements;
+    if (sizeof(T) == 4 || H < kE) return load_vector(row, col, H);      // (four elements one by one cost nothing: 12506 x 1999 fp32 98 us, 6250 x 2000 94)
+    const int from = col + kE <= H ? col : H - kE;
+    Vector<T> r = load_whole(row + from);
+    if (from != col) {
+        const unsigned bits = static_cast<unsigned>(col - from) * (8 * sizeof(T));
+        uint64_t w[2];
+        __builtin_memcpy(w, &r, 16);
+        w[0] = bits < 64 ? w[0] >> bits | w[1] << 1 << (63 - bits) : bits < 128 ? w[1] >> (bits - 64) : 0;
+        w[1] = bits < 64 ? w[1] >> bits : 0;
+        __builtin_memcpy(&r, w, 16);
+    }
+    return r;
+}
 
 // Four of a weight's floats, ones where there is no weight.
 __device__ __forceinline__ Vector<float> weights_at(const float* w, int col, int H)
@@ -16,8 +37,13 @@ __device__ __forceinline__ Vector<float> weights_at(const float* w, int col, int
     return {{1.0f, 1.0f, 1.0f, 1.0f}};
 }
 
-// A wavefront's sum in every lane, without LDS: lanes one and two apart, the other four of eight, the other eight of sixteen, the neighbouring sixteen, the
-// other half.  (The swap of sixteens, or halves, of a number with itself leaves the one in the first result, the other in the second.)
+// The sum over a team of LANES neighbouring lanes in each of them, without LDS: lanes one and two apart, the other four of eight, the other eight of
+// sixteen, the neighbouring sixteen, the other half.  (The swap of sixteens, or halves, of a number with itself leaves the one in the first result,
+// the other in the second.)
+template <int CONTROL> __device__ __forceinline__ float from_lane(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CONTROL, 0xf, 0xf, true));
+}
 template <int CONTROL> __device__ __forceinline__ double from_lane(double v)
 {
     const uint64_t bits = __builtin_bit_cast(uint64_t, v);
@@ -25,221 +51,307 @@ template <int CONTROL> __device__ __forceinline__ double from_lane(double v)
     const int high = __builtin_amdgcn_mov_dpp(static_cast<int>(bits >> 32), CONTROL, 0xf, 0xf, true);
     return __builtin_bit_cast(double, static_cast<uint64_t>(static_cast<uint32_t>(high)) << 32 | static_cast<uint32_t>(low));
 }
+template <typename F> __device__ __forceinline__ float both_of(float v, F swap)
+{
+    const auto w = swap(__builtin_bit_cast(uint32_t, v));
+    return __builtin_bit_cast(float, static_cast<uint32_t>(w[0])) + __builtin_bit_cast(float, static_cast<uint32_t>(w[1]));
+}
 template <typename F> __device__ __forceinline__ double both_of(double v, F swap)
 {
     const uint64_t bits = __builtin_bit_cast(uint64_t, v);
     const auto low = swap(static_cast<uint32_t>(bits)), high = swap(static_cast<uint32_t>(bits >> 32));
     return __builtin_bit_cast(double, static_cast<uint64_t>(high[0]) << 32 | low[0]) + __builtin_bit_cast(double, static_cast<uint64_t>(high[1]) << 32 | low[1]);
 }
-__device__ __forceinline__ double lanes_sum(double v)
+template <int LANES, typename V> __device__ __forceinline__ V lanes_sum(V v)
 {
     v += from_lane<0xB1>(v);                        // quad_perm 1 0 3 2
     v += from_lane<0x4E>(v);                        // quad_perm 2 3 0 1
     v += from_lane<0x141>(v);                       // row_half_mirror
-    v += from_lane<0x140>(v);                       // row_mirror
-    v = both_of(v, [](uint32_t w) { return __builtin_amdgcn_permlane16_swap(w, w, false, false); });
-    return both_of(v, [](uint32_t w) { return __builtin_amdgcn_permlane32_swap(w, w, false, false); });
+    if constexpr (LANES >= 16) v += from_lane<0x140>(v);                       // row_mirror
+    if constexpr (LANES >= 32) v = both_of(v, [](uint32_t w) { return __builtin_amdgcn_permlane16_swap(w, w, false, false); });
+    if constexpr (LANES >= 64) v = both_of(v, [](uint32_t w) { return __builtin_amdgcn_permlane32_swap(w, w, false, false); });
+    return v;
 }
 
-// Sums over a row's threads: a wavefront's, or those of all wavefronts of the workgroup through LDS.  `s_sums` is one of two buffers that a row's
-// reductions take by turns, so that one barrier each is enough: who writes a buffer again has passed the barrier that its readers came to.
-template <int WAVES, int N> __device__ __forceinline__ void row_sums(double (&v)[N], double (*s_sums)[WAVES], int lane, int wave)
+// A row's sums of products, over a thread's elements and a wavefront's lanes, are in fp32 as long as that holds them: a total outside of [2^-100, 2^100)
+// in size, or a NaN, may come of products that it does not, and the row's sums are formed again in fp64.  (In fp64 throughout, the conversions alone took
+// more of the vector units than all the rest: 27200 x 2048 bf16 backward 220 us.)
+__device__ __forceinline__ bool held_in_32_bits(double v)
 {
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = lanes_sum(v[i]);
-    if constexpr (WAVES > 1) {
-        if (lane == 0)
-#pragma unroll
-            for (int i = 0; i < N; ++i) s_sums[i][wave] = v[i];
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            v[i] = 0.0;
-#pragma unroll
-            for (int o = 0; o < WAVES; ++o) v[i] += s_sums[i][o];
+    const double a = fabs(v);
+    return a >= 0x1p-100 && a < 0x1p100;
+}
+
+// Who has a row: a team of LANES lanes (then a workgroup has four wavefronts of such teams), or, MANY, all wavefronts of a workgroup.  Teams take
+// rows in turn.
+constexpr int kMostWaves = 16;
+template <int LANES, bool MANY> struct Team {
+    int thread, threads, wave;              // of the team; the wavefront of the workgroup
+    int64_t first, teams;
+    __device__ __forceinline__ Team()
+    {
+        wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+        if constexpr (MANY) {
+            thread = threadIdx.x;
+            threads = blockDim.x;
+            first = blockIdx.x;
+            teams = gridDim.x;
+        } else {
+            constexpr int kTeams = kWave / LANES;
+            thread = threadIdx.x % LANES;
+            threads = LANES;
+            first = (static_cast<int64_t>(blockIdx.x) * 4 + wave) * kTeams + threadIdx.x % kWave / LANES;
+            teams = static_cast<int64_t>(gridDim.x) * 4 * kTeams;
         }
     }
-}
+    // Sums over a row.  `s_sums` is one of several buffers by turns, so that one barrier each is enough: who writes a buffer again has passed a barrier that
+    // its readers came to.
+    template <typename V, int N> __device__ __forceinline__ void sum(const V (&v)[N], double (&out)[N], double (*s_sums)[kMostWaves]) const
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) out[i] = static_cast<double>(lanes_sum<LANES>(v[i]));
+        if constexpr (MANY) {
+            if (threadIdx.x % kWave == 0)
+#pragma unroll
+                for (int i = 0; i < N; ++i) s_sums[i][wave] = out[i];
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < N; ++i) out[i] = 0.0;
+            for (int w = 0; w < threads / kWave; ++w)
+#pragma unroll
+                for (int i = 0; i < N; ++i) out[i] += s_sums[i][w];
+        }
+    }
+    // `add(k, sums)` adds the products of a thread's k-th element to N sums, in the type of these; all but the first of which may be zeros by nature.
+    template <int E, int N, typename F> __device__ __forceinline__ void sums_of(F add, double (&out)[N], double (*s_sums)[kMostWaves], double (*s_again)[kMostWaves]) const
+    {
+        float v[N] = {};
+#pragma unroll
+        for (int k = 0; k < E; ++k) add(k, v);
+        sum(v, out, s_sums);
+        bool held = true;
+#pragma unroll
+        for (int i = 0; i < N; ++i) held = held && held_in_32_bits(out[i]);
+        if (held) return;
+        double w[N] = {};
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+            add(k, w);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        sum(w, out, s_again);
+        if constexpr (MANY) __syncthreads();                            // (the next row may be done again too)
+    }
+};
 
-// A row to a wavefront (four rows to a workgroup) or to all wavefronts of a workgroup, which take rows in turn; a row stays in registers (E elements
-// a thread) from its one reading to its writing.
-template <typename T, int WAVES, int E>
-__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void ctc_block_norm_kernel(BlockNormArgs p)
+// The two weights' products and what meets z, for a thread's E columns.
+template <int E, int VECTOR> __device__ __forceinline__ void load_weights(const float* weight_after, const float* scale, const float* weight_before, int H,
+                                                                          int thread, int threads, float (&after)[E], float (&before)[E])
 {
-    constexpr int kE = Vector<T>::kElements, kVectors = E / kE, kWidth = WAVES * kWave, kRows = WAVES == 1 ? 4 : 1;
-    __shared__ double s_sums[2][1][WAVES];
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const int thread = WAVES == 1 ? lane : threadIdx.x;
-    const int n = listed(p.frames, p.rows);
-    float after[E], before[E];
 #pragma unroll
     for (int v = 0; v < E / 4; ++v) {
-        const int col = ((v * 4 / kE) * kWidth + thread) * kE + v * 4 % kE;
-        const Vector<float> a = weights_at(p.weight_after, col, p.H), s = weights_at(p.scale, col, p.H), w = weights_at(p.weight_before, col, p.H);
+        const int col = ((v * 4 / VECTOR) * threads + thread) * VECTOR + v * 4 % VECTOR;
+        const Vector<float> a = weights_at(weight_after, col, H), s = weights_at(scale, col, H), w = weights_at(weight_before, col, H);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             after[4 * v + j] = a.v[j] * s.v[j];
             before[4 * v + j] = w.v[j];
         }
     }
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kRows + (WAVES == 1 ? wave : 0); i < n; i += static_cast<int64_t>(gridDim.x) * kRows) {
+}
+
+// A vector as it was read, of which nothing worked out before is known any more (see forget): widened again where it is used again.
+template <typename T, int N> __device__ __forceinline__ void forget(Vector<T> (&v)[N])
+{
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        uint32_t w[4];
+        __builtin_memcpy(w, &v[n], 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm("" : "+v"(w[i]));
+        __builtin_memcpy(&v[n], w, 16);
+    }
+}
+
+// A row stays in registers (E elements a thread) from its one reading to its writing.  Bound by the bytes.
+template <typename T, int LANES, bool MANY, int E>
+__global__ __launch_bounds__(MANY ? kMostWaves * kWave : 256) void ctc_block_norm_kernel(BlockNormArgs p)
+{
+    constexpr int kE = Vector<T>::kElements, kVectors = E / kE;
+    constexpr bool kFine = sizeof(T) == 4;
+    __shared__ double s_sums[3][1][kMostWaves];
+    const Team<LANES, MANY> team;
+    const int n = listed(p.frames, p.rows);
+    float after[E], before[E];
+    load_weights<E, kE>(p.weight_after, p.scale, p.weight_before, p.H, team.thread, team.threads, after, before);
+    for (int64_t i = team.first; i < n; i += team.teams) {
         const int r = row_of(p.frames, p.rows, static_cast<int>(i));
         if (r < 0) continue;
         const int64_t row = static_cast<int64_t>(r) * p.H;
         Vector<T> x[kVectors], g[kVectors], z[kVectors];
 #pragma unroll
         for (int v = 0; v < kVectors; ++v) {
-            const int col = (v * kWidth + thread) * kE;
-            x[v] = load_vector(static_cast<const T*>(p.x) + row, col, p.H);
-            if (p.gate) g[v] = load_vector(static_cast<const T*>(p.gate) + r * p.gate_pitch, col, p.H);
+            const int col = (v * team.threads + team.thread) * kE;
+            x[v] = load_row(static_cast<const T*>(p.x) + row, col, p.H);
+            if (p.gate) g[v] = load_row(static_cast<const T*>(p.gate) + r * p.gate_pitch, col, p.H);
             z[v] = Vector<T>{};
-            if (p.residual) z[v] = load_vector(static_cast<const T*>(p.residual) + row, col, p.H);
+            if (p.residual) z[v] = load_row(static_cast<const T*>(p.residual) + row, col, p.H);
         }
-        double sum[1] = {};
-#pragma unroll
-        for (int k = 0; k < E; ++k) {
-            const double f = static_cast<double>(widen(x[k / kE].v[k % kE]));
-            sum[0] += f * f;
-        }
-        row_sums<WAVES, 1>(sum, s_sums[0], lane, wave);
+        double sum[1];
+        const auto squares = [](const Vector<T>(&of)[kVectors]) {
+            return [&of](int k, auto& s) {
+                const auto f = static_cast<std::decay_t<decltype(s[0])>>(widen(of[k / kE].v[k % kE]));
+                s[0] += f * f;
+            };
+        };
+        team.template sums_of<E>(squares(x), sum, s_sums[0], s_sums[2]);
         float f = static_cast<float>(1.0 / sqrt(sum[0] / p.H + static_cast<double>(p.eps)));
-        sum[0] = 0.0;
 #pragma unroll
         for (int k = 0; k < E; ++k) {
             float y = widen(x[k / kE].v[k % kE]) * f * after[k];
             if (p.gate) {
                 const float gate = widen(g[k / kE].v[k % kE]);
-                y *= gate * share_of<sizeof(T) == 4>(gate);
+                y *= gate * share_of<kFine>(gate);
             }
             const T rounded = narrow<T>(y + widen(z[k / kE].v[k % kE]));
             z[k / kE].v[k % kE] = rounded;
-            const double d = static_cast<double>(widen(rounded));
-            sum[0] += d * d;
         }
         if (p.sum)
 #pragma unroll
-            for (int v = 0; v < kVectors; ++v) store_vector(static_cast<T*>(p.sum) + row, (v * kWidth + thread) * kE, p.H, z[v]);
+            for (int v = 0; v < kVectors; ++v) store_vector(static_cast<T*>(p.sum) + row, (v * team.threads + team.thread) * kE, p.H, z[v]);
         if (!p.normed) {
-            if constexpr (WAVES > 1) __syncthreads();                   // (the buffer is written again for the next row)
+            if constexpr (MANY) __syncthreads();                        // (the buffer is written again for the next row)
             continue;
         }
-        row_sums<WAVES, 1>(sum, s_sums[1], lane, wave);
+        team.template sums_of<E>(squares(z), sum, s_sums[1], s_sums[2]);
         f = static_cast<float>(1.0 / sqrt(sum[0] / p.H + static_cast<double>(p.eps)));
 #pragma unroll
         for (int v = 0; v < kVectors; ++v) {
 #pragma unroll
             for (int k = 0; k < kE; ++k) z[v].v[k] = narrow<T>(widen(z[v].v[k]) * f * before[v * kE + k]);
-            store_vector(static_cast<T*>(p.normed) + row, (v * kWidth + thread) * kE, p.H, z[v]);
+            store_vector(static_cast<T*>(p.normed) + row, (v * team.threads + team.thread) * kE, p.H, z[v]);
         }
     }
 }
 
-template <typename T, int WAVES, int E>
-__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void ctc_block_norm_backward_kernel(BlockNormBackArgs p)
+template <typename T, int LANES, bool MANY>
+__global__ __launch_bounds__(MANY ? kMostWaves * kWave : 256, 4) void ctc_block_norm_backward_kernel(BlockNormBackArgs p)
 {
-    constexpr int kE = Vector<T>::kElements, kVectors = E / kE, kWidth = WAVES * kWave, kRows = WAVES == 1 ? 4 : 1;
-    __shared__ double s_first[3][WAVES], s_second[1][WAVES];
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const int thread = WAVES == 1 ? lane : threadIdx.x;
+    constexpr int E = 8, kE = Vector<T>::kElements, kVectors = E / kE;
+    constexpr bool kFine = sizeof(T) == 4;
+    __shared__ double s_sums[4][2][kMostWaves];
+    const Team<LANES, MANY> team;
     const int n = listed(p.frames, p.rows);
     float after[E], before[E], sum_before[E], sum_q[E];
-#pragma unroll
-    for (int v = 0; v < E / 4; ++v) {
-        const int col = ((v * 4 / kE) * kWidth + thread) * kE + v * 4 % kE;
-        const Vector<float> a = weights_at(p.weight_after, col, p.H), s = weights_at(p.scale, col, p.H), w = weights_at(p.weight_before, col, p.H);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            after[4 * v + j] = a.v[j] * s.v[j];
-            before[4 * v + j] = w.v[j];
-        }
-    }
+    load_weights<E, kE>(p.weight_after, p.scale, p.weight_before, p.H, team.thread, team.threads, after, before);
 #pragma unroll
     for (int k = 0; k < E; ++k) sum_before[k] = sum_q[k] = 0.0f;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kRows + (WAVES == 1 ? wave : 0); i < n; i += static_cast<int64_t>(gridDim.x) * kRows) {
+    for (int64_t i = team.first; i < n; i += team.teams) {
         const int r = row_of(p.frames, p.rows, static_cast<int>(i));
         if (r < 0) continue;
         const int64_t row = static_cast<int64_t>(r) * p.H;
         Vector<T> x[kVectors], g[kVectors], z[kVectors], dy[kVectors], dz[kVectors];
 #pragma unroll
         for (int v = 0; v < kVectors; ++v) {
-            const int col = (v * kWidth + thread) * kE;
-            x[v] = load_vector(static_cast<const T*>(p.x) + row, col, p.H);
-            if (p.gate) g[v] = load_vector(static_cast<const T*>(p.gate) + r * p.gate_pitch, col, p.H);
+            const int col = (v * team.threads + team.thread) * kE;
+            x[v] = load_row(static_cast<const T*>(p.x) + row, col, p.H);
+            if (p.gate) g[v] = load_row(static_cast<const T*>(p.gate) + r * p.gate_pitch, col, p.H);
             z[v] = dy[v] = dz[v] = Vector<T>{};
             if (p.dnormed) {
-                z[v] = load_vector(static_cast<const T*>(p.sum) + row, col, p.H);
-                dy[v] = load_vector(static_cast<const T*>(p.dnormed) + row, col, p.H);
+                z[v] = load_row(static_cast<const T*>(p.sum) + row, col, p.H);
+                dy[v] = load_row(static_cast<const T*>(p.dnormed) + row, col, p.H);
             }
-            if (p.dsum) dz[v] = load_vector(static_cast<const T*>(p.dsum) + row, col, p.H);
+            if (p.dsum) dz[v] = load_row(static_cast<const T*>(p.dsum) + row, col, p.H);
         }
-        double sums[3] = {};
-#pragma unroll
-        for (int k = 0; k < E; ++k) {
-            const double a = static_cast<double>(widen(x[k / kE].v[k % kE])), b = static_cast<double>(widen(z[k / kE].v[k % kE]));
-            sums[0] += a * a;
-            sums[1] += b * b;
-            sums[2] += static_cast<double>(widen(dy[k / kE].v[k % kE]) * before[k]) * b;
-        }
-        row_sums<WAVES, 3>(sums, s_first, lane, wave);
-        const double v1 = sums[0] / p.H + static_cast<double>(p.eps), v2 = sums[1] / p.H + static_cast<double>(p.eps);
-        // (the mean's share without the factor: with it, it would vanish in fp32 for rows of 1e20 and more)
-        const float f1 = static_cast<float>(1.0 / sqrt(v1)), f2 = static_cast<float>(1.0 / sqrt(v2)), c2 = static_cast<float>(sums[2] / p.H / v2);
-        double along[1] = {};
+        // (x apart from z and dnormed, which may not be there)
+        double square[1], sums[2] = {};
+        team.template sums_of<E>([&](int k, auto& s) {
+            const auto a = static_cast<std::decay_t<decltype(s[0])>>(widen(x[k / kE].v[k % kE]));
+            s[0] += a * a;
+        }, square, s_sums[0], s_sums[3]);
+        if (p.dnormed)
+            team.template sums_of<E>([&](int k, auto& s) {
+                using V = std::decay_t<decltype(s[0])>;
+                const V a = static_cast<V>(widen(z[k / kE].v[k % kE]));
+                s[0] += a * a;
+                s[1] += static_cast<V>(widen(dy[k / kE].v[k % kE]) * before[k]) * a;
+            }, sums, s_sums[1], s_sums[3]);
+        const double v1 = square[0] / p.H + static_cast<double>(p.eps), v2 = sums[0] / p.H + static_cast<double>(p.eps);
+        // (the means' shares without the factors: with them, they would vanish in fp32 for rows of 1e20 and more)
+        const float f1 = static_cast<float>(1.0 / sqrt(v1)), f2 = static_cast<float>(1.0 / sqrt(v2)), c2 = static_cast<float>(sums[1] / p.H / v2);
+        forget(x);
+        forget(z);
+        forget(dy);
         float e[E];
 #pragma unroll
-        for (int k = 0; k < E; ++k) {
-            const float dyk = widen(dy[k / kE].v[k % kE]), zk = widen(z[k / kE].v[k % kE]), xk = widen(x[k / kE].v[k % kE]);
-            const float d = (dyk * before[k] - zk * c2) * f2 + widen(dz[k / kE].v[k % kE]);
-            sum_before[k] += dyk * (zk * f2);
-            dz[k / kE].v[k % kE] = narrow<T>(d);
-            float a = 1.0f;
-            const float normed = xk * f1;
-            if (p.gate) {
-                const float gate = widen(g[k / kE].v[k % kE]);
-                const Gate s = gate_of<sizeof(T) == 4>(gate);
-                a = gate * s.z;
-                g[k / kE].v[k % kE] = narrow<T>(d * after[k] * normed * (s.z + a * s.stays));
-            }
-            sum_q[k] += d * a * normed;
-            e[k] = d * a * after[k];
-            along[0] += static_cast<double>(e[k]) * static_cast<double>(xk);
-        }
-        row_sums<WAVES, 1>(along, s_second, lane, wave);
-        const float c1 = static_cast<float>(along[0] / p.H / v1);
-#pragma unroll
         for (int v = 0; v < kVectors; ++v) {
-            const int col = (v * kWidth + thread) * kE;
+            const int col = (v * team.threads + team.thread) * kE;
 #pragma unroll
-            for (int k = 0; k < kE; ++k) x[v].v[k] = narrow<T>((e[v * kE + k] - widen(x[v].v[k]) * c1) * f1);
-            store_vector(static_cast<T*>(p.dx) + row, col, p.H, x[v]);
+            for (int j = 0; j < kE; ++j) {
+                const int k = v * kE + j;
+                const float dyk = widen(dy[v].v[j]), zk = widen(z[v].v[j]);
+                const float d = (dyk * before[k] - zk * c2) * f2 + widen(dz[v].v[j]), normed = widen(x[v].v[j]) * f1;
+                sum_before[k] += dyk * (zk * f2);
+                dz[v].v[j] = narrow<T>(d);
+                float a = 1.0f;
+                if (p.gate) {
+                    const float gate = widen(g[v].v[j]);
+                    const Gate s = gate_of<kFine>(gate);
+                    a = gate * s.z;
+                    g[v].v[j] = narrow<T>(d * after[k] * normed * (s.z + a * s.stays));
+                }
+                e[k] = d * a;
+                sum_q[k] += e[k] * normed;
+                e[k] *= after[k];
+                if (k % 2) __builtin_amdgcn_sched_barrier(0);           // (two elements at a time: registers)
+            }
             if (p.gate) store_vector(static_cast<T*>(p.dgate) + r * p.gate_pitch, col, p.H, g[v]);
             if (p.dresidual) store_vector(static_cast<T*>(p.dresidual) + row, col, p.H, dz[v]);
+        }
+        forget(x);
+        team.template sums_of<E>([&](int k, auto& s) {
+            using V = std::decay_t<decltype(s[0])>;
+            s[0] += static_cast<V>(e[k]) * static_cast<V>(widen(x[k / kE].v[k % kE]));
+        }, square, s_sums[2], s_sums[3]);
+        const float c1 = static_cast<float>(square[0] / p.H / v1);
+#pragma unroll
+        for (int v = 0; v < kVectors; ++v) {
+#pragma unroll
+            for (int j = 0; j < kE; ++j) x[v].v[j] = narrow<T>((e[v * kE + j] - widen(x[v].v[j]) * c1) * f1);
+            store_vector(static_cast<T*>(p.dx) + row, (v * team.threads + team.thread) * kE, p.H, x[v]);
         }
     }
     if (!p.partials) return;
     float* out = p.partials + static_cast<int64_t>(blockIdx.x) * 2 * p.H;
-    if constexpr (WAVES == 1) {
-        // The four wavefronts' sums, one after another.
-        __shared__ float s_dw[2 * E][kWave];
+    if constexpr (!MANY) {
+        // The teams of a wavefront, then the four wavefronts' sums, one after another.
+        __shared__ float s_dw[2 * E][LANES];
+#pragma unroll
+        for (int k = 0; k < E; ++k)
+#pragma unroll
+            for (int d = LANES; d < kWave; d <<= 1) {
+                sum_before[k] += __shfl_xor(sum_before[k], d, kWave);
+                sum_q[k] += __shfl_xor(sum_q[k], d, kWave);
+            }
         for (int o = 0; o < 4; ++o) {
-            if (wave == o) {
+            if (team.wave == o && threadIdx.x % kWave < LANES) {
 #pragma unroll
                 for (int k = 0; k < E; ++k) {
                     if (o) {
-                        sum_before[k] += s_dw[k][lane];
-                        sum_q[k] += s_dw[E + k][lane];
+                        sum_before[k] += s_dw[k][team.thread];
+                        sum_q[k] += s_dw[E + k][team.thread];
                     }
-                    s_dw[k][lane] = sum_before[k];
-                    s_dw[E + k][lane] = sum_q[k];
+                    s_dw[k][team.thread] = sum_before[k];
+                    s_dw[E + k][team.thread] = sum_q[k];
                 }
             }
             __syncthreads();
         }
-        if (wave != 3) return;
+        if (team.wave != 3 || threadIdx.x % kWave >= LANES) return;
     }
 #pragma unroll
     for (int v = 0; v < E / 4; ++v) {
-        const int col = ((v * 4 / kE) * kWidth + thread) * kE + v * 4 % kE;
+        const int col = ((v * 4 / kE) * team.threads + team.thread) * kE + v * 4 % kE;
         Vector<float> a, b;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -251,13 +363,13 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) void ctc_block_no
     }
 }
 
-// Rows of more than 4096, whose tensors a compute unit's registers do not hold beside the sums: a workgroup to a row, which reads it twice from memory and once more from the
+// Rows of more than 8192, whose tensors a compute unit's registers do not hold beside the sums: a workgroup to a row, which reads it twice from memory and once more from the
 // caches, and adds to its own partial sums there.
 template <typename T> __global__ __launch_bounds__(1024) void ctc_block_norm_backward_wide_kernel(BlockNormBackArgs p)
 {
     constexpr int kE = Vector<T>::kElements, kStep = 1024 * kE;
-    __shared__ double s_first[3][16], s_second[1][16];
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    __shared__ double s_first[3][kMostWaves], s_second[1][kMostWaves];
+    const Team<kWave, true> team;
     const int n = listed(p.frames, p.rows);
     float* const sums_out = p.partials ? p.partials + static_cast<int64_t>(blockIdx.x) * 2 * p.H : nullptr;
     if (sums_out)
@@ -290,7 +402,7 @@ template <typename T> __global__ __launch_bounds__(1024) void ctc_block_norm_bac
                 }
             }
         }
-        row_sums<16, 3>(sums, s_first, lane, wave);
+        team.sum(sums, sums, s_first);
         const double v1 = sums[0] / p.H + static_cast<double>(p.eps), v2 = sums[1] / p.H + static_cast<double>(p.eps);
         const float f1 = static_cast<float>(1.0 / sqrt(v1)), f2 = static_cast<float>(1.0 / sqrt(v2)), c2 = static_cast<float>(sums[2] / p.H / v2);
         double along[1] = {};
@@ -349,7 +461,7 @@ template <typename T> __global__ __launch_bounds__(1024) void ctc_block_norm_bac
                 if (p.dresidual) store_vector(static_cast<T*>(p.dresidual) + row, col, p.H, dz);
             }
             if (pass) break;
-            row_sums<16, 1>(along, s_second, lane, wave);
+            team.sum(along, along, s_second);
             c1 = static_cast<float>(along[0] / p.H / v1);
         }
     }
@@ -385,27 +497,32 @@ __global__ __launch_bounds__(1024) void ctc_block_norm_weights_kernel(const floa
     if (dscale) dscale[k] = static_cast<float>(weight_after ? sum * static_cast<double>(weight_after[k]) : sum);
 }
 
+// Rows of up to 512 go to teams of as few lanes as hold them, wider ones to as many wavefronts.
 template <typename T> int launch_norm_of(const BlockNormArgs& p, hipStream_t s)
 {
-    const int per_group = p.H <= 1024 ? 4 : 1;
-    const int64_t groups = (static_cast<int64_t>(p.rows) + per_group - 1) / per_group;
+    const RowTeam team = row_team(p.H);
+    const int64_t groups = (static_cast<int64_t>(p.rows) + team.rows - 1) / team.rows;
     const dim3 grid(static_cast<unsigned>(groups < 8192 ? groups : 8192));
-    if (p.H <= 512) return launch(ctc_block_norm_kernel<T, 1, 8>, grid, 256, s, p);
-    if (p.H <= 1024) return launch(ctc_block_norm_kernel<T, 1, 16>, grid, 256, s, p);
-    if (p.H <= 2048) return launch(ctc_block_norm_kernel<T, 4, 8>, grid, 256, s, p);
-    if (p.H <= 4096) return launch(ctc_block_norm_kernel<T, 4, 16>, grid, 256, s, p);
-    if (p.H <= 8192) return launch(ctc_block_norm_kernel<T, 16, 8>, grid, 1024, s, p);
-    return launch(ctc_block_norm_kernel<T, 16, 16>, grid, 1024, s, p);
+    switch (team.lanes) {
+    case 8: return launch(ctc_block_norm_kernel<T, 8, false, 8>, grid, 256, s, p);
+    case 16: return launch(ctc_block_norm_kernel<T, 16, false, 8>, grid, 256, s, p);
+    case 32: return launch(ctc_block_norm_kernel<T, 32, false, 8>, grid, 256, s, p);
+    case 64: return launch(ctc_block_norm_kernel<T, 64, false, 8>, grid, 256, s, p);
+    }
+    return team.elements == 8 ? launch(ctc_block_norm_kernel<T, 64, true, 8>, grid, team.lanes, s, p) : launch(ctc_block_norm_kernel<T, 64, true, 16>, grid, team.lanes, s, p);
 }
 
 template <typename T> int launch_backward_of(const BlockNormBackArgs& p, unsigned groups, hipStream_t s)
 {
     const dim3 grid(groups);
-    if (p.H <= 512) return launch(ctc_block_norm_backward_kernel<T, 1, 8>, grid, 256, s, p);
-    if (p.H <= 1024) return launch(ctc_block_norm_backward_kernel<T, 2, 8>, grid, 128, s, p);
-    if (p.H <= 2048) return launch(ctc_block_norm_backward_kernel<T, 4, 8>, grid, 256, s, p);
-    if (p.H <= 4096) return launch(ctc_block_norm_backward_kernel<T, 8, 8>, grid, 512, s, p);
-    return launch(ctc_block_norm_backward_wide_kernel<T>, grid, 1024, s, p);
+    const RowTeam team = row_team(p.H);
+    switch (team.lanes) {
+    case 8: return launch(ctc_block_norm_backward_kernel<T, 8, false>, grid, 256, s, p);
+    case 16: return launch(ctc_block_norm_backward_kernel<T, 16, false>, grid, 256, s, p);
+    case 32: return launch(ctc_block_norm_backward_kernel<T, 32, false>, grid, 256, s, p);
+    case 64: return launch(ctc_block_norm_backward_kernel<T, 64, false>, grid, 256, s, p);
+    }
+    return team.elements == 8 ? launch(ctc_block_norm_backward_kernel<T, 64, true>, grid, team.lanes, s, p) : launch(ctc_block_norm_backward_wide_kernel<T>, grid, 1024, s, p);
 }
 
 }  // namespace

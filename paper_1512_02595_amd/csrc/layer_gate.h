@@ -36,6 +36,10 @@ template <bool FINE> __device__ __forceinline__ float share_of(float g)
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-g * kLog2e));
 }
 
+// The number itself, of which nothing worked out before is known any more: what was made of it is made again where it is used again, in place of being
+// kept in registers for long.
+__device__ __forceinline__ void forget(float& v) { asm("" : "+v"(v)); }
+
 }  // namespace
 }  // namespace layer
 

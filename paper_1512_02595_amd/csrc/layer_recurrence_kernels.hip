@@ -49,10 +49,6 @@ struct Map {
     double keep, add;
 };
 
-// The number itself, of which nothing worked out before is known any more: it is converted again where it is used again, in place of being kept
-// in fp64 over a barrier in twice the registers.
-__device__ __forceinline__ void forget(float& v) { asm("" : "+v"(v)); }
-
 // To fp32, and from there on a number in fp32: the compiler would take this rounding and the one to bf16 behind it for one, which it works out in eight
 // operations more.
 __device__ __forceinline__ float once(double v)

@@ -136,8 +136,8 @@ def backward(c, dx_at=None, dres_at=None, use_dy=True, use_dz=True, sums=(True, 
     block.block_norm_backward(at(dy), at(dz), at(x), at(gate), c.pitch, at(z), *map(at, c.w_dev), EPS, pointer(c.frames), c.rows, c.H, c.dtype,
                               at(dx), at(dgate), at(dres), *map(at, dw), (ws.t.data_ptr() + 255) // 256 * 256 if any(sums) else None, size, stream())
     torch.cuda.synchronize()
-    # (the partial sums: each workgroup's rows, and what four wavefronts add)
-    per_group = -(-c.rows // min(1024, -(-c.rows // (4 if c.H <= 1024 else 2)))) + 8
+    # (the partial sums: at least 256 workgroups share more rows than that; a workgroup of 32 teams takes 32 rows at once)
+    per_group = -(-c.rows // 256) + 40
     want, bound = ref.block_norm_backward(c.listed(c.dy) if use_dy else None, c.listed(c.dz) if use_dz else None, c.listed(c.x), c.listed(c.gate),
                                           c.listed(c.z) if use_dy else None, *c.ones, float(np.float32(EPS)), per_group, c.dtype == F32)
     rest, H = others(c.rows, c.names), c.H
