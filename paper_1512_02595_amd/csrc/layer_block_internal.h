@@ -111,14 +111,20 @@ inline RowTeam row_team(int H)
     return {(H + 1023) / 1024 * 64, 16, 1};
 }
 
-// Workgroups of the backward pass, each of which leaves its partial sums: as many as are at work at once, by their registers four wavefronts to each of a
-// compute unit's four SIMDs.  (One of five wavefronts leaves room for one more such, not for two: 5000 x 2500 fp32 in 768 of them 132 us.)
+// Workgroups of such teams that a compute unit has at work at once, where registers leave so many wavefronts to each of its four SIMDs.  (A workgroup of five
+// has two on one of them: 5000 x 2500 fp32 backward in 768 workgroups 132 us, in 512 89.)
+inline int groups_at_once(const RowTeam& team, int waves_to_a_simd)
+{
+    const int waves = team.lanes <= 64 ? 4 : team.lanes / 64;
+    return waves < 4 ? 4 * waves_to_a_simd / waves : waves_to_a_simd / ((waves + 3) / 4) > 0 ? waves_to_a_simd / ((waves + 3) / 4) : 1;
+}
+
+// Workgroups of the backward pass, each of which leaves its partial sums: as many as are at work at once.
 inline int block_norm_groups(int rows, int H)
 {
     const RowTeam team = row_team(H);
-    const int waves = team.lanes <= 64 ? 4 : team.lanes / 64, at_once = waves <= 2 ? 8 : 4 / ((waves + 3) / 4);
-    const int groups = (rows - 1) / team.rows + 1;
-    return groups < 256 * at_once ? groups : 256 * at_once;
+    const int most = 256 * groups_at_once(team, 4), groups = (rows - 1) / team.rows + 1;
+    return groups < most ? groups : most;
 }
 
 int launch_block_norm(const BlockNormArgs& p, bool bf16, void* stream);

@@ -11,23 +11,23 @@
 namespace layer {
 namespace {
 
-// load_vector, but that a row's last lane waits for no more than the others: where a vector reaches over the row's end it is the row's last one, shifted.  (Its
-// elements one by one: 10000 x 2500 bf16 97 us, backward 199.)
-template <typename T> __device__ __forceinline__ Vector<T> load_row(const T* row, int col, int H)
+// A vector of a row of H >= kElements, asked for without a branch: one that reaches over the row's end is the row's last whole one.  Its lane shifts it to
+// its place when it has come (behind the end then are zeros), so that nobody waits for it sooner, or for elements one by one (which made 10000 x 2500 bf16
+// 97 us in place of 89, backward 199 in place of 158).
+template <typename T> __device__ __forceinline__ Vector<T> ask(const T* row, int col, int H)
 {
     constexpr int kE = Vector<T>::kElements;
-    if (sizeof(T) == 4 || H < kE) return load_vector(row, col, H);      // (four elements one by one cost nothing: 12506 x 1999 fp32 98 us, 6250 x 2000 94)
-    const int from = col + kE <= H ? col : H - kE;
-    Vector<T> r = load_whole(row + from);
-    if (from != col) {
-        const unsigned bits = static_cast<unsigned>(col - from) * (8 * sizeof(T));
-        uint64_t w[2];
-        __builtin_memcpy(w, &r, 16);
-        w[0] = bits < 64 ? w[0] >> bits | w[1] << 1 << (63 - bits) : bits < 128 ? w[1] >> (bits - 64) : 0;
-        w[1] = bits < 64 ? w[1] >> bits : 0;
-        __builtin_memcpy(&r, w, 16);
-    }
-    return r;
+    if (H < kE) return load_vector(row, col, H);
+    return load_whole(row + (col + kE <= H ? col : H - kE));
+}
+template <typename T> __device__ __forceinline__ void shift(Vector<T>& r, int col, int H)
+{
+    const unsigned bits = static_cast<unsigned>(col + Vector<T>::kElements - H) * (8 * sizeof(T));
+    uint64_t w[2];
+    __builtin_memcpy(w, &r, 16);
+    w[0] = bits < 64 ? w[0] >> bits | w[1] << 1 << (63 - bits) : bits < 128 ? w[1] >> (bits - 64) : 0;
+    w[1] = bits < 64 ? w[1] >> bits : 0;
+    __builtin_memcpy(&r, w, 16);
 }
 
 // Four of a weight's floats, ones where there is no weight.
@@ -127,7 +127,10 @@ template <int LANES, bool MANY> struct Team {
     {
         float v[N] = {};
 #pragma unroll
-        for (int k = 0; k < E; ++k) add(k, v);
+        for (int k = 0; k < E; ++k) {
+            add(k, v);
+            if (k % 2) __builtin_amdgcn_sched_barrier(0);               // (two elements at a time: registers)
+        }
         sum(v, out, s_sums);
         bool held = true;
 #pragma unroll
@@ -173,29 +176,58 @@ template <typename T, int N> __device__ __forceinline__ void forget(Vector<T> (&
     }
 }
 
-// A row stays in registers (E elements a thread) from its one reading to its writing.  Bound by the bytes.
+// A row stays in registers (E elements a thread) from its one reading to its writing; the next one is asked for before it is gone over (not where a
+// thread has 16 elements, for want of registers).  Bound by the bytes.
 template <typename T, int LANES, bool MANY, int E>
 __global__ __launch_bounds__(MANY ? kMostWaves * kWave : 256) void ctc_block_norm_kernel(BlockNormArgs p)
 {
     constexpr int kE = Vector<T>::kElements, kVectors = E / kE;
-    constexpr bool kFine = sizeof(T) == 4;
+    constexpr bool kFine = sizeof(T) == 4, kAhead = E == 8;
     __shared__ double s_sums[3][1][kMostWaves];
     const Team<LANES, MANY> team;
     const int n = listed(p.frames, p.rows);
     float after[E], before[E];
     load_weights<E, kE>(p.weight_after, p.scale, p.weight_before, p.H, team.thread, team.threads, after, before);
-    for (int64_t i = team.first; i < n; i += team.teams) {
-        const int r = row_of(p.frames, p.rows, static_cast<int>(i));
-        if (r < 0) continue;
-        const int64_t row = static_cast<int64_t>(r) * p.H;
+    struct Row {
         Vector<T> x[kVectors], g[kVectors], z[kVectors];
+    } here, ahead;
+    const auto bring = [&](int r, Row& to) {
+        if (r < 0) return;
+        const int64_t row = static_cast<int64_t>(r) * p.H;
 #pragma unroll
         for (int v = 0; v < kVectors; ++v) {
             const int col = (v * team.threads + team.thread) * kE;
-            x[v] = load_row(static_cast<const T*>(p.x) + row, col, p.H);
-            if (p.gate) g[v] = load_row(static_cast<const T*>(p.gate) + r * p.gate_pitch, col, p.H);
-            z[v] = Vector<T>{};
-            if (p.residual) z[v] = load_row(static_cast<const T*>(p.residual) + row, col, p.H);
+            to.x[v] = ask(static_cast<const T*>(p.x) + row, col, p.H);
+            to.g[v] = Vector<T>{};
+            if (p.gate) to.g[v] = ask(static_cast<const T*>(p.gate) + r * p.gate_pitch, col, p.H);
+            to.z[v] = Vector<T>{};
+            if (p.residual) to.z[v] = ask(static_cast<const T*>(p.residual) + row, col, p.H);
+        }
+    };
+    const auto row_number = [&](int64_t i) { return i < n ? row_of(p.frames, p.rows, static_cast<int>(i)) : -1; };
+    int next = row_number(team.first), after_next = row_number(team.first + team.teams);
+    if constexpr (kAhead) bring(next, ahead);
+    for (int64_t i = team.first; i < n; i += team.teams) {
+        const int r = next;
+        next = after_next;
+        after_next = row_number(i + 2 * team.teams);
+        if constexpr (kAhead) {
+            here = ahead;
+            bring(next, ahead);
+        } else {
+            bring(r, here);
+        }
+        if (r < 0) continue;
+        const int64_t row = static_cast<int64_t>(r) * p.H;
+        auto &x = here.x, &g = here.g, &z = here.z;
+#pragma unroll
+        for (int v = 0; v < kVectors; ++v) {
+            const int col = (v * team.threads + team.thread) * kE;
+            if (col + kE > p.H && p.H >= kE) {
+                shift(x[v], col, p.H);
+                shift(g[v], col, p.H);
+                shift(z[v], col, p.H);
+            }
         }
         double sum[1];
         const auto squares = [](const Vector<T>(&of)[kVectors]) {
@@ -254,14 +286,25 @@ __global__ __launch_bounds__(MANY ? kMostWaves * kWave : 256, 4) void ctc_block_
 #pragma unroll
         for (int v = 0; v < kVectors; ++v) {
             const int col = (v * team.threads + team.thread) * kE;
-            x[v] = load_row(static_cast<const T*>(p.x) + row, col, p.H);
-            if (p.gate) g[v] = load_row(static_cast<const T*>(p.gate) + r * p.gate_pitch, col, p.H);
-            z[v] = dy[v] = dz[v] = Vector<T>{};
+            x[v] = ask(static_cast<const T*>(p.x) + row, col, p.H);
+            g[v] = z[v] = dy[v] = dz[v] = Vector<T>{};
+            if (p.gate) g[v] = ask(static_cast<const T*>(p.gate) + r * p.gate_pitch, col, p.H);
             if (p.dnormed) {
-                z[v] = load_row(static_cast<const T*>(p.sum) + row, col, p.H);
-                dy[v] = load_row(static_cast<const T*>(p.dnormed) + row, col, p.H);
+                z[v] = ask(static_cast<const T*>(p.sum) + row, col, p.H);
+                dy[v] = ask(static_cast<const T*>(p.dnormed) + row, col, p.H);
             }
-            if (p.dsum) dz[v] = load_row(static_cast<const T*>(p.dsum) + row, col, p.H);
+            if (p.dsum) dz[v] = ask(static_cast<const T*>(p.dsum) + row, col, p.H);
+        }
+#pragma unroll
+        for (int v = 0; v < kVectors; ++v) {
+            const int col = (v * team.threads + team.thread) * kE;
+            if (col + kE > p.H && p.H >= kE) {
+                shift(x[v], col, p.H);
+                shift(g[v], col, p.H);
+                shift(z[v], col, p.H);
+                shift(dy[v], col, p.H);
+                shift(dz[v], col, p.H);
+            }
         }
         // (x apart from z and dnormed, which may not be there)
         double square[1], sums[2] = {};
@@ -364,7 +407,7 @@ __global__ __launch_bounds__(MANY ? kMostWaves * kWave : 256, 4) void ctc_block_
 }
 
 // Rows of more than 8192, whose tensors a compute unit's registers do not hold beside the sums: a workgroup to a row, which reads it twice from memory and once more from the
-// caches, and adds to its own partial sums there.
+// caches, and adds to its own partial sums t
 template <typename T> __global__ __launch_bounds__(1024) void ctc_block_norm_backward_wide_kernel(BlockNormBackArgs p)
 {
     constexpr int kE = Vector<T>::kElements, kStep = 1024 * kE;
@@ -502,7 +545,8 @@ template <typename T> int launch_norm_of(const BlockNormArgs& p, hipStream_t s)
 {
     const RowTeam team = row_team(p.H);
     const int64_t groups = (static_cast<int64_t>(p.rows) + team.rows - 1) / team.rows;
-    const dim3 grid(static_cast<unsigned>(groups < 8192 ? groups : 8192));
+    const int most = 256 * groups_at_once(team, sizeof(T) == 2 && team.elements == 8 ? 5 : 4);
+    const dim3 grid(static_cast<unsigned>(groups < most ? groups : most));
     switch (team.lanes) {
     case 8: return launch(ctc_block_norm_kernel<T, 8, false, 8>, grid, 256, s, p);
     case 16: return launch(ctc_block_norm_kernel<T, 16, false, 8>, grid, 256, s, p);
