@@ -152,6 +152,17 @@ struct LinearI4Args {
     void* logits;
 };
 
+// Rows and symbols to a workgroup.
+enum class I4Tile { k16x16, k16x16Deep, k32x16, k64x16, k64x32, k64x64 };
+inline I4Tile i4_tile(int rows, int pitch, int A)
+{
+    const auto tiles = [&](int m, int n) { return (static_cast<int64_t>(rows) + m - 1) / m * ((A + n - 1) / n); };
+    if (rows <= 16) return tiles(16, 16) < 256 && pitch >= 1024 ? I4Tile::k16x16Deep : I4Tile::k16x16;
+    if (rows <= 32) return I4Tile::k32x16;
+    if (tiles(64, 32) < 512) return I4Tile::k64x16;
+    return tiles(64, 64) < 512 ? I4Tile::k64x32 : I4Tile::k64x64;
+}
+
 int launch_quantize_i4(const void* weights, int A, int H, int group, bool bf16, uint8_t* weight_q, float* weight_scales, void* stream);
 int launch_dequantize_i4(const uint8_t* weight_q, const float* weight_scales, int A, int H, int group, bool bf16, void* out, void* stream);
 int launch_linear_i4(const LinearI4Args& p, bool bf16, void* stream);

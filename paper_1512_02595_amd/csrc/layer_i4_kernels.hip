@@ -159,31 +159,23 @@ __global__ __launch_bounds__(256) void ctc_dequantize_weights_i4_kernel(const ui
 typedef int int4v __attribute__((ext_vector_type(4)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 
-// RT by ST tiles of 16 rows by 16 symbols to a workgroup, each of whose four wavefronts takes every fourth 128 columns of all of them, straight from
-// memory into the matrix cores; their sums are added in LDS.  A weight's four bits become the upper half of a byte, sixteen times their
-// value: that takes one `and` (and a shift for the lower half) for four weights, and a sixteenth comes into the row's scale.
+// RT by ST tiles of 16 rows by 16 symbols to a workgroup, each of whose wavefronts takes every WAVES-th 128 columns of all of them, straight from memory
+// into the matrix cores, the next ones asked for before these are multiplied; their sums are added in LDS.  A weight's four bits become the upper half
+// of a byte, sixteen times their value: that takes one `and` (and a shift for the lower half) for four weights, and a sixteenth comes into the row's scale.
 // v_mfma_i32_16x16x64_i8: lane l gives bytes 16 (l / 16) .. of row l % 16 of either operand, and holds rows 4 (l / 16) .. + 3 of column
 // l % 16 of the result.
-template <typename T, int RT, int ST, bool BY_64>
-__global__ __launch_bounds__(256) void ctc_linear_i4_kernel(LinearI4Args p)
+template <typename T, int RT, int ST, int WAVES, bool BY_64>
+__global__ __launch_bounds__(WAVES * kWave) void ctc_linear_i4_kernel(LinearI4Args p)
 {
-    constexpr int kWaves = 4, kColumns = 16 * ST;
-    __shared__ float s_sum[kWaves][16 * RT][kColumns];
+    constexpr int kColumns = 16 * ST, kThreads = WAVES * kWave;
+    __shared__ float s_sum[WAVES][16 * RT][kColumns];
     __shared__ int s_row[16 * RT];
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const unsigned across = static_cast<unsigned>((p.A + kColumns - 1) / kColumns);
-    const int64_t group = group_number();
-    const int64_t m0 = group / across * (16 * RT);
+    const unsigned across = static_cast<unsigned>((p.A + kColumns - 1) / kColumns), group = static_cast<unsigned>(group_number());
+    const int64_t m0 = static_cast<int64_t>(group / across) * (16 * RT);
     const int n0 = static_cast<int>(group % across) * ST;                         // in tiles of 16 symbols
     if (m0 >= p.rows) return;
     const int tiles = p.pitch / kTileColumns, last_tile = (p.A + 15) / 16 - 1;
-    const int8_t* q[RT];
-#pragma unroll
-    for (int i = 0; i < RT; ++i) {
-        const int r = row_at(p.frames, p.rows, m0 + 16 * i + lane % 16);
-        if (wave == 0 && lane < 16) s_row[16 * i + lane] = r;
-        q[i] = p.q + static_cast<int64_t>(r < 0 ? 0 : r) * p.pitch + 16 * (lane / 16);          // (what row 0 gives instead is not written)
-    }
     const uint8_t* w[ST];
     const float* scale[ST];
 #pragma unroll
@@ -192,41 +184,63 @@ __global__ __launch_bounds__(256) void ctc_linear_i4_kernel(LinearI4Args p)
         w[s] = p.weight_q + tile * tiles * kTileBytes + 16 * lane;
         scale[s] = p.weight_scales + tile * p.groups * 16 + lane % 16;
     }
+    const int8_t* q[RT];
+    struct Columns {
+        int4v low[RT], high[RT], w[ST];
+        float by[ST], by_high[ST];
+    } here, next;
+    const auto weights = [&](int t, Columns& to) {
+        const int g = BY_64 ? 2 * t : t * kTileColumns / p.group;
+#pragma unroll
+        for (int s = 0; s < ST; ++s) {
+            __builtin_memcpy(&to.w[s], __builtin_assume_aligned(w[s] + static_cast<int64_t>(t) * kTileBytes, 16), 16);
+            to.by[s] = scale[s][static_cast<int64_t>(g) * 16];
+            if constexpr (BY_64) to.by_high[s] = scale[s][static_cast<int64_t>(g + 1 < p.groups ? g + 1 : g) * 16];      // (behind the last group the weights are zeros)
+        }
+    };
+    const auto rows = [&](int t, Columns& to) {
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            __builtin_memcpy(&to.low[i], __builtin_assume_aligned(q[i] + t * kTileColumns, 16), 16);
+            __builtin_memcpy(&to.high[i], __builtin_assume_aligned(q[i] + t * kTileColumns + 64, 16), 16);
+        }
+    };
+    // (the weights wait for nothing, the rows for the list)
+    if (wave < tiles) weights(wave, next);
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+        const int r = row_at(p.frames, p.rows, m0 + 16 * i + lane % 16);
+        if (wave == 0 && lane < 16) s_row[16 * i + lane] = r;
+        q[i] = p.q + static_cast<int64_t>(r < 0 ? 0 : r) * p.pitch + 16 * (lane / 16);          // (what row 0 gives instead is not written)
+    }
+    if (wave < tiles) rows(wave, next);
     float4v sum[RT][ST];
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
         for (int s = 0; s < ST; ++s) sum[i][s] = float4v{};
-    for (int t = wave; t < tiles; t += kWaves) {
-        int4v low[RT], high[RT];
-#pragma unroll
-        for (int i = 0; i < RT; ++i) {
-            __builtin_memcpy(&low[i], __builtin_assume_aligned(q[i] + t * kTileColumns, 16), 16);
-            __builtin_memcpy(&high[i], __builtin_assume_aligned(q[i] + t * kTileColumns + 64, 16), 16);
+    for (int t = wave; t < tiles; t += WAVES) {
+        here = next;
+        if (t + WAVES < tiles) {
+            weights(t + WAVES, next);
+            rows(t + WAVES, next);
         }
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int s = 0; s < ST; ++s) {
-            int4v v;
-            __builtin_memcpy(&v, __builtin_assume_aligned(w[s] + static_cast<int64_t>(t) * kTileBytes, 16), 16);
-            const int4v w_low = v << 4 & static_cast<int>(0xf0f0f0f0u), w_high = v & static_cast<int>(0xf0f0f0f0u);
-            const int g = t * kTileColumns / p.group;
-            const float by = scale[s][static_cast<int64_t>(g) * 16];
-            if constexpr (BY_64) {
-                const float by_high = g + 1 < p.groups ? scale[s][static_cast<int64_t>(g + 1) * 16] : 0.0f;
+            const int4v w_low = here.w[s] << 4 & static_cast<int>(0xf0f0f0f0u), w_high = here.w[s] & static_cast<int>(0xf0f0f0f0u);
 #pragma unroll
-                for (int i = 0; i < RT; ++i) {
-                    const int4v a = __builtin_amdgcn_mfma_i32_16x16x64_i8(low[i], w_low, int4v{}, 0, 0, 0);
-                    const int4v b = __builtin_amdgcn_mfma_i32_16x16x64_i8(high[i], w_high, int4v{}, 0, 0, 0);
+            for (int i = 0; i < RT; ++i) {
+                int4v a = __builtin_amdgcn_mfma_i32_16x16x64_i8(here.low[i], w_low, int4v{}, 0, 0, 0);
+                if constexpr (BY_64) {
+                    const int4v b = __builtin_amdgcn_mfma_i32_16x16x64_i8(here.high[i], w_high, int4v{}, 0, 0, 0);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) sum[i][s][k] = fmaf(static_cast<float>(b[k]), by_high, fmaf(static_cast<float>(a[k]), by, sum[i][s][k]));
-                }
-            } else {
+                    for (int k = 0; k < 4; ++k)
+                        sum[i][s][k] = fmaf(static_cast<float>(b[k]), here.by_high[s], fmaf(static_cast<float>(a[k]), here.by[s], sum[i][s][k]));
+                } else {
+                    a = __builtin_amdgcn_mfma_i32_16x16x64_i8(here.high[i], w_high, a, 0, 0, 0);
 #pragma unroll
-                for (int i = 0; i < RT; ++i) {
-                    int4v a = __builtin_amdgcn_mfma_i32_16x16x64_i8(low[i], w_low, int4v{}, 0, 0, 0);
-                    a = __builtin_amdgcn_mfma_i32_16x16x64_i8(high[i], w_high, a, 0, 0, 0);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) sum[i][s][k] = fmaf(static_cast<float>(a[k]), by, sum[i][s][k]);
+                    for (int k = 0; k < 4; ++k) sum[i][s][k] = fmaf(static_cast<float>(a[k]), here.by[s], sum[i][s][k]);
                 }
             }
         }
@@ -238,27 +252,34 @@ __global__ __launch_bounds__(256) void ctc_linear_i4_kernel(LinearI4Args p)
 #pragma unroll
             for (int k = 0; k < 4; ++k) s_sum[wave][16 * i + 4 * (lane / 16) + k][16 * s + lane % 16] = sum[i][s][k];
     __syncthreads();
-    for (int at = threadIdx.x; at < 16 * RT * kColumns; at += 256) {
+    for (int at = threadIdx.x; at < 16 * RT * kColumns; at += kThreads) {
         const int i = at / kColumns, j = at % kColumns, r = s_row[i];
         const int64_t a = static_cast<int64_t>(n0) * 16 + j;
         if (r < 0 || a >= p.A) continue;
         float v = s_sum[0][i][j];
 #pragma unroll
-        for (int o = 1; o < kWaves; ++o) v += s_sum[o][i][j];
+        for (int o = 1; o < WAVES; ++o) v += s_sum[o][i][j];
         static_cast<T*>(p.logits)[static_cast<int64_t>(r) * p.A + a] = narrow<T>(fmaf(v, p.scales[r] * 0.0625f, p.bias ? p.bias[a] : 0.0f));
     }
 }
 
-template <typename T, int RT, int ST> int launch_linear_tiles_of(const LinearI4Args& p, hipStream_t s)
+template <typename T, int RT, int ST, int WAVES> int launch_i4_tile(const LinearI4Args& p, hipStream_t s)
 {
-    const int64_t groups = static_cast<int64_t>(blocks(p.rows, 16 * RT)) * blocks(p.A, 16 * ST);
-    const dim3 grid = spread(static_cast<unsigned>(groups));
-    return p.group == 64 ? launch(ctc_linear_i4_kernel<T, RT, ST, true>, grid, 256, s, p) : launch(ctc_linear_i4_kernel<T, RT, ST, false>, grid, 256, s, p);
+    const dim3 grid = spread(blocks(p.rows, 16 * RT) * blocks(p.A, 16 * ST));
+    return p.group == 64 ? launch(ctc_linear_i4_kernel<T, RT, ST, WAVES, true>, grid, WAVES * kWave, s, p)
+                         : launch(ctc_linear_i4_kernel<T, RT, ST, WAVES, false>, grid, WAVES * kWave, s, p);
 }
 
 template <typename T> int launch_linear_of(const LinearI4Args& p, hipStream_t s)
 {
-    return p.rows <= 16 ? launch_linear_tiles_of<T, 1, 1>(p, s) : launch_linear_tiles_of<T, 4, 4>(p, s);
+    switch (i4_tile(p.rows, p.pitch, p.A)) {
+    case I4Tile::k16x16: return launch_i4_tile<T, 1, 1, 4>(p, s);
+    case I4Tile::k16x16Deep: return launch_i4_tile<T, 1, 1, 16>(p, s);
+    case I4Tile::k32x16: return launch_i4_tile<T, 2, 1, 8>(p, s);
+    case I4Tile::k64x16: return launch_i4_tile<T, 4, 1, 8>(p, s);
+    case I4Tile::k64x32: return launch_i4_tile<T, 4, 2, 4>(p, s);
+    default: return launch_i4_tile<T, 4, 4, 4>(p, s);
+    }
 }
 
 }  // namespace
