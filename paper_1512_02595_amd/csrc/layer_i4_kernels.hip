@@ -156,20 +156,31 @@ __global__ __launch_bounds__(256) void ctc_dequantize_weights_i4_kernel(const ui
     }
 }
 
+// What a wavefront's lanes have written to LDS is there for its other lanes: its accesses are in order, if the compiler leaves them so.
+__device__ __forceinline__ void in_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 typedef int int4v __attribute__((ext_vector_type(4)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 
 // RT by ST tiles of 16 rows by 16 symbols to a workgroup, each of whose wavefronts takes every WAVES-th 128 columns of all of them, straight from memory
 // into the matrix cores, the next ones asked for before these are multiplied; their sums are added in LDS.  A weight's four bits become the upper half
 // of a byte, sixteen times their value: that takes one `and` (and a shift for the lower half) for four weights, and a sixteenth comes into the row's scale.
+// (64 rows by 32 symbols: three wavefronts to a SIMD, by 64 symbols two; 256 x 2048 by 6144 bf16 13.7 us a pass, 16.8.)
 // v_mfma_i32_16x16x64_i8: lane l gives bytes 16 (l / 16) .. of row l % 16 of either operand, and holds rows 4 (l / 16) .. + 3 of column
 // l % 16 of the result.
 template <typename T, int RT, int ST, int WAVES, bool BY_64>
-__global__ __launch_bounds__(WAVES * kWave) void ctc_linear_i4_kernel(LinearI4Args p)
+__global__ __launch_bounds__(WAVES * kWave, RT * ST >= 8 ? 3 : 1) void ctc_linear_i4_kernel(LinearI4Args p)
 {
     constexpr int kColumns = 16 * ST, kThreads = WAVES * kWave;
-    __shared__ float s_sum[WAVES][16 * RT][kColumns];
+    constexpr bool kTurned = RT > 1;                                              // (of one tile of rows the few that count are soon read)
+    constexpr int kSumBytes = WAVES * 16 * RT * kColumns * 4, kRowBytes = kTurned ? WAVES * RT * 16 * kTileColumns : 0;
+    __shared__ int4v s_quads[(kSumBytes > kRowBytes ? kSumBytes : kRowBytes) / 16];
     __shared__ int s_row[16 * RT];
+    float (*const s_sum)[16 * RT][kColumns] = reinterpret_cast<float (*)[16 * RT][kColumns]>(s_quads);
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const unsigned across = static_cast<unsigned>((p.A + kColumns - 1) / kColumns), group = static_cast<unsigned>(group_number());
     const int64_t m0 = static_cast<int64_t>(group / across) * (16 * RT);
@@ -184,9 +195,12 @@ __global__ __launch_bounds__(WAVES * kWave) void ctc_linear_i4_kernel(LinearI4Ar
         w[s] = p.weight_q + tile * tiles * kTileBytes + 16 * lane;
         scale[s] = p.weight_scales + tile * p.groups * 16 + lane % 16;
     }
-    const int8_t* q[RT];
+    // A row's 128 bytes are brought by eight neighbouring lanes (16 rows' same 16 bytes, as the matrix cores take them, are 16 lines of memory to a quarter of a
+    // wavefront: 256 x 2048 by 6144 bf16 17.4 us on the GPU) and turned over in the wavefront's own part of LDS, chunk c of row r at chunk c ^ r % 8.
+    constexpr int kLoads = 2 * RT;
+    const int8_t* q[kLoads];
     struct Columns {
-        int4v low[RT], high[RT], w[ST];
+        int4v q[kLoads], w[ST];
         float by[ST], by_high[ST];
     } here, next;
     const auto weights = [&](int t, Columns& to) {
@@ -200,19 +214,22 @@ __global__ __launch_bounds__(WAVES * kWave) void ctc_linear_i4_kernel(LinearI4Ar
     };
     const auto rows = [&](int t, Columns& to) {
 #pragma unroll
-        for (int i = 0; i < RT; ++i) {
-            __builtin_memcpy(&to.low[i], __builtin_assume_aligned(q[i] + t * kTileColumns, 16), 16);
-            __builtin_memcpy(&to.high[i], __builtin_assume_aligned(q[i] + t * kTileColumns + 64, 16), 16);
-        }
+        for (int i = 0; i < kLoads; ++i)
+            __builtin_memcpy(&to.q[i], __builtin_assume_aligned(q[i] + t * kTileColumns + (kTurned ? 0 : 64 * i), 16), 16);
     };
     // (the weights wait for nothing, the rows for the list)
     if (wave < tiles) weights(wave, next);
+    // One lane asks the list for each row.
+    const int asked = row_at(p.frames, p.rows, m0 + lane % (16 * RT));
+    if (wave == 0 && lane < 16 * RT) s_row[lane] = asked;
 #pragma unroll
-    for (int i = 0; i < RT; ++i) {
-        const int r = row_at(p.frames, p.rows, m0 + 16 * i + lane % 16);
-        if (wave == 0 && lane < 16) s_row[16 * i + lane] = r;
-        q[i] = p.q + static_cast<int64_t>(r < 0 ? 0 : r) * p.pitch + 16 * (lane / 16);          // (what row 0 gives instead is not written)
+    for (int i = 0; i < kLoads; ++i) {
+        const int r = kTurned ? __shfl(asked, 8 * i + lane / 8, kWave) : asked;
+        q[i] = p.q + static_cast<int64_t>(r < 0 ? 0 : r) * p.pitch + 16 * (kTurned ? lane % 8 : lane / 16);          // (what row 0 gives instead is not written)
     }
+    // (in pieces of 16 bytes, eight to a row)
+    const int mine = wave * (kRowBytes / WAVES / 16), to_lds = mine + lane / 8 * 8 + (lane % 8 ^ lane / 8);
+    const int from_low = mine + lane % 16 * 8 + (lane / 16 ^ lane % 8), from_high = mine + lane % 16 * 8 + ((lane / 16 + 4) ^ lane % 8);
     if (wave < tiles) rows(wave, next);
     float4v sum[RT][ST];
 #pragma unroll
@@ -226,25 +243,41 @@ __global__ __launch_bounds__(WAVES * kWave) void ctc_linear_i4_kernel(LinearI4Ar
             rows(t + WAVES, next);
         }
         __builtin_amdgcn_sched_barrier(0);
+        int4v low[RT], high[RT];
+        if constexpr (kTurned) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) s_quads[to_lds + i * 64] = here.q[i];
+            in_order();
+#pragma unroll
+            for (int i = 0; i < RT; ++i) {
+                low[i] = s_quads[from_low + i * 128];
+                high[i] = s_quads[from_high + i * 128];
+            }
+            in_order();
+        } else {
+            low[0] = here.q[0];
+            high[0] = here.q[1];
+        }
 #pragma unroll
         for (int s = 0; s < ST; ++s) {
             const int4v w_low = here.w[s] << 4 & static_cast<int>(0xf0f0f0f0u), w_high = here.w[s] & static_cast<int>(0xf0f0f0f0u);
 #pragma unroll
             for (int i = 0; i < RT; ++i) {
-                int4v a = __builtin_amdgcn_mfma_i32_16x16x64_i8(here.low[i], w_low, int4v{}, 0, 0, 0);
+                int4v a = __builtin_amdgcn_mfma_i32_16x16x64_i8(low[i], w_low, int4v{}, 0, 0, 0);
                 if constexpr (BY_64) {
-                    const int4v b = __builtin_amdgcn_mfma_i32_16x16x64_i8(here.high[i], w_high, int4v{}, 0, 0, 0);
+                    const int4v b = __builtin_amdgcn_mfma_i32_16x16x64_i8(high[i], w_high, int4v{}, 0, 0, 0);
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
                         sum[i][s][k] = fmaf(static_cast<float>(b[k]), here.by_high[s], fmaf(static_cast<float>(a[k]), here.by[s], sum[i][s][k]));
                 } else {
-                    a = __builtin_amdgcn_mfma_i32_16x16x64_i8(here.high[i], w_high, a, 0, 0, 0);
+                    a = __builtin_amdgcn_mfma_i32_16x16x64_i8(high[i], w_high, a, 0, 0, 0);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) sum[i][s][k] = fmaf(static_cast<float>(a[k]), here.by[s], sum[i][s][k]);
                 }
             }
         }
     }
+    if constexpr (kTurned) __syncthreads();                                       // (the sums take the rows' place)
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
@@ -277,8 +310,7 @@ template <typename T> int launch_linear_of(const LinearI4Args& p, hipStream_t s)
     case I4Tile::k16x16Deep: return launch_i4_tile<T, 1, 1, 16>(p, s);
     case I4Tile::k32x16: return launch_i4_tile<T, 2, 1, 8>(p, s);
     case I4Tile::k64x16: return launch_i4_tile<T, 4, 1, 8>(p, s);
-    case I4Tile::k64x32: return launch_i4_tile<T, 4, 2, 4>(p, s);
-    default: return launch_i4_tile<T, 4, 4, 4>(p, s);
+    default: return launch_i4_tile<T, 4, 2, 4>(p, s);
     }
 }
 
