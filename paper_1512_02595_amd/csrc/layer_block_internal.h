@@ -35,13 +35,17 @@ struct RecurrenceArgs {
 constexpr int kRun = 16, kRunBack = 4, kRecurrenceWaves = 8;
 
 // How an utterance's T frames are dealt out in runs, where `places` workgroups would have one tile of channels of one utterance each: one wavefront has
-// few of them; many go in rounds to eight; and where that leaves compute units without work, they go in stretches of whole rounds to several workgroups.
+// few of them (runs of one or four frames where there are no more: 512 x 1 x 4096 bf16 by a run of sixteen 26 us, so 8; 512 x 4 x 2048 16 and 9.6), four
+// or eight more (256 x 16 x 2048 bf16 backward by eight 30 us, by four 21); many go in rounds to eight; and where that leaves compute units without work,
+// they go in stretches of whole rounds to several workgroups (1 x 40000 x 1024 fp32, a thread to a channel 18.6 ms; in as many stretches as make 256
+// workgroups 165, 512 155, 1024 169, 2048 160).
 struct RecurrencePlan {
     int waves, stretches, steps;
 };
 inline RecurrencePlan recurrence_plan(int T, int64_t places, int run)
 {
     if (T <= run) return {1, 1, T};
+    if (T <= 4 * run) return {4, 1, T};
     const int round = run * kRecurrenceWaves, rounds = (T - 1) / round + 1;
     if (places > 256 || rounds == 1) return {kRecurrenceWaves, 1, T};
     const int64_t wanted = 512 / places, most = wanted < rounds ? wanted : rounds;

@@ -17,16 +17,16 @@ template <typename T> __device__ __forceinline__ Eight load_eight(const T* row, 
 {
     Eight e;
     T low[4], high[4];
-    if (col + 68 <= H) {
-        __builtin_memcpy(low, row + col, sizeof(low));
-        __builtin_memcpy(high, row + col + 64, sizeof(high));
-    } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            low[k] = col + k < H ? row[col + k] : narrow<T>(0.0f);
-            high[k] = col + 64 + k < H ? row[col + 64 + k] : narrow<T>(0.0f);
+    const auto four = [&](T (&v)[4], int at) {
+        if (at + 4 <= H) {
+            __builtin_memcpy(v, row + at, sizeof(v));
+            return;
         }
-    }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = at + k < H ? row[at + k] : narrow<T>(0.0f);
+    };
+    four(low, col);
+    four(high, col + 64);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         e.low[k] = widen(low[k]);
@@ -56,7 +56,8 @@ __device__ __forceinline__ uint32_t largest_of_16(uint32_t v)
     return v;
 }
 
-// What rounds a group's values: its largest, lifted where that is tiny (which is exact), and seven over it.
+// What rounds a group's values: its largest, lifted where that is tiny and lowered where it is huge (by powers of two), and seven over it, which is off by
+// less than two units of its last place, so that a quotient is off by less than 2^-19.
 struct Rounding {
     float lift, m, inverse;
     bool finite;
@@ -65,61 +66,107 @@ __device__ __forceinline__ Rounding rounding_of(uint32_t most)
 {
     Rounding r;
     r.finite = most < kInfinity;
-    r.lift = most < 0x20000000u ? 0x1p80f : 1.0f;
+    r.lift = most < 0x20000000u ? 0x1p80f : most >= 0x5f000000u ? 0x1p-40f : 1.0f;
     r.m = __uint_as_float(most) * r.lift;
-    r.inverse = most && r.finite ? static_cast<float>(7.0 / static_cast<double>(r.m)) : 0.0f;
+    r.inverse = most && r.finite ? 7.0f * __builtin_amdgcn_rcpf(r.m) : 0.0f;
     return r;
 }
-__device__ __forceinline__ uint32_t nibble(float v, const Rounding& r)
+// Four values' bits, one in each byte's lower half.  The nearest whole numbers by the quotients; by comparing exactly (level) where one of the four quotients
+// is near the middle between two.
+__device__ __forceinline__ uint32_t nibbles(const float (&v)[4], const Rounding& r)
 {
-    return r.finite ? static_cast<uint32_t>(level<7>(v * r.lift, r.m, r.inverse)) & 15u : 0u;
+    float u[4], t[4];
+    bool near = false;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        u[k] = v[k] * r.lift;
+        const float quotient = u[k] * r.inverse;
+        t[k] = rintf(quotient);
+        near = near || fabsf(quotient - t[k]) > 0.5f - 0x1p-15f;
+    }
+    int q[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) q[k] = static_cast<int>(t[k]);
+    if (near) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) q[k] = level<7>(u[k], r.m, r.inverse);
+    }
+    uint32_t word = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) word |= (static_cast<uint32_t>(q[k]) & 15u) << (8 * k);
+    return r.finite ? word : 0u;
 }
-__device__ __forceinline__ float scale_of(uint32_t most)
+__device__ __forceinline__ float scale_of(uint32_t most) { return most < kInfinity ? __uint_as_float(most) / 7.0f : __uint_as_float(0x7fc00000u); }
+
+constexpr int kTilesAtOnce = 2;
+
+__device__ __forceinline__ void store_tile(uint8_t* tile, int r, int j, const Eight& e, const Rounding& by_low, const Rounding& by_high)
 {
-    return most < kInfinity ? static_cast<float>(static_cast<double>(__uint_as_float(most)) / 7.0) : __uint_as_float(0x7fc00000u);
+    const uint32_t word = nibbles(e.low, by_low) | nibbles(e.high, by_high) << 4;
+    __builtin_memcpy(__builtin_assume_aligned(tile + 256 * (j / 4) + 16 * r + 4 * (j % 4), 4), &word, 4);
 }
 
-// Sixteen rows, and as many columns as a scale has (128 where that is 64), to a workgroup.
+// Groups of 64 or 128 columns: sixteen rows and two tiles of 128 columns to a workgroup (and back, 12000 x 999 bf16: 26.0 us,
+// with one tile 27.3, with four 27.8).
 template <typename T>
 __global__ __launch_bounds__(256) void ctc_quantize_weights_i4_kernel(const T* __restrict__ weights, int A, int H, int group, int groups,
                                                                       int tiles, uint8_t* __restrict__ weight_q,
                                                                       float* __restrict__ weight_scales)
 {
     const int r = threadIdx.x / 16, j = threadIdx.x % 16;
-    const int64_t units = group == 64 ? tiles : groups;
-    const int64_t at = group_number(), row_tile = at / units;
-    const int unit = static_cast<int>(at % units);
-    if (row_tile >= (A + 15) / 16) return;
+    const int64_t at = group_number(), units = (tiles + kTilesAtOnce - 1) / kTilesAtOnce, row_tile = at / units;
+    const int first = static_cast<int>(at % units) * kTilesAtOnce;
     const int64_t a = row_tile * 16 + r;
-    const int reach = group == 64 ? 1 : group / 128, first = unit * reach, last = first + reach < tiles ? first + reach : tiles;
+    if (row_tile * 16 >= A) return;
+    Eight e[kTilesAtOnce] = {};
+#pragma unroll
+    for (int n = 0; n < kTilesAtOnce; ++n)
+        if (a < A) e[n] = load_eight(weights + a * H, (first + n) * 128 + 4 * j, H);
+    uint8_t* const tile = weight_q + (row_tile * tiles + first) * kTileBytes;
+    float* const scales = weight_scales + row_tile * groups * 16 + r;
+#pragma unroll
+    for (int n = 0; n < kTilesAtOnce; ++n) {
+        if (first + n >= tiles) return;
+        uint32_t low = largest_of_16(largest(e[n].low)), high = largest_of_16(largest(e[n].high));
+        if (group != 64) low = high = low > high ? low : high;
+        store_tile(tile + n * kTileBytes, r, j, e[n], rounding_of(low), rounding_of(high));
+        if (j) continue;
+        if (group != 64) {
+            scales[static_cast<int64_t>(first + n) * 16] = scale_of(low);
+            continue;
+        }
+        scales[static_cast<int64_t>(2 * (first + n)) * 16] = scale_of(low);
+        if (2 * (first + n) + 1 < groups) scales[static_cast<int64_t>(2 * (first + n) + 1) * 16] = scale_of(high);
+    }
+}
+
+// Wider ones: sixteen rows and a group to a workgroup, which goes over it twice (the second time in the caches).
+template <typename T>
+__global__ __launch_bounds__(256) void ctc_quantize_weights_i4_wide_kernel(const T* __restrict__ weights, int A, int H, int group, int groups,
+                                                                           int tiles, uint8_t* __restrict__ weight_q,
+                                                                           float* __restrict__ weight_scales)
+{
+    const int r = threadIdx.x / 16, j = threadIdx.x % 16;
+    const int64_t at = group_number(), row_tile = at / groups;
+    const int unit = static_cast<int>(at % groups);
+    const int64_t a = row_tile * 16 + r;
+    if (row_tile * 16 >= A) return;
+    const int reach = group / 128, first = unit * reach, last = first + reach < tiles ? first + reach : tiles;
     const T* const row = weights + a * H;
     Eight e{};
-    uint32_t low = 0, high = 0;
+    uint32_t most = 0;
     for (int t = first; t < last; ++t) {
         if (a < A) e = load_eight(row, t * 128 + 4 * j, H);
-        const uint32_t l = largest(e.low), h = largest(e.high);
-        low = low > l ? low : l;
-        high = high > h ? high : h;
+        const uint32_t l = largest(e.low), h = largest(e.high), here = l > h ? l : h;
+        most = most > here ? most : here;
     }
-    low = largest_of_16(low);
-    high = largest_of_16(high);
-    if (group != 64) low = high = low > high ? low : high;
-    const Rounding by_low = rounding_of(low), by_high = rounding_of(high);
+    most = largest_of_16(most);
+    const Rounding by = rounding_of(most);
     for (int t = first; t < last; ++t) {
-        if (reach > 1 && a < A) e = load_eight(row, t * 128 + 4 * j, H);           // (from the caches)
-        uint32_t word = 0;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) word |= (nibble(e.low[k], by_low) | nibble(e.high[k], by_high) << 4) << (8 * k);
-        __builtin_memcpy(__builtin_assume_aligned(weight_q + ((row_tile * tiles + t) * kTileBytes + 256 * (j / 4) + 16 * r + 4 * (j % 4)), 4), &word, 4);
+        if (a < A) e = load_eight(row, t * 128 + 4 * j, H);
+        store_tile(weight_q + (row_tile * tiles + t) * kTileBytes, r, j, e, by, by);
     }
-    if (j) return;
-    float* const scales = weight_scales + row_tile * groups * 16 + r;
-    if (group == 64) {
-        scales[static_cast<int64_t>(2 * unit) * 16] = scale_of(low);
-        if (2 * unit + 1 < groups) scales[static_cast<int64_t>(2 * unit + 1) * 16] = scale_of(high);
-    } else {
-        scales[static_cast<int64_t>(unit) * 16] = scale_of(low);
-    }
+    if (j == 0) weight_scales[(row_tile * groups + unit) * 16 + r] = scale_of(most);
 }
 
 template <typename T>
@@ -127,32 +174,44 @@ __global__ __launch_bounds__(256) void ctc_dequantize_weights_i4_kernel(const ui
                                                                         int A, int H, int group, int groups, int tiles, T* __restrict__ out)
 {
     const int r = threadIdx.x / 16, j = threadIdx.x % 16;
-    const int64_t at = group_number(), row_tile = at / tiles;
-    const int t = static_cast<int>(at % tiles);
+    const int64_t at = group_number(), units = (tiles + kTilesAtOnce - 1) / kTilesAtOnce, row_tile = at / units;
+    const int first = static_cast<int>(at % units) * kTilesAtOnce;
     const int64_t a = row_tile * 16 + r;
     if (a >= A) return;
-    uint32_t word;
-    __builtin_memcpy(&word, __builtin_assume_aligned(weight_q + at * kTileBytes + 256 * (j / 4) + 16 * r + 4 * (j % 4), 4), 4);
-    const int col = t * 128 + 4 * j;
     const float* const scales = weight_scales + row_tile * groups * 16 + r;
-    const int g_low = col / group, g_high = (col + 64) / group;
-    const float low = scales[static_cast<int64_t>(g_low) * 16], high = g_high < groups ? scales[static_cast<int64_t>(g_high) * 16] : 0.0f;
-    T l[4], h[4];
+    const uint8_t* const tile = weight_q + (row_tile * tiles + first) * kTileBytes + 256 * (j / 4) + 16 * r + 4 * (j % 4);
+    T* const row = out + a * H;
+    uint32_t word[kTilesAtOnce];
+    float low[kTilesAtOnce], high[kTilesAtOnce];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        l[k] = narrow<T>(static_cast<float>(static_cast<int32_t>(word << (28 - 8 * k)) >> 28) * low);
-        h[k] = narrow<T>(static_cast<float>(static_cast<int32_t>(word << (24 - 8 * k)) >> 28) * high);
-    }
-    T* const to = out + a * H + col;
-    if (col + 68 <= H) {
-        store_past<sizeof(l)>(to, l);
-        store_past<sizeof(h)>(to + 64, h);
-        return;
+    for (int n = 0; n < kTilesAtOnce; ++n) {
+        if (first + n >= tiles) break;
+        const int col = (first + n) * 128 + 4 * j, g_low = col / group, g_high = (col + 64) / group;
+        __builtin_memcpy(&word[n], __builtin_assume_aligned(tile + n * kTileBytes, 4), 4);
+        low[n] = g_low < groups ? scales[static_cast<int64_t>(g_low) * 16] : 0.0f;
+        high[n] = g_high < groups ? scales[static_cast<int64_t>(g_high) * 16] : 0.0f;
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        if (col + k < H) to[k] = l[k];
-        if (col + 64 + k < H) to[64 + k] = h[k];
+    for (int n = 0; n < kTilesAtOnce; ++n) {
+        if (first + n >= tiles) break;
+        const int col = (first + n) * 128 + 4 * j;
+        T l[4], h[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            l[k] = narrow<T>(static_cast<float>(static_cast<int32_t>(word[n] << (28 - 8 * k)) >> 28) * low[n]);
+            h[k] = narrow<T>(static_cast<float>(static_cast<int32_t>(word[n] << (24 - 8 * k)) >> 28) * high[n]);
+        }
+        const auto four = [&](const T (&v)[4], int c) {
+            if (c + 4 <= H) {
+                store_past<sizeof(v)>(row + c, v);
+                return;
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (c + k < H) row[c + k] = v[k];
+        };
+        four(l, col);
+        four(h, col + 64);
     }
 }
 
@@ -320,16 +379,23 @@ int launch_quantize_i4(const void* weights, int A, int H, int group, bool bf16, 
 {
     hipStream_t s = static_cast<hipStream_t>(stream);
     const int tiles = pitch_of(H) / kTileColumns, groups = groups_of(H, group);
-    const dim3 grid = spread(blocks(A, 16) * static_cast<unsigned>(group == 64 ? tiles : groups));
-    if (bf16) return launch(ctc_quantize_weights_i4_kernel<bf16_t>, grid, 256, s, static_cast<const bf16_t*>(weights), A, H, group, groups, tiles, weight_q, weight_scales);
-    return launch(ctc_quantize_weights_i4_kernel<float>, grid, 256, s, static_cast<const float*>(weights), A, H, group, groups, tiles, weight_q, weight_scales);
+    const bool wide = group > 128;
+    const dim3 grid = spread(blocks(A, 16) * (wide ? static_cast<unsigned>(groups) : blocks(tiles, kTilesAtOnce)));
+    if (bf16) {
+        const bf16_t* const w = static_cast<const bf16_t*>(weights);
+        return wide ? launch(ctc_quantize_weights_i4_wide_kernel<bf16_t>, grid, 256, s, w, A, H, group, groups, tiles, weight_q, weight_scales)
+                    : launch(ctc_quantize_weights_i4_kernel<bf16_t>, grid, 256, s, w, A, H, group, groups, tiles, weight_q, weight_scales);
+    }
+    const float* const w = static_cast<const float*>(weights);
+    return wide ? launch(ctc_quantize_weights_i4_wide_kernel<float>, grid, 256, s, w, A, H, group, groups, tiles, weight_q, weight_scales)
+                : launch(ctc_quantize_weights_i4_kernel<float>, grid, 256, s, w, A, H, group, groups, tiles, weight_q, weight_scales);
 }
 
 int launch_dequantize_i4(const uint8_t* weight_q, const float* weight_scales, int A, int H, int group, bool bf16, void* out, void* stream)
 {
     hipStream_t s = static_cast<hipStream_t>(stream);
     const int tiles = pitch_of(H) / kTileColumns, groups = groups_of(H, group);
-    const dim3 grid = spread(blocks(A, 16) * static_cast<unsigned>(tiles));
+    const dim3 grid = spread(blocks(A, 16) * blocks(tiles, kTilesAtOnce));
     if (bf16) return launch(ctc_dequantize_weights_i4_kernel<bf16_t>, grid, 256, s, weight_q, weight_scales, A, H, group, groups, tiles, static_cast<bf16_t*>(out));
     return launch(ctc_dequantize_weights_i4_kernel<float>, grid, 256, s, weight_q, weight_scales, A, H, group, groups, tiles, static_cast<float*>(out));
 }

@@ -343,7 +343,10 @@ template <typename T, int V, bool BACK> int launch_channels(RecurrenceArgs p, hi
     const RecurrencePlan plan = recurrence_plan(p.T, tiles * p.B, kFrames);
     p.stretches = plan.stretches;
     p.stretch_steps = plan.steps;
+    if (p.T == 1) return launch_part<T, V, 1, 1, Part::kWhole, BACK>(p, tiles, s);
+    if (p.T <= 4) return launch_part<T, V, 4, 1, Part::kWhole, BACK>(p, tiles, s);
     if (plan.waves == 1) return launch_part<T, V, kFrames, 1, Part::kWhole, BACK>(p, tiles, s);
+    if (plan.waves == 4) return launch_part<T, V, kFrames, 4, Part::kWhole, BACK>(p, tiles, s);
     if (plan.stretches == 1) return launch_part<T, V, kFrames, kRecurrenceWaves, Part::kWhole, BACK>(p, tiles, s);
     const int err = launch_part<T, V, kFrames, kRecurrenceWaves, Part::kSummary, BACK>(p, tiles, s);
     return err ? err : launch_part<T, V, kFrames, kRecurrenceWaves, Part::kStretch, BACK>(p, tiles, s);
