@@ -1,6 +1,6 @@
 // Kernels of the gated linear recurrence (ctc_block.h).
 //
-// A step h = h' + z (c - h') is a map h' -> P h' + S with P = 1 - z, and so is any run of steps: the state behind it is P times the state before it, plus
+// A step h = (1 - z) h' + z c is a map h' -> P h' + S with P = 1 - z (in fp64: exactly), and so is any run of steps: the state behind it is P times the state before it, plus
 // the state that it ends in from zero.  So the frames of an utterance are dealt out in runs of kRun to the wavefronts of a workgroup, whose
 // lanes have channels: each finds its run's P and S from what it has brought into registers, the runs' are exchanged through LDS, and each wavefront
 // goes through its run once more from the state that the runs before it lead to, and writes.  The gradient is the same with the frames the other
@@ -222,8 +222,8 @@ __global__ __launch_bounds__(WAVES * kWave) void ctc_recurrence_kernel(Recurrenc
                 held += hop_states;
             }
         } else {
-            // Steps behind the end: the last one again, with a gate that leaves all as it was.  (The gradient's last step has no frame before it; what is
-            // read in its place is not used.)
+            // Steps behind the end: the last one again, which is not used.  (The gradient's last step has no frame before it; what is read in its place is not
+            // used either.)
             held += first + 1 < at.steps ? hop_states : 0;
 #pragma unroll
             for (int i = 0; i < RUN; ++i) {
@@ -240,8 +240,7 @@ __global__ __launch_bounds__(WAVES * kWave) void ctc_recurrence_kernel(Recurrenc
         Map run[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) run[v] = {1.0, 0.0};
-#pragma unroll
-        for (int i = 0; i < RUN; ++i)
+        const auto step = [&](int i) {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 if constexpr (BACK && PART != Part::kSummary) {
@@ -251,16 +250,27 @@ __global__ __launch_bounds__(WAVES * kWave) void ctc_recurrence_kernel(Recurrenc
                 } else {
                     z[i][v] = share_of<kFine>(widen(g[i].v[v]));
                 }
-                if (first + i >= end) z[i][v] = 0.0f;
-                const double zd = static_cast<double>(z[i][v]);
-                if constexpr (BACK) {
-                    const double whole = run[v].add + static_cast<double>(first + i < end ? widen(d[i].v[v]) : 0.0f);
-                    run[v].add = fma(-zd, whole, whole);
-                } else {
-                    run[v].add = fma(zd, static_cast<double>(widen(c[i].v[v])) - run[v].add, run[v].add);
-                }
-                run[v].keep = fma(-zd, run[v].keep, run[v].keep);
+                const double zd = static_cast<double>(z[i][v]), keep = 1.0 - zd;
+                if constexpr (BACK)
+                    run[v].add = keep * (run[v].add + static_cast<double>(widen(d[i].v[v])));
+                else
+                    run[v].add = fma(keep, run[v].add, zd * static_cast<double>(widen(c[i].v[v])));
+                run[v].keep *= keep;
             }
+        };
+        if (full) {
+#pragma unroll
+            for (int i = 0; i < RUN; ++i) step(i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < RUN; ++i) {
+                if (first + i < end)
+                    step(i);
+                else
+#pragma unroll
+                    for (int v = 0; v < V; ++v) z[i][v] = slope[i][v] = 0.0f;
+            }
+        }
         through_waves<V, WAVES>(s_map[turn], run, lane, wave, carry, before);
         if constexpr (WAVES > 1) turn ^= 1;
         if constexpr (PART == Part::kSummary) {
@@ -274,7 +284,7 @@ __global__ __launch_bounds__(WAVES * kWave) void ctc_recurrence_kernel(Recurrenc
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 forget(z[i][v]);
-                const double zd = static_cast<double>(z[i][v]);
+                const double zd = static_cast<double>(z[i][v]), keep = 1.0 - zd;
                 float here = widen(BACK ? d[i].v[v] : c[i].v[v]);
                 forget(here);
                 if constexpr (BACK) {
@@ -282,9 +292,9 @@ __global__ __launch_bounds__(WAVES * kWave) void ctc_recurrence_kernel(Recurrenc
                     const float w = once(whole);
                     g[i].v[v] = narrow<T>(w * slope[i][v]);
                     c[i].v[v] = narrow<T>(w * z[i][v]);
-                    before[v] = fma(-zd, whole, whole);
+                    before[v] = keep * whole;
                 } else {
-                    before[v] = fma(zd, static_cast<double>(here) - before[v], before[v]);
+                    before[v] = fma(keep, before[v], zd * static_cast<double>(here));
                     g[i].v[v] = narrow<T>(once(before[v]));
                 }
             }

@@ -10,7 +10,7 @@ import contextlib
 import numpy as np
 import torch
 
-from . import ctc, layer, workloads
+from . import block, ctc, layer, workloads
 
 
 def require_gpu() -> torch.device:
@@ -158,7 +158,25 @@ class DeviceMetaBatch:
         return int(self.status.item()), self.costs.cpu().numpy(), self.grads.float().cpu().numpy()
 
 
-class OutputLayer:
+class _Layer:
+    """What the layers share: the call's stream, and which tensors the library may be given.  They have a `device` and a list of `frames`."""
+
+    def _stream(self, stream):
+        return torch.cuda.current_stream(self.device).cuda_stream if stream is None else stream
+
+    def _on(self, stream):
+        """Where torch does its part of a call: on the call's stream."""
+        s = self._stream(stream)
+        if s == torch.cuda.current_stream(self.device).cuda_stream:
+            return contextlib.nullcontext()
+        return torch.cuda.stream(torch.cuda.ExternalStream(s, device=self.device))
+
+    def _here(self, t):
+        """Whether the library may be given the tensor's address."""
+        return t.device == self.frames.device and t.is_contiguous()
+
+
+class OutputLayer(_Layer):
     """The layer that makes CTC's activations, with its states in 8 bits, over the buffers of a minibatch [T, B].
 
     `forward` takes the last layer's states and the residual stream to activations [T, B, A] (`logits`, which may be a
@@ -179,8 +197,7 @@ class OutputLayer:
 
         pitch = layer.row_pitch(H)
         # (the number of rows, then their indices: all of them, until set_lengths says otherwise)
-        self.frames = torch.cat((torch.tensor([self.rows], dtype=torch.int32, device=self.device),
-                                 torch.arange(self.rows, dtype=torch.int32, device=self.device)))
+        self.frames = _all_frames(self.rows, self.device)
         self.norm_weight, self.bias = torch.ones(H, device=self.device), zeros(A)
         self.weight_q, self.weight_scales = zeros(A, pitch, dtype=torch.int8), zeros(A)
         self.sum, self.dsum = zeros(T, B, H, dtype=tdtype), zeros(T, B, H, dtype=tdtype)
@@ -192,20 +209,6 @@ class OutputLayer:
         # (the two gradients need nothing of each other and may be on two streams: a workspace each)
         self.ws = [torch.empty(n + 256, dtype=torch.uint8, device=self.device) for n in self.ws_bytes]
         self.ws_ptr = [(w.data_ptr() + 255) // 256 * 256 for w in self.ws]
-
-    def _stream(self, stream):
-        return torch.cuda.current_stream(self.device).cuda_stream if stream is None else stream
-
-    def _on(self, stream):
-        """Where torch does its part of a call: on the call's stream."""
-        s = self._stream(stream)
-        if s == torch.cuda.current_stream(self.device).cuda_stream:
-            return contextlib.nullcontext()
-        return torch.cuda.stream(torch.cuda.ExternalStream(s, device=self.device))
-
-    def _here(self, t):
-        """Whether the library may be given the tensor's address."""
-        return t.device == self.frames.device and t.is_contiguous()
 
     def _states(self, t):
         assert t.numel() == self.rows * self.H and t.dtype == self.sum.dtype and self._here(t)
@@ -258,3 +261,147 @@ class OutputLayer:
                                 self.frames.data_ptr(), self.rows, self.H, self.dtype, self.dsum.data_ptr(),
                                 self.dnorm_weight.data_ptr(), self.ws_ptr[1], self.ws_bytes[1], self._stream(stream))
         return self.dsum, self.dnorm_weight
+
+
+def _all_frames(rows, device):
+    """The list of all rows: their number, then their indices."""
+    return torch.cat((torch.tensor([rows], dtype=torch.int32, device=device), torch.arange(rows, dtype=torch.int32, device=device)))
+
+
+class _Block(_Layer):
+    """The buffers of a recurrent block that training and streaming both have, over T frames of B utterances, H wide."""
+
+    def __init__(self, T, B, H, dtype, eps, device):
+        self.device = device or require_gpu()
+        self.T, self.B, self.H, self.dtype, self.eps, self.rows = T, B, H, dtype, eps, T * B
+        self.tdtype = torch.float32 if dtype == ctc.DTYPE_F32 else torch.bfloat16
+        self.frames = _all_frames(self.rows, self.device)
+        self.lengths = torch.full((B,), T, dtype=torch.int32, device=self.device)
+        self.weight_after, self.scale = (torch.ones(H, device=self.device) for _ in range(2))
+        self.states, self.sum = (self._zeros(T, B, H) for _ in range(2))
+        self.ws_bytes = block.recurrence_workspace_size(T, B, H)
+        self.ws, self.ws_ptr = self._workspace(self.ws_bytes)
+
+    def _zeros(self, *shape, dtype=None):
+        return torch.zeros(shape, dtype=dtype or self.tdtype, device=self.device)
+
+    def _workspace(self, size):
+        ws = torch.empty(size + 256, dtype=torch.uint8, device=self.device)
+        return ws, (ws.data_ptr() + 255) // 256 * 256
+
+    def _given(self, t, *shape, dtype=None):
+        """A tensor's address, or None; refused if the library would take it for another than it is."""
+        if t is None:
+            return None
+        assert tuple(t.shape) == shape and t.dtype == (dtype or self.tdtype) and self._here(t)
+        return t.data_ptr()
+
+    def _columns(self, t, first):
+        """Address of the columns from `first` H on of a matrix of projections."""
+        return self._given(t, self.T, self.B, 3 * self.H) + first * self.H * t.element_size()
+
+    def set_lengths(self, input_lengths, stream=None):
+        """int32 [B] on the GPU: the frames of this minibatch, for all calls until the next one's (before the first: all)."""
+        s, at = self._stream(stream), self._given(input_lengths, self.B, dtype=torch.int32)
+        layer.pack_frames(at, self.T, self.B, self.frames.data_ptr(), s)
+        with self._on(stream):
+            self.lengths.copy_(input_lengths)
+
+
+class RecurrentBlock(_Block):
+    """A recurrent block in training, over the buffers of a minibatch [T, B]: a gated linear recurrence, then the norm of its states, gated, scaled and
+    added to the residual stream, and the norm before the next block.
+
+    `projections` [T, B, 3 H] is what the caller's matrix product makes of the block's input (the `normed` of the block before): in each row H gates of the
+    recurrence, H candidates, H gates of its output.  Channels from `forward_channels` on run backward in time.  The sum goes on as
+    the residual stream, at last as OutputLayer.forward's states.  Frames behind an utterance's end take no part; their gradients are zeros.
+
+    All of a call's work is on `stream` (a handle; None: torch's current one), whose owner keeps the tensors until it is done.
+    """
+
+    def __init__(self, T, B, H, forward_channels=None, dtype: int = ctc.DTYPE_F32, eps=1e-6, device=None):
+        super().__init__(T, B, H, dtype, eps, device)
+        self.forward_channels = H if forward_channels is None else forward_channels
+        self.weight_before = torch.ones(H, device=self.device)
+        self.normed, self.dstates, self.dresidual = (self._zeros(T, B, H) for _ in range(3))
+        self.dprojections = self._zeros(T, B, 3 * H)
+        self.final, self.dinitial = (self._zeros(B, H, dtype=torch.float32) for _ in range(2))
+        self.dweight_after, self.dscale, self.dweight_before = (self._zeros(H, dtype=torch.float32) for _ in range(3))
+        self.norm_ws_bytes = block.block_norm_workspace_size(self.rows, H)
+        self.norm_ws, self.norm_ws_ptr = self._workspace(self.norm_ws_bytes)
+
+    def set_weights(self, weight_after=None, scale=None, weight_before=None, stream=None):
+        with self._on(stream):
+            for mine, given in ((self.weight_after, weight_after), (self.scale, scale), (self.weight_before, weight_before)):
+                if given is not None:
+                    mine.copy_(given)
+
+    def forward(self, projections, residual=None, initial=None, stream=None):
+        """(sum, its norm) [T, B, H]; `initial` fp32 [B, H] are the states before the first frame, `self.final` those behind the last."""
+        s, H = self._stream(stream), self.H
+        given = self._given(residual, self.T, self.B, H)
+        block.recurrence(self._columns(projections, 0), 3 * H, self.lengths.data_ptr(), self._given(initial, self.B, H, dtype=torch.float32),
+                         self.T, self.B, H, self.forward_channels, self.dtype, self.states.data_ptr(), self.final.data_ptr(),
+                         self.ws_ptr, self.ws_bytes, s)
+        block.block_norm(self.states.data_ptr(), self._columns(projections, 2), 3 * H, given, self.weight_after.data_ptr(),
+                         self.scale.data_ptr(), self.weight_before.data_ptr(), self.eps, self.frames.data_ptr(), self.rows, H, self.dtype,
+                         self.sum.data_ptr(), self.normed.data_ptr(), s)
+        return self.sum, self.normed
+
+    def backward(self, projections, dnormed=None, dsum=None, initial=None, dfinal=None, stream=None):
+        """(gradient of the projections [T, B, 3 H], of the residual [T, B, H]), from those of the norm, of the sum (by other ways), or of both, after the
+        forward call with the same projections and initial states; `self.dinitial`, `dweight_after`, `dscale` and `dweight_before` hold the others."""
+        s, H = self._stream(stream), self.H
+        dn, ds = (self._given(t, self.T, self.B, H) for t in (dnormed, dsum))
+        df, first = (self._given(t, self.B, H, dtype=torch.float32) for t in (dfinal, initial))
+        assert not {dn, ds} & {self.dresidual.data_ptr(), self.dstates.data_ptr()}
+        with self._on(stream):
+            # (The library leaves rows behind an utterance's end as they were, which may be the last minibatch's.  Which they are only the GPU knows.)
+            self.dprojections.zero_()
+            self.dresidual.zero_()
+        block.block_norm_backward(dn, ds, self.states.data_ptr(), self._columns(projections, 2), 3 * H, self.sum.data_ptr(),
+                                  self.weight_after.data_ptr(), self.scale.data_ptr(), self.weight_before.data_ptr(), self.eps,
+                                  self.frames.data_ptr(), self.rows, H, self.dtype, self.dstates.data_ptr(), self._columns(self.dprojections, 2),
+                                  self.dresidual.data_ptr(), self.dweight_after.data_ptr(), self.dscale.data_ptr(),
+                                  self.dweight_before.data_ptr(), self.norm_ws_ptr, self.norm_ws_bytes, s)
+        block.recurrence_backward(self.dstates.data_ptr(), df, self._columns(projections, 0), 3 * H, self.states.data_ptr(),
+                                  self.lengths.data_ptr(), first, self.T, self.B, H, self.forward_channels, self.dtype,
+                                  self._columns(self.dprojections, 0), self.dinitial.data_ptr(), self.ws_ptr, self.ws_bytes, s)
+        return self.dprojections, self.dresidual
+
+
+class StreamingBlock(_Block):
+    """A recurrent block (forward in time) for T frames at a time of B streams, with the weights of its projections [3 H, H] in 4 bits: norm to 8 bits,
+    product, recurrence from the states that the call before left, norm, gate, scale and residual.  Streams whose length is set to 0 wait: their rows and
+    states stay."""
+
+    def __init__(self, B, H, T=1, group=128, dtype: int = ctc.DTYPE_F32, eps=1e-6, device=None):
+        super().__init__(T, B, H, dtype, eps, device)
+        self.group, self.weight = group, torch.ones(H, device=self.device)
+        sizes = block.weights_i4_sizes(3 * H, H, group)
+        self.weight_q, self.weight_scales = self._zeros(sizes[0], dtype=torch.uint8), self._zeros(sizes[1] // 4, dtype=torch.float32)
+        self.q, self.scales = self._zeros(self.rows, layer.row_pitch(H), dtype=torch.int8), self._zeros(self.rows, dtype=torch.float32)
+        self.projections, self.carried = self._zeros(T, B, 3 * H), self._zeros(B, H, dtype=torch.float32)
+
+    def set_weights(self, weight, norm_weight=None, weight_after=None, scale=None, stream=None):
+        """fp32 weights [3 H, H] to 4 bits, and copies of the others: once per recogniser."""
+        block.quantize_weights_i4(self._given(weight, 3 * self.H, self.H, dtype=torch.float32), 3 * self.H, self.H, self.group, ctc.DTYPE_F32,
+                                  self.weight_q.data_ptr(), self.weight_scales.data_ptr(), self._stream(stream))
+        with self._on(stream):
+            for mine, given in ((self.weight, norm_weight), (self.weight_after, weight_after), (self.scale, scale)):
+                if given is not None:
+                    mine.copy_(given)
+
+    def forward(self, residual, stream=None):
+        """The residual stream [T, B, H] behind the block; the states go on to the next call."""
+        s, H, frames = self._stream(stream), self.H, self.frames.data_ptr()
+        x = self._given(residual, self.T, self.B, H)
+        layer.rms_norm_i8(x, None, self.weight.data_ptr(), self.eps, frames, self.rows, H, self.dtype, None, self.q.data_ptr(),
+                          self.scales.data_ptr(), s)
+        block.linear_i4(self.q.data_ptr(), self.scales.data_ptr(), self.weight_q.data_ptr(), self.weight_scales.data_ptr(), self.group, None,
+                        frames, self.rows, H, 3 * H, self.dtype, self.projections.data_ptr(), s)
+        block.recurrence(self._columns(self.projections, 0), 3 * H, self.lengths.data_ptr(), self.carried.data_ptr(), self.T, self.B, H, H,
+                         self.dtype, self.states.data_ptr(), self.carried.data_ptr(), self.ws_ptr, self.ws_bytes, s)
+        block.block_norm(self.states.data_ptr(), self._columns(self.projections, 2), 3 * H, x, self.weight_after.data_ptr(),
+                         self.scale.data_ptr(), None, self.eps, frames, self.rows, H, self.dtype, self.sum.data_ptr(), None, s)
+        return self.sum

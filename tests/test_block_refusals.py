@@ -126,6 +126,8 @@ def test_sizes_and_types(name):
             assert status(name, forward_channels=-1) == INVALID and status(name, forward_channels=101) == INVALID
         if k == "workspace_bytes" and name == "block_norm_backward":
             assert status(name, workspace_bytes=block.block_norm_workspace_size(200, 100) - 1) == SMALL
+        elif k == "workspace_bytes":
+            assert status(name, workspace_bytes=block.recurrence_workspace_size(500, 4, 100) - 1) == SMALL
     if "B" in CALLS[name]:
         assert status(name, B=65536) == UNSUPPORTED
         assert status(name, T=1 << 20, B=1 << 11) == UNSUPPORTED

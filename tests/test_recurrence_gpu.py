@@ -142,3 +142,236 @@ def test_gradient(T, B, H, more, forward, dtype, kind):
     c = Call(T, B, H, dtype, kind, 2 * H + more, forward, carried=kind != "all" or T % 2 == 1, slow=T > 200)
     c.backward_call()
     c.check_backward()
+
+
+# ---- what may be done with the calls ----------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T, B, H, forward", [(1, 3, 200, 200), (40, 5, 130, 60), (300, 2, 128, 128), (5000, 1, 96, 48)])
+def test_states_carried_in_place(T, B, H, forward, dtype):
+    """final_states in initial's place, dinitial in dfinal's: also where several workgroups share an utterance."""
+    say("in place", T, B, H, forward, dtype)
+    c = Call(T, B, H, dtype, "some", None, forward)
+    place = put(c.initial, torch.float32)
+    block.recurrence(c.inputs.t.data_ptr(), c.pitch, pointer(c.lengths), place.t.data_ptr(), T, B, H, forward, dtype,
+                     Guarded((T, B, H), c.tt).t.data_ptr(), place.t.data_ptr(), c.ws_at, c.ws_bytes, stream())
+    c.forward_call()
+    c.check_forward()
+    assert torch.equal(place.t, c.final.t) and place.intact()
+    place = put(c.dfinal, torch.float32)
+    c.backward_call()
+    c.check_backward()
+    block.recurrence_backward(c.d[0].t.data_ptr(), place.t.data_ptr(), c.inputs.t.data_ptr(), c.pitch, c.d[2].t.data_ptr(), pointer(c.lengths),
+                              c.initial_dev.t.data_ptr(), T, B, H, forward, dtype, Guarded((T, B, c.pitch), c.tt).t.data_ptr(),
+                              place.t.data_ptr(), c.ws_at, c.ws_bytes, stream())
+    torch.cuda.synchronize()
+    assert torch.equal(place.t, c.dinitial.t) and place.intact()
+
+
+def test_without_last_states():
+    say("no last states")
+    for T in (1, 60, 700):
+        c = Call(T, 2, 70, F32, "some")
+        c.forward_call()
+        states = Guarded((T, 2, 70), c.tt)
+        block.recurrence(c.inputs.t.data_ptr(), c.pitch, pointer(c.lengths), c.initial_dev.t.data_ptr(), T, 2, 70, 70, F32, states.t.data_ptr(), None,
+                         c.ws_at, c.ws_bytes, stream())
+        c.backward_call()
+        dinputs = Guarded((T, 2, c.pitch), c.tt)
+        block.recurrence_backward(c.d[0].t.data_ptr(), c.d[1].t.data_ptr(), c.inputs.t.data_ptr(), c.pitch, c.d[2].t.data_ptr(), pointer(c.lengths),
+                                  c.initial_dev.t.data_ptr(), T, 2, 70, 70, F32, dinputs.t.data_ptr(), None, c.ws_at, c.ws_bytes, stream())
+        torch.cuda.synchronize()
+        assert torch.equal(states.raw, c.states.raw) and torch.equal(dinputs.raw, c.dinputs.raw)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shift", [2, 4, 6, 10])
+def test_alignments(shift, dtype):
+    """Inputs that begin anywhere their type may, with rows of odd lengths."""
+    if dtype == F32 and shift % 4:
+        pytest.skip("no alignment of a float")
+    say("alignment", shift, dtype)
+    for H, pitch in ((101, 205), (64, 129), (2, 5), (3, 6)):
+        c = Call(50, 3, H, dtype, "some", pitch, H // 2, shift=shift)
+        c.forward_call()
+        c.check_forward()
+        c.backward_call()
+        c.check_backward()
+
+
+@pytest.mark.parametrize("T, at", [(30, 7), (30, 29), (300, 0), (300, 143), (300, 299), (4000, 2000)])
+def test_values_that_are_not_finite(T, at):
+    """A gate of infinite size is 0 or 1; an infinity or a NaN stays in its channel, behind its frame (the gradient: before it)."""
+    say("not finite", T, at)
+    c = Call(T, 1, 64, F32, "all", carried=True)
+    c.forward_call()
+    clean = c.states.t.clone()
+    c.backward_call()
+    clean_back = c.dinputs.t.clone()
+    inputs = c.inputs.t
+    inputs[at, 0, 3], inputs[at, 0, 5], inputs[at, 0, 64 + 9], inputs[at, 0, 11], inputs[at, 0, 64 + 13] = 1e30, -float("inf"), float("inf"), float("nan"), float("nan")
+    c.forward_call()
+    torch.cuda.synchronize()
+    got, before = c.states.t[:, 0], c.initial_dev.t[0] if at == 0 else clean[at - 1, 0]
+    assert float(got[at, 3]) == float(inputs[at, 0, 64 + 3]) and float(got[at, 5]) == float(before[5])
+    assert bool(torch.isinf(got[at:, 9]).all()) and float(c.final.t[0, 9]) == float("inf")
+    assert bool(torch.isnan(got[at:, [11, 13]]).all()) and bool(torch.isnan(c.final.t[0, [11, 13]]).all())
+    assert torch.equal(got[:at], clean[:at, 0])
+    untouched = [k for k in range(64) if k not in (3, 5, 9, 11, 13)]
+    assert torch.equal(got[:, untouched], clean[:, 0, untouched])
+    grads = c.d[0].t
+    c.backward_call()
+    torch.cuda.synchronize()
+    assert torch.equal(c.dinputs.t[:, 0, untouched], clean_back[:, 0, untouched])
+    # a NaN in a gate makes the gradients of its channel NaNs from its frame back, one in a candidate those of that frame's gate only
+    assert bool(torch.isnan(c.dinputs.t[:at + 1, 0, 11]).all()) and torch.equal(c.dinputs.t[at + 1:, 0, 11], clean_back[at + 1:, 0, 11])
+    assert bool(torch.isnan(c.dinputs.t[at, 0, 13])) and torch.equal(c.dinputs.t[:at, 0, 13], clean_back[:at, 0, 13])
+    assert torch.equal(c.dinputs.t[:, 0, 64 + 13], clean_back[:, 0, 64 + 13])
+    assert grads is not c.d[0].t
+
+
+def test_gates_of_every_size():
+    """z and 1 - z are good relative to themselves: slow channels forget what they should."""
+    say("gates")
+    g = torch.cat((torch.linspace(-90, 90, 4001), torch.tensor([0.0, -0.0, 1e-30, -1e-30, 150.0, -150.0, 3e38, -3e38])))
+    H = g.numel()
+    for dtype in TYPES:
+        gates = g.to(torch_type(dtype)).float()
+        inputs = torch.cat((gates, torch.ones(H)))[None].to(torch_type(dtype)).cuda()
+        states, final = torch.empty(1, H, dtype=inputs.dtype, device="cuda"), torch.empty(1, H, device="cuda")
+        block.recurrence(inputs.data_ptr(), 2 * H, None, None, 1, 1, H, H, dtype, states.data_ptr(), final.data_ptr(), None, 0, stream())
+        torch.cuda.synchronize()
+        z = ref.sigmoid(gates.double())[0]
+        off = (final.cpu().double()[0] - z).abs() / ((ref.gate_error(gates, dtype == F32) + HALF) * z + 2.0 ** -125)
+        say("   %.3f of what is allowed" % float(off.max()))
+        assert float(off.max()) <= 1
+
+
+def test_refuses_a_small_workspace():
+    size = block.recurrence_workspace_size(1000, 2, 64)
+    assert size > 0
+    for call in ("recurrence", "recurrence_backward"):
+        c = Call(1000, 2, 64, F32, "all")
+        c.ws_bytes -= 1
+        with pytest.raises(ctc.CTCError):
+            c.forward_call() if call == "recurrence" else c.backward_call()
+
+
+@pytest.mark.parametrize("T, B, H, forward", [(1, 4, 256, 256), (60, 3, 100, 50), (500, 40, 128, 64), (3000, 1, 64, 64)])
+def test_replays_of_a_captured_call(T, B, H, forward):
+    """Lengths, inputs and states are read afresh; two graphs that share a workspace, replayed in turn on one stream, do not disturb each other."""
+    say("graphs", T, B, H)
+    calls = [Call(T, B, H, F32, "some", None, forward, seed=s) for s in (1, 2)]
+    for c in calls:                                      # (a workspace for both)
+        c.ws, c.ws_at = calls[0].ws, calls[0].ws_at
+        c.forward_call()
+        c.backward_call()
+    torch.cuda.synchronize()
+    graphs = []
+    side = torch.cuda.Stream()
+    for c in calls:
+        g = torch.cuda.CUDAGraph()
+        args = (c.initial_dev, c.states, c.final, c.d, c.dinputs, c.dinitial)
+        with torch.cuda.graph(g, stream=side):
+            s = torch.cuda.current_stream().cuda_stream
+            block.recurrence(c.inputs.t.data_ptr(), c.pitch, c.lengths.data_ptr(), args[0].t.data_ptr(), T, B, H, forward, F32, args[1].t.data_ptr(),
+                             args[2].t.data_ptr(), c.ws_at, c.ws_bytes, s)
+            block.recurrence_backward(args[3][0].t.data_ptr(), args[3][1].t.data_ptr(), c.inputs.t.data_ptr(), c.pitch, args[3][2].t.data_ptr(),
+                                      c.lengths.data_ptr(), args[0].t.data_ptr(), T, B, H, forward, F32, args[4].t.data_ptr(),
+                                      args[5].t.data_ptr(), c.ws_at, c.ws_bytes, s)
+        graphs.append(g)
+    for turn in range(4):
+        for c, g in zip(calls, graphs):
+            want = [t.t.clone() for t in (c.states, c.final, c.dinputs, c.dinitial)]
+            for t in (c.states, c.final, c.dinputs, c.dinitial):
+                t.t.fill_(7.0)
+            eager = Call(T, B, H, F32, "some", None, forward, seed=9)         # (the program's own work in between)
+            eager.forward_call()
+            torch.cuda.synchronize()
+            g.replay()
+            torch.cuda.synchronize()
+            there = c.counts.cuda()
+            assert torch.equal(c.states.t[there], want[0][there]) and torch.equal(c.final.t, want[1])
+            assert torch.equal(c.dinputs.t[there], want[2][there]) and torch.equal(c.dinitial.t, want[3])
+    # other contents in the same buffers
+    c = calls[0]
+    c.lengths.copy_(calls[1].lengths)
+    c.inputs.t.copy_(calls[1].inputs.t)
+    c.initial_dev.t.copy_(calls[1].initial_dev.t)
+    graphs[0].replay()
+    torch.cuda.synchronize()
+    there = calls[1].counts.cuda()
+    assert torch.equal(c.states.t[there], calls[1].states.t[there]) and torch.equal(c.final.t, calls[1].final.t)
+
+
+def test_calls_at_once():
+    """Two streams, each with its own outputs and workspace, from two threads."""
+    import threading
+    say("two streams")
+    calls = [Call(2000, 2, 200, F32, "some", seed=s) for s in (3, 4)]
+    for c in calls:
+        c.forward_call()
+        c.backward_call()
+    torch.cuda.synchronize()
+    want = [[t.t.clone() for t in (c.states, c.final, c.dinputs, c.dinitial)] for c in calls]
+    errors = []
+
+    def work(c):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(20):
+                    c.forward_call()
+                    c.backward_call()
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:                                                # noqa: BLE001 (told to the test)
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(c,)) for c in calls]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not errors
+    for c, w in zip(calls, want):
+        there = c.counts.cuda()
+        assert torch.equal(c.states.t[there], w[0][there]) and torch.equal(c.final.t, w[1])
+        assert torch.equal(c.dinputs.t[there], w[2][there]) and torch.equal(c.dinitial.t, w[3])
+
+
+def test_beyond_2_31_elements():
+    """More than 2^31 elements of inputs and of states: the last utterances and channels are those of a call of their own."""
+    T, B, H = 1500, 1000, 1536
+    say("beyond 2^31", T * B * H)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    inputs = torch.empty(T, B, 2 * H, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    states, final = torch.empty(T, B, H, dtype=torch.bfloat16, device="cuda"), torch.empty(B, H, device="cuda")
+    lengths = torch.full((B,), T, dtype=torch.int32, device="cuda")
+    lengths[-1] = T - 3
+    block.recurrence(inputs.data_ptr(), 2 * H, lengths.data_ptr(), None, T, B, H, H - 64, BF16, states.data_ptr(), final.data_ptr(), *workspace(T, B, H), stream())
+    torch.cuda.synchronize()
+    part = inputs[:, -2:].contiguous()
+    ps, pf = torch.zeros(T, 2, H, dtype=torch.bfloat16, device="cuda"), torch.empty(2, H, device="cuda")
+    block.recurrence(part.data_ptr(), 2 * H, lengths[-2:].data_ptr(), None, T, 2, H, H - 64, BF16, ps.data_ptr(), pf.data_ptr(), *workspace(T, 2, H), stream())
+    torch.cuda.synchronize()
+    # (two ways to deal the frames out: the states agree but for fp64's roundings, which now and then are the other side of a bf16's middle)
+    assert float((states[:T - 3, -2:].float() - ps[:T - 3].float()).abs().max()) <= 2.0 ** -7 * float(ps.abs().max())
+    assert torch.allclose(final[-2:], pf, rtol=0, atol=2.0 ** -23 * float(pf.abs().max()))
+    dinputs, d0 = torch.empty_like(inputs), torch.empty(B, H, device="cuda")
+    block.recurrence_backward(states.data_ptr(), None, inputs.data_ptr(), 2 * H, states.data_ptr(), lengths.data_ptr(), None, T, B, H, H - 64, BF16,
+                              dinputs.data_ptr(), d0.data_ptr(), *workspace(T, B, H), stream())
+    torch.cuda.synchronize()
+    ps.copy_(states[:, -2:])
+    pd, p0 = torch.empty_like(part), torch.empty(2, H, device="cuda")
+    block.recurrence_backward(ps.data_ptr(), None, part.data_ptr(), 2 * H, ps.data_ptr(), lengths[-2:].data_ptr(), None, T, 2, H, H - 64, BF16,
+                              pd.data_ptr(), p0.data_ptr(), *workspace(T, 2, H), stream())
+    torch.cuda.synchronize()
+    assert float((dinputs[:T - 3, -2:].float() - pd[:T - 3].float()).abs().max()) <= 2.0 ** -7 * float(pd[:T - 3].abs().max())
+    assert torch.allclose(d0[-2:], p0, rtol=0, atol=2.0 ** -22 * float(p0.abs().max()))
+
+
+def workspace(T, B, H):
+    size = block.recurrence_workspace_size(T, B, H)
+    ws = torch.empty(size + 256, dtype=torch.uint8, device="cuda")
+    workspace.kept = ws                                  # (until the next one: the calls above are waited for)
+    return (ws.data_ptr() + 255) // 256 * 256, size
