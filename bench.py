@@ -153,6 +153,9 @@ def main():
                     help="grad: cost + gradient (headline); loss: cost only; align: most probable alignment; layer: grad with the "
                          "output layer's forward pass and weights' gradient in 8 bits")
     ap.add_argument("--width", type=int, default=2048, help="--mode layer: width of a state")
+    ap.add_argument("--blocks", type=int, default=0,
+                    help="--mode layer: recurrent blocks under the output layer, forward and backward (their projections are given, as "
+                         "the matrix products of a network would leave them; no product is timed)")
     ap.add_argument("--metadata", choices=("host", "device"), default="host",
                     help="device: ctc_loss_and_grad_device (lengths and labels resident on the GPU, workspace "
                          "sized by bounds)")
@@ -244,7 +247,7 @@ def main():
         dbs = [harness.DeviceBatch(b, dtype, dev, poison=False) for b in batches]
         if args.mode == "layer":
             torch.manual_seed(workloads.BASE_SEED)
-            layers = {}
+            layers, stacks = {}, {}
             for d in dbs:
                 b = d.batch
                 out = harness.OutputLayer(b.T, b.B, args.width, b.A, dtype, logits=d.x, device=dev)
@@ -252,14 +255,23 @@ def main():
                 lengths = torch.from_numpy(np.ascontiguousarray(b.input_lengths, dtype=np.int32)).to(dev)
                 states = [torch.randn(b.T, b.B, args.width, device=dev).to(d.x.dtype) for _ in range(2)]
                 layers[id(d)] = (out, lengths, *states)
+                stacks[id(d)] = [(harness.RecurrentBlock(b.T, b.B, args.width, dtype=dtype, device=dev),
+                                  torch.randn(b.T, b.B, 3 * args.width, device=dev).to(d.x.dtype)) for _ in range(args.blocks)]
             args.profile_steps = 0             # (the per-launch times are the CTC call's alone: --mode grad)
 
             def step(d, stream, kernel_ms=None):
                 out, lengths, states, residual = layers[id(d)]
                 out.set_lengths(lengths, stream)
+                for recurrent, projections in stacks[id(d)]:
+                    recurrent.set_lengths(lengths, stream)
+                    residual, _ = recurrent.forward(projections, residual, stream=stream)
                 out.forward(states, residual, stream)
                 d.run(stream)
                 out.weight_gradient(d.grads, stream)
+                if stacks[id(d)]:              # (the gradient of the norm's output is the product that is not timed: states stand for it)
+                    dsum, _ = out.norm_backward(states, stream=stream)
+                    for recurrent, projections in reversed(stacks[id(d)]):
+                        _, dsum = recurrent.backward(projections, None, dsum, stream=stream)
         else:
             step = {"grad": harness.DeviceBatch.run, "loss": harness.DeviceBatch.run_loss,
                     "align": harness.DeviceBatch.run_best_path}[args.mode]
@@ -297,11 +309,17 @@ def main():
     if args.mode == "layer":
         layer_bytes = sum(t.numel() * t.element_size() for out, *given in layers.values()
                           for t in (*given, out.sum, out.q, out.scales, out.weight_q, out.dweight, *out.ws))
+        layer_bytes += sum(t.numel() * t.element_size() for stack in stacks.values() for recurrent, projections in stack
+                           for t in (projections, recurrent.states, recurrent.sum, recurrent.normed, recurrent.dstates, recurrent.dprojections,
+                                     recurrent.dresidual))
     if args.mode in ("grad", "layer"):
         compulsory = float(np.mean([b.compulsory_bytes(elem) for b in batches]))
         if args.mode == "layer":    # states and residual once, their sum written, rows in 8 bits written and read twice, weights read, their gradient written,
             #                         activations written and their gradient read
             compulsory += frames * args.width * (3 * elem + 3) + batches[0].A * args.width * 5 + 2 * frames * batches[0].A * elem
+            # the recurrence's 3 tensors and its gradient's 6, the norms' 5 and their gradient's 7 (no gradient of a norm that is not used); the output norm's
+            # gradient's 3
+            compulsory += frames * args.width * elem * (21 * args.blocks + (3 if args.blocks else 0))
     else:       # the valid activations once; the alignment also writes one int32 per frame of the tensor
         compulsory = float(np.mean([b.frames * b.A * elem for b in batches]))
         if args.mode == "align":
@@ -382,6 +400,7 @@ def main():
                    % (args.config, batches[0].name, B, batches[0].A, batches[0].T, len(batches)),
                    "mode": args.mode, "metadata": args.metadata, "graph": bool(args.graph),
                    **({"width": args.width} if args.mode == "layer" else {}),
+                   **({"blocks": args.blocks} if args.mode == "layer" and args.blocks else {}),
                    "sequential_chains": bool(args.sequential_chains)},
         "activation_frames_per_s": round(frames / (ms_per_step * 1e-3), 1),
         "hbm_roofline_frac_end_to_end": round(compulsory / (ms_per_step * 1e-3) / 1e9 / HBM_PEAK_GBS, 5),
