@@ -118,6 +118,23 @@ __device__ __forceinline__ void through_waves(Map (*s_map)[V][kWave], const Map 
     }
 }
 
+// The round's map, from the wavefronts' (of which each is given its own).
+template <int V, int WAVES> __device__ __forceinline__ void of_waves(Map (*s_map)[V][kWave], Map (&map)[V], int lane, int wave)
+{
+#pragma unroll
+    for (int v = 0; v < V; ++v) s_map[wave][v][lane] = map[v];
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        map[v] = {1.0, 0.0};
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const Map m = s_map[w][v][lane];
+            map[v] = {map[v].keep * m.keep, fma(m.keep, map[v].add, m.add)};
+        }
+    }
+}
+
 // The state before this stretch: the initial one through the maps of the stretches before, a share of which each wavefront puts together.
 template <int V, int WAVES>
 __device__ __forceinline__ void through_stretches(const RecurrenceArgs& p, const Place& at, Map (*s_map)[V][kWave], int lane, int wave, double (&carry)[V])
@@ -187,10 +204,7 @@ __global__ __launch_bounds__(WAVES * kWave) void ctc_recurrence_kernel(Recurrenc
         carry_from<V>(before_all, channel, carry);
     else {
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            carry[v] = 0.0;
-            all[v] = {1.0, 0.0};
-        }
+        for (int v = 0; v < V; ++v) all[v] = {1.0, 0.0};
     }
     // Bytes from a step's row to that of the kernel's next step, rows of the inputs and of states; a row's begin is the same for all lanes.
     constexpr bool kFine = sizeof(T) == 4;
@@ -198,7 +212,10 @@ __global__ __launch_bounds__(WAVES * kWave) void ctc_recurrence_kernel(Recurrenc
     const int64_t hop_rows = at.backwards != BACK ? -p.B : p.B, hop = hop_rows * row_bytes, hop_states = hop_rows * state_bytes;
     const uint32_t at_gate = static_cast<uint32_t>(at.k) * sizeof(T), at_candidate = static_cast<uint32_t>(p.H + at.k) * sizeof(T);
     int turn = 0;
-    for (int round = begin; round < end; round += WAVES * RUN) {
+    constexpr int kRound = WAVES * RUN;
+    for (int from = begin; from < end; from += kRound) {
+        // A summary goes from the stretch's last round to its first, with which the launch behind it begins: what was read last is still in the caches.
+        const int round = PART == Part::kSummary ? begin + (end - 1 - from) / kRound * kRound : from;
         const int first = round + wave * RUN;
         Some<T, V> g[RUN], c[RUN], d[RUN], h[RUN];
         const bool full = first + RUN <= end && (!BACK || first + RUN < at.steps);
@@ -271,14 +288,15 @@ __global__ __launch_bounds__(WAVES * kWave) void ctc_recurrence_kernel(Recurrenc
                     for (int v = 0; v < V; ++v) z[i][v] = slope[i][v] = 0.0f;
             }
         }
-        through_waves<V, WAVES>(s_map[turn], run, lane, wave, carry, before);
-        if constexpr (WAVES > 1) turn ^= 1;
         if constexpr (PART == Part::kSummary) {
-            // (the carry of a summary begins with zero; the product is every wavefront's own to keep)
+            of_waves<V, WAVES>(s_map[turn], run, lane, wave);
+            turn ^= 1;
 #pragma unroll
-            for (int v = 0; v < V; ++v) all[v].keep *= run[v].keep;
+            for (int v = 0; v < V; ++v) all[v] = {all[v].keep * run[v].keep, fma(all[v].keep, run[v].add, all[v].add)};
             continue;
         }
+        through_waves<V, WAVES>(s_map[turn], run, lane, wave, carry, before);
+        if constexpr (WAVES > 1) turn ^= 1;
 #pragma unroll
         for (int i = 0; i < RUN; ++i)
 #pragma unroll
@@ -315,21 +333,6 @@ __global__ __launch_bounds__(WAVES * kWave) void ctc_recurrence_kernel(Recurrenc
         }
     }
     if constexpr (PART == Part::kSummary) {
-        // The stretch's product: the wavefronts' own, multiplied.
-        if constexpr (WAVES > 1) {
-            __syncthreads();
-#pragma unroll
-            for (int v = 0; v < V; ++v) s_map[0][wave][v][lane] = all[v];
-            __syncthreads();
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                all[v].keep = 1.0;
-#pragma unroll
-                for (int w = 0; w < WAVES; ++w) all[v].keep *= s_map[0][w][v][lane].keep;
-            }
-        }
-#pragma unroll
-        for (int v = 0; v < V; ++v) all[v].add = carry[v];
         if (wave == 0) leave_map<V>(p, at, before_all, all);
         return;
     }
