@@ -9,7 +9,7 @@ namespace {
 
 // z = 1 / (1 + exp(-g)), 1 - z and their product, each to a few units of its own last place: from t = exp(-|g|), which does not overflow, all are
 // quotients without a difference.  An infinite g gives 0 and 1, a NaN NaNs.  The exponent is a product; its rounding would be an error of |g| half
-// steps of t, so for FINE, where results are in 32 bits, the rest that the product leaves is made good (five operations more).
+// steps of t, so for FINE, where results are in 32 bits, the rest that the product leaves is made good (five operations more), and the reciprocal's.
 struct Gate {
     float z, stays, both;
 };
@@ -24,8 +24,10 @@ template <bool FINE> __device__ __forceinline__ float exp_of_minus(float a)     
 }
 template <bool FINE> __device__ __forceinline__ Gate gate_of(float g)
 {
-    const float t = exp_of_minus<FINE>(fabsf(g));
-    const float large = __builtin_amdgcn_rcpf(1.0f + t), small = t * large;
+    const float t = exp_of_minus<FINE>(fabsf(g)), sum = 1.0f + t;
+    float large = __builtin_amdgcn_rcpf(sum);
+    if constexpr (FINE) large = fmaf(fmaf(-sum, large, 1.0f), large, large);        // (a step of Newton's method: to half a unit)
+    const float small = t * large;
     const bool up = g >= 0.0f;
     return {up ? large : small, up ? small : large, large * small};
 }

@@ -307,9 +307,14 @@ __global__ __launch_bounds__(WAVES * kWave) void ctc_recurrence_kernel(Recurrenc
                 forget(here);
                 if constexpr (BACK) {
                     const double whole = before[v] + static_cast<double>(here);
-                    const float w = once(whole);
-                    g[i].v[v] = narrow<T>(w * slope[i][v]);
-                    c[i].v[v] = narrow<T>(w * z[i][v]);
+                    if constexpr (kFine) {
+                        g[i].v[v] = narrow<T>(static_cast<float>(whole * static_cast<double>(slope[i][v])));
+                        c[i].v[v] = narrow<T>(static_cast<float>(whole * zd));
+                    } else {
+                        const float w = once(whole);
+                        g[i].v[v] = narrow<T>(w * slope[i][v]);
+                        c[i].v[v] = narrow<T>(w * z[i][v]);
+                    }
                     before[v] = keep * whole;
                 } else {
                     before[v] = fma(keep, before[v], zd * static_cast<double>(here));
