@@ -2,7 +2,7 @@
 """Benchmark of the batched CTC cost + gradient on one MI355X.
 
     python bench.py [--gpus 1] [--steps K] [--warmup W] [--config 1] [--dtype f32|bf16]
-                    [--mode grad|loss|align|layer]
+                    [--mode grad|loss|align|layer [--blocks N]]
 
 A step is one ctc_loss_and_grad call (host launcher + all kernels) over one synthetic
 minibatch whose activations already sit in HBM.  The default workload is the English-shaped
@@ -11,7 +11,9 @@ per-GPU minibatch (config index 1: B=64, A=29, T<=750).  Prints one JSON line.
 alignment (ctc_best_path); the default, grad, is the headline metric.  --mode layer times the
 output layer around it as well: states of --width to activations to cost and gradient to the
 weights' gradient, with states and weights in 8 bits (and not what lies below: the states'
-gradient, which the library does not compute, and the norm's, which follows from it).
+gradient, which the library does not compute, and the norm's, which follows from it); with
+--blocks N recurrent blocks under it, forward and backward, and then the norm's gradient too
+(between them random numbers stand for what the network's matrix products would give).
 """
 from __future__ import annotations
 
