@@ -33,6 +33,9 @@ struct RecurrenceArgs {
 
 // Frames that a wavefront has in registers at once (of the gradient, which has twice the tensors and a slope to keep, four), and wavefronts that share an utterance's.
 constexpr int kRun = 16, kRunBack = 4, kRecurrenceWaves = 8;
+// Up to two rounds (of the gradient's short ones six) one launch takes less time than two: 40 x 130 x 600 bf16 10.9 us and 18, backward 16 and 20; from
+// three (eight) on it takes more: 2 x 500 x 256 14 us and 11.5, backward of 2 x 250 x 4000 18 and 12.4.
+inline int few_rounds(int run) { return run == kRun ? 2 : 6; }
 
 // How an utterance's T frames are dealt out in runs, where `places` workgroups would have one tile of channels of one utterance each: one wavefront has
 // few of them (runs of one or four frames where there are no more: 512 x 1 x 4096 bf16 by a run of sixteen 26 us, so 8; 512 x 4 x 2048 16 and 9.6), four
@@ -47,7 +50,7 @@ inline RecurrencePlan recurrence_plan(int T, int64_t places, int run)
     if (T <= run) return {1, 1, T};
     if (T <= 4 * run) return {4, 1, T};
     const int round = run * kRecurrenceWaves, rounds = (T - 1) / round + 1;
-    if (places > 256 || rounds == 1) return {kRecurrenceWaves, 1, T};
+    if (places > 256 || rounds <= few_rounds(run)) return {kRecurrenceWaves, 1, T};
     const int64_t wanted = 512 / places, most = wanted < rounds ? wanted : rounds;
     const int each = static_cast<int>((rounds + most - 1) / most);
     return {kRecurrenceWaves, (rounds + each - 1) / each, each * round};
@@ -60,7 +63,7 @@ constexpr int kShortestStretch = kRunBack * kRecurrenceWaves;
 constexpr int64_t kMostCarried = (512 + 256) * 128;
 inline size_t recurrence_bytes(int T, int B, int H)
 {
-    if (T <= kShortestStretch) return 0;
+    if (T <= 6 * kShortestStretch) return 0;                    // (few_rounds of the gradient; the forward call's are more frames)
     const int64_t stretches = (static_cast<int64_t>(T) + kShortestStretch - 1) / kShortestStretch, all = (stretches + 1) * B * H;
     return static_cast<size_t>(all < kMostCarried ? all : kMostCarried) * 16;
 }

@@ -28,12 +28,13 @@ static void look(int T, int B, int H, int F)
         if (p.stretches > 1 && static_cast<int64_t>(p.steps) * (p.stretches - 1) >= T) fail("an empty stretch", T, B, H, F, V);
         if (tiles * B * p.stretches > 0x7fffffffll) fail("groups", T, B, H, F, V);
         if (p.stretches > 1 && static_cast<size_t>(p.stretches + 1) * B * H * 16 > recurrence_bytes(T, B, H)) fail("workspace", T, B, H, F, V);
+        if (p.stretches > 1 && recurrence_bytes(T, B, H) == 0) fail("no workspace", T, B, H, F, V);
         if (p.stretches > 1 && p.stretches * (tiles * B) > 512) fail("more than fill the compute units", T, B, H, F, V);
     }
 }
 int main()
 {
-    for (int T : {1, 2, 4, 5, 16, 17, 32, 33, 64, 65, 127, 128, 129, 255, 257, 1000, 40000, 1 << 20, 1 << 30})
+    for (int T : {1, 2, 4, 5, 16, 17, 32, 33, 64, 65, 127, 128, 129, 191, 192, 193, 224, 255, 256, 257, 1000, 40000, 1 << 20, 1 << 30})
         for (int B : {1, 2, 3, 31, 64, 512, 65535})
             for (int H : {1, 2, 3, 63, 64, 65, 127, 128, 129, 1999, 2048, 16383, 16384})
                 for (int F : {0, 1, H / 2, H - 1, H})
