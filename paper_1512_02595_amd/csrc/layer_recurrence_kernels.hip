@@ -84,9 +84,14 @@ template <int V> __device__ __forceinline__ bool place_of(const RecurrenceArgs& 
     at.backwards = tile >= tiles_forward;
     if (at.backwards) tile -= tiles_forward;
     const int first = at.backwards ? p.forward : 0, end = at.backwards ? p.H : p.forward;
-    const int k = first + tile * kTile + static_cast<int>(threadIdx.x % kWave) * V;
-    at.mine = k < end;
-    at.k = k + V <= end ? k : end - V;          // (a direction's channels are at least V: a lane at its end takes some that another lane has too)
+    // A last tile with fewer channels than a lane takes has the V before them too, and the tile before it that many fewer: no channel is two workgroups', of
+    // which one might find its state where the other has written its last already.
+    int begin = first + tile * kTile, stop = begin + kTile < end ? begin + kTile : end;
+    if (end - begin < V) begin -= V;
+    else if (end > stop && end - stop < V) stop -= V;
+    const int k = begin + static_cast<int>(threadIdx.x % kWave) * V;
+    at.mine = k < stop;
+    at.k = k + V <= stop ? k : stop - V;        // (a lane at a tile's end takes some that another of its lanes has too)
     at.steps = __builtin_amdgcn_readfirstlane(length_of(p.lengths, at.b, p.T));
     return true;
 }

@@ -147,9 +147,11 @@ def test_gradient(T, B, H, more, forward, dtype, kind):
 # ---- what may be done with the calls ----------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("T, B, H, forward", [(1, 3, 200, 200), (40, 5, 130, 60), (300, 2, 128, 128), (5000, 1, 96, 48)])
+@pytest.mark.parametrize("T, B, H, forward", [(1, 3, 200, 200), (40, 5, 130, 60), (300, 2, 128, 128), (5000, 1, 96, 48), (1, 600, 1025, 1025), (3, 600, 386, 129),
+                                              (20, 400, 258, 257), (150, 300, 257, 129), (260, 300, 129, 129), (400, 100, 385, 128), (2000, 1, 385, 256)])
 def test_states_carried_in_place(T, B, H, forward, dtype):
-    """final_states in initial's place, dinitial in dfinal's: also where several workgroups share an utterance."""
+    """final_states in initial's place, dinitial in dfinal's: also where several workgroups share an utterance, or where one of them has a single channel, of
+    which a lane of two brings the one before it, another workgroup's, too."""
     say("in place", T, B, H, forward, dtype)
     c = Call(T, B, H, dtype, "some", None, forward)
     place = put(c.initial, torch.float32)
