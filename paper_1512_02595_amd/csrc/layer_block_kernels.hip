@@ -407,7 +407,7 @@ __global__ __launch_bounds__(MANY ? kMostWaves * kWave : 256, 4) void ctc_block_
 }
 
 // Rows of more than 8192, whose tensors a compute unit's registers do not hold beside the sums: a workgroup to a row, which reads it twice from memory and once more from the
-// caches, and adds to its own partial sums t
+// caches, and adds to its own partial sums where they lie.
 template <typename T> __global__ __launch_bounds__(1024) void ctc_block_norm_backward_wide_kernel(BlockNormBackArgs p)
 {
     constexpr int kE = Vector<T>::kElements, kStep = 1024 * kE;

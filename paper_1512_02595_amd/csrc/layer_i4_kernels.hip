@@ -280,6 +280,7 @@ __global__ __launch_bounds__(WAVES * kWave, RT * ST >= 8 ? 3 : 1) void ctc_linea
     if (wave < tiles) weights(wave, next);
     // One lane asks the list for each row.
     const int asked = row_at(p.frames, p.rows, m0 + lane % (16 * RT));
+    if (p.frames && !__ballot(asked >= 0)) return;                                // (all of them behind the list's end: 512 of 1024 x 2048 by 6144 bf16 30 us, so 18)
     if (wave == 0 && lane < 16 * RT) s_row[lane] = asked;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
