@@ -33,9 +33,15 @@ struct RecurrenceArgs {
 
 // Frames that a wavefront has in registers at once (of the gradient, which has twice the tensors and a slope to keep, four), and wavefronts that share an utterance's.
 constexpr int kRun = 16, kRunBack = 4, kRecurrenceWaves = 8;
-// Up to two rounds (of the gradient's short ones six) one launch takes less time than two: 40 x 130 x 600 bf16 10.9 us and 18, backward 16 and 20; from
-// three (eight) on it takes more: 2 x 500 x 256 14 us and 11.5, backward of 2 x 250 x 4000 18 and 12.4.
-inline int few_rounds(int run) { return run == kRun ? 2 : 6; }
+// Up to so many rounds one launch takes less time than two, which for near as many workgroups as kFewPlaces read what they read twice at the memory's rate: bf16
+// 40 x 130 x 600 (200 workgroups, two rounds) 10.9 us and 18, 2 x 500 x 256 (four) 14.1 and 11.8, 112 x 1000 x 128 (eight) 29 and 34; backward 2 x 190 x 1024 fp32
+// (16, six) 17 and 13, 112 x 170 x 128 (six) 17.6 and 20.7.
+inline int few_rounds(int run, int64_t places) { return run == kRun ? (places > 96 ? 16 : 2) : places > 96 ? 8 : 4; }
+
+// With more workgroups than this (one tile of channels of one utterance each) a compute unit's share is read fast enough in one launch, and a second reading
+// costs more than it gives: 16 x 1000 x 2048 (256 workgroups) bf16 55 us in stretches, 37 in one launch, backward 95 and 78, fp32 backward 169 and 135;
+// 9 x 1000 (144) 44 and 30, 62 and 60, 106 and 103; 7 x 8000 (112) 220 and 254, 372 and 444, 664 and 883.
+constexpr int kFewPlaces = 128;
 
 // How an utterance's T frames are dealt out in runs, where `places` workgroups would have one tile of channels of one utterance each: one wavefront has
 // few of them (runs of one or four frames where there are no more: 512 x 1 x 4096 bf16 by a run of sixteen 26 us, so 8; 512 x 4 x 2048 16 and 9.6), four
@@ -50,20 +56,20 @@ inline RecurrencePlan recurrence_plan(int T, int64_t places, int run)
     if (T <= run) return {1, 1, T};
     if (T <= 4 * run) return {4, 1, T};
     const int round = run * kRecurrenceWaves, rounds = (T - 1) / round + 1;
-    if (places > 256 || rounds <= few_rounds(run)) return {kRecurrenceWaves, 1, T};
+    if (places > kFewPlaces || rounds <= few_rounds(run, places)) return {kRecurrenceWaves, 1, T};
     const int64_t wanted = 512 / places, most = wanted < rounds ? wanted : rounds;
     const int each = static_cast<int>((rounds + most - 1) / most);
     return {kRecurrenceWaves, (rounds + each - 1) / each, each * round};
 }
 
 // Bytes of workspace: two numbers in fp64 for each channel of each stretch of frames, and the initial states; of more than one stretch only
-// where there are few places (by recurrence_plan at most 256, of at most 128 channels each, and then at most 512 stretches in all), so that kMostCarried is never
+// where there are few places (by recurrence_plan at most kFewPlaces, of at most 128 channels each, and then at most 512 stretches in all), so that kMostCarried is never
 // exceeded.
 constexpr int kShortestStretch = kRunBack * kRecurrenceWaves;
-constexpr int64_t kMostCarried = (512 + 256) * 128;
+constexpr int64_t kMostCarried = (512 + kFewPlaces) * 128;
 inline size_t recurrence_bytes(int T, int B, int H)
 {
-    if (T <= 6 * kShortestStretch) return 0;                    // (few_rounds of the gradient; the forward call's are more frames)
+    if (T <= 4 * kShortestStretch) return 0;                    // (few_rounds of the gradient; the forward call's are more frames)
     const int64_t stretches = (static_cast<int64_t>(T) + kShortestStretch - 1) / kShortestStretch, all = (stretches + 1) * B * H;
     return static_cast<size_t>(all < kMostCarried ? all : kMostCarried) * 16;
 }

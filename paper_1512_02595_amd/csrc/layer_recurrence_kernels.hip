@@ -218,27 +218,28 @@ __global__ __launch_bounds__(WAVES * kWave) void ctc_recurrence_kernel(Recurrenc
     const uint32_t at_gate = static_cast<uint32_t>(at.k) * sizeof(T), at_candidate = static_cast<uint32_t>(p.H + at.k) * sizeof(T);
     int turn = 0;
     constexpr int kRound = WAVES * RUN;
-    for (int from = begin; from < end; from += kRound) {
-        // A summary goes from the stretch's last round to its first, with which the launch behind it begins: what was read last is still in the caches.
-        const int round = PART == Part::kSummary ? begin + (end - 1 - from) / kRound * kRound : from;
-        const int first = round + wave * RUN;
+    // The gradient's next run is asked for before this one is gone over (64 x 750 x 2048 bf16 249 us, so 227; 16 x 1000 x 2048 fp32 149 and 135).  A run of
+    // sixteen frames is itself enough on its way: bf16 115 us, the next one asked for ahead 131, the registers leaving half as many wavefronts.
+    constexpr bool kAhead = BACK && PART == Part::kWhole && WAVES == kRecurrenceWaves;
+    struct Frames {
         Some<T, V> g[RUN], c[RUN], d[RUN], h[RUN];
-        const bool full = first + RUN <= end && (!BACK || first + RUN < at.steps);
+    } ahead;
+    const auto bring = [&](int first, Frames& f) {
         const int64_t row = at.row(BACK ? at.steps - 1 - (first < end ? first : end - 1) : first < end ? first : end - 1, p.B);
         const char* in = static_cast<const char*>(p.inputs) + row * row_bytes;
         const char* grad = static_cast<const char*>(p.dstates) + row * state_bytes;
         const char* held = static_cast<const char*>(p.states_in) + row * state_bytes;
-        const auto bring = [&](int i) {
-            g[i] = load_some<T, V>(in, at_gate);
-            if constexpr (!BACK || PART != Part::kSummary) c[i] = load_some<T, V>(in, at_candidate);
-            if constexpr (BACK) d[i] = load_some<T, V>(grad, at_gate);
-            if constexpr (BACK && PART != Part::kSummary) h[i] = load_some<T, V>(held, at_gate);
+        const auto one = [&](int i) {
+            f.g[i] = load_some<T, V>(in, at_gate);
+            if constexpr (!BACK || PART != Part::kSummary) f.c[i] = load_some<T, V>(in, at_candidate);
+            if constexpr (BACK) f.d[i] = load_some<T, V>(grad, at_gate);
+            if constexpr (BACK && PART != Part::kSummary) f.h[i] = load_some<T, V>(held, at_gate);
         };
-        if (full) {
+        if (first + RUN <= end && (!BACK || first + RUN < at.steps)) {
             held += hop_states;
 #pragma unroll
             for (int i = 0; i < RUN; ++i) {
-                bring(i);
+                one(i);
                 in += hop;
                 grad += hop_states;
                 held += hop_states;
@@ -249,13 +250,30 @@ __global__ __launch_bounds__(WAVES * kWave) void ctc_recurrence_kernel(Recurrenc
             held += first + 1 < at.steps ? hop_states : 0;
 #pragma unroll
             for (int i = 0; i < RUN; ++i) {
-                bring(i);
+                one(i);
                 in += first + i + 1 < end ? hop : 0;
                 grad += first + i + 1 < end ? hop_states : 0;
                 held += first + i + 1 < end && first + i + 2 < at.steps ? hop_states : 0;
             }
         }
-        // All of a run is asked for before any of it is waited for.
+    };
+    if constexpr (kAhead)
+        if (begin < end) bring(begin + wave * RUN, ahead);
+    for (int from = begin; from < end; from += kRound) {
+        // A summary goes from the stretch's last round to its first, with which the launch behind it begins: what was read last is still in the caches.
+        const int round = PART == Part::kSummary ? begin + (end - 1 - from) / kRound * kRound : from;
+        const int first = round + wave * RUN;
+        const bool full = first + RUN <= end && (!BACK || first + RUN < at.steps);
+        const int64_t row = at.row(BACK ? at.steps - 1 - (first < end ? first : end - 1) : first < end ? first : end - 1, p.B);
+        Frames here;
+        if constexpr (kAhead) {
+            here = ahead;
+            if (from + kRound < end) bring(first + kRound, ahead);
+        } else {
+            bring(first, here);
+        }
+        auto &g = here.g, &c = here.c, &d = here.d, &h = here.h;
+        // All of it is asked for before any is waited for.
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
         float z[RUN][V], slope[RUN][V];

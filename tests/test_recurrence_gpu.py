@@ -121,7 +121,8 @@ SIZES = [(1, 1, 1, 0, 1), (1, 3, 70, 0, 70), (2, 1, 64, 0, 0), (3, 5, 129, 7, 60
          (16, 2, 128, 0, 128), (17, 2, 127, 5, 1), (33, 3, 65, 1, 64), (63, 1, 500, 0, 250), (64, 4, 96, 0, 96), (65, 4, 96, 0, 48), (127, 2, 130, 0, 0),
          (128, 2, 258, 0, 258), (129, 3, 64, 64, 64), (200, 1, 1000, 0, 499), (256, 5, 40, 0, 40), (257, 2, 8, 2, 3), (511, 1, 16, 0, 16),
          (513, 3, 200, 0, 100), (1000, 2, 65, 1, 65), (1500, 1, 300, 0, 150), (4097, 1, 130, 0, 131 // 2), (20000, 1, 33, 0, 33), (50, 130, 64, 0, 64),
-         (300, 70, 128, 0, 64), (1, 700, 512, 512, 512), (4, 2, 16384, 0, 16384), (140, 1, 4099, 3, 2050)]
+         (300, 70, 128, 0, 64), (1, 700, 512, 512, 512), (4, 2, 16384, 0, 16384), (140, 1, 4099, 3, 2050), (700, 100, 65, 1, 65), (180, 140, 34, 0, 17),
+         (260, 56, 128, 0, 64)]
 
 
 @pytest.mark.parametrize("kind", ["all", "some", "none"])
