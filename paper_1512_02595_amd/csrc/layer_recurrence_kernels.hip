@@ -60,27 +60,50 @@ __device__ __forceinline__ float once(double v)
 
 enum class Part { kWhole, kSummary, kStretch };
 
-// What of the grid a workgroup is: a tile of channels of one direction, an utterance, a stretch of its frames.  Workgroups are dealt out to the eight dies
-// in turn; each die's take neighbouring tiles of all utterances, so that lines of memory that two tiles share are in one die's cache, and
-// each die has its share of the long utterances.
+// What of the grid a workgroup is: a tile of channels of one direction, an utterance, a stretch of its frames.
 struct Place {
     int b, k, stretch, steps;           // k: this lane's first channel; steps of the utterance
     bool backwards, mine;               // in time; whether the lane has channels that no lane before it has
 
     __device__ __forceinline__ int64_t row(int step, int B) const { return static_cast<int64_t>(backwards ? steps - 1 - step : step) * B + b; }
 };
-template <int V> __device__ __forceinline__ bool place_of(const RecurrenceArgs& p, unsigned groups, Place& at)
+
+// Of 64 utterances from b on the one that has the rank-th most frames (of as many, the first has the lower rank), by the bits of their lengths.
+__device__ __forceinline__ void by_length(const RecurrenceArgs& p, int rank, Place& at)
+{
+    const int lane = threadIdx.x % kWave;
+    const int length = at.b + lane < p.B ? length_of(p.lengths, at.b + lane, p.T) : 0;
+    uint64_t left = at.b + kWave <= p.B ? ~0ull : (1ull << (p.B - at.b)) - 1;
+    for (int bit = 31 - __builtin_clz(p.T); bit >= 0; --bit) {
+        const uint64_t set = __ballot(length >> bit & 1) & left;
+        const int n = __popcll(set);
+        left = rank < n ? set : left & ~set;
+        rank -= rank < n ? 0 : n;
+    }
+    const int before = __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(left >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(left), 0u));
+    const int found = __builtin_ctzll(__ballot(before == rank) & left);
+    at.b += found;
+    at.steps = __builtin_amdgcn_readlane(length, found);
+}
+
+// LONGEST: of 64 utterances at a time those with many frames come first, so that at the end no few workgroups go on alone (64 x 750 x 2048, 27200 frames bf16 86 us,
+// so 76, backward 162 and 145).
+template <int V, bool LONGEST> __device__ __forceinline__ bool place_of(const RecurrenceArgs& p, Place& at)
 {
     constexpr int kTile = kWave * V;
-    const unsigned per_die = (groups + 7) / 8, number = static_cast<unsigned>(group_number());
-    if (number / 8 >= per_die) return false;
-    const unsigned i = number % 8 * per_die + number / 8;
-    if (i >= groups) return false;
-    const int tiles_forward = (p.forward + kTile - 1) / kTile;
-    const unsigned B = static_cast<unsigned>(p.B), stretches = static_cast<unsigned>(p.stretches), rest = i / B;
-    at.b = static_cast<int>(i % B);
-    at.stretch = static_cast<int>(rest % stretches);
-    int tile = static_cast<int>(rest / stretches);
+    const int tiles_forward = (p.forward + kTile - 1) / kTile, tiles = tiles_forward + (p.H - p.forward + kTile - 1) / kTile;
+    const unsigned number = static_cast<unsigned>(group_number()), units = static_cast<unsigned>(tiles * p.stretches), B = static_cast<unsigned>(p.B);
+    const Unit here = unit_of(number, units, B);
+    if (here.utterance >= B) return false;
+    at.stretch = static_cast<int>(here.unit % static_cast<unsigned>(p.stretches));
+    int tile = static_cast<int>(here.unit / static_cast<unsigned>(p.stretches));
+    at.b = static_cast<int>(here.utterance);
+    if (LONGEST && p.lengths) {
+        at.b = at.b / kWave * kWave;
+        by_length(p, static_cast<int>(here.utterance % kWave), at);
+    } else {
+        at.steps = __builtin_amdgcn_readfirstlane(length_of(p.lengths, at.b, p.T));
+    }
     at.backwards = tile >= tiles_forward;
     if (at.backwards) tile -= tiles_forward;
     const int first = at.backwards ? p.forward : 0, end = at.backwards ? p.H : p.forward;
@@ -92,7 +115,6 @@ template <int V> __device__ __forceinline__ bool place_of(const RecurrenceArgs& 
     const int k = begin + static_cast<int>(threadIdx.x % kWave) * V;
     at.mine = k < stop;
     at.k = k + V <= stop ? k : stop - V;        // (a lane at a tile's end takes some that another of its lanes has too)
-    at.steps = __builtin_amdgcn_readfirstlane(length_of(p.lengths, at.b, p.T));
     return true;
 }
 
@@ -186,12 +208,12 @@ template <int V> __device__ __forceinline__ void leave_map(const RecurrenceArgs&
 
 // Rounds of WAVES runs of RUN frames.  BACK: the gradient, whose steps are an utterance's in the other order.
 template <typename T, int V, int RUN, int WAVES, Part PART, bool BACK>
-__global__ __launch_bounds__(WAVES * kWave) void ctc_recurrence_kernel(RecurrenceArgs p, unsigned groups)
+__global__ __launch_bounds__(WAVES * kWave) void ctc_recurrence_kernel(RecurrenceArgs p)
 {
     __shared__ Map s_map[WAVES > 1 ? 2 : 1][WAVES][V][kWave];
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     Place at;
-    if (!place_of<V>(p, groups, at)) return;
+    if (!place_of<V, PART == Part::kWhole && WAVES == kRecurrenceWaves>(p, at)) return;
     const int64_t channel = static_cast<int64_t>(at.b) * p.H + at.k;
     const float* const before_all = BACK ? p.dfinal : p.initial;
     const int begin = PART == Part::kWhole ? 0 : static_cast<int>(static_cast<int64_t>(at.stretch) * p.stretch_steps < at.steps ? at.stretch * p.stretch_steps : at.steps);
@@ -373,8 +395,9 @@ __global__ __launch_bounds__(WAVES * kWave) void ctc_recurrence_kernel(Recurrenc
 template <typename T, int V, int RUN, int WAVES, Part PART, bool BACK> int launch_part(RecurrenceArgs p, int64_t tiles, hipStream_t s)
 {
     if (PART == Part::kSummary) --p.stretches;                  // (nobody asks for the last one's)
-    const unsigned groups = static_cast<unsigned>(tiles * p.B * p.stretches);         // (at most 257 tiles by 65535 utterances: stretches come where places are few)
-    return launch(ctc_recurrence_kernel<T, V, RUN, WAVES, PART, BACK>, spread(blocks(groups, 8) * 8), WAVES * kWave, s, p, groups);
+    // (at most 257 tiles by 65535 utterances: stretches come where places are few)
+    const dim3 grid = spread(8 * units_of_a_die(static_cast<unsigned>(tiles * p.stretches), static_cast<unsigned>(p.B)));
+    return launch(ctc_recurrence_kernel<T, V, RUN, WAVES, PART, BACK>, grid, WAVES * kWave, s, p);
 }
 
 template <typename T, int V, bool BACK> int launch_channels(RecurrenceArgs p, hipStream_t s)

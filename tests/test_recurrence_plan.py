@@ -9,6 +9,7 @@ PROGRAM = r'''
 #include <cstdio>
 #include <cstdlib>
 #include <initializer_list>
+#include <vector>
 #include "layer_block_internal.h"
 using namespace layer;
 static unsigned long long seed = 12345;
@@ -54,6 +55,23 @@ int main()
             last = g;
         }
     }
+    // Each unit of each utterance is one workgroup's, and no die has many more than another.
+    for (unsigned B : {1, 2, 5, 7, 8, 9, 15, 16, 17, 27, 63, 64, 65, 200})
+        for (unsigned units : {1, 2, 3, 4, 7, 8, 9, 13, 16, 17, 31, 128, 257, 512}) {
+            const unsigned each = units_of_a_die(units, B);
+            std::vector<int> seen(static_cast<size_t>(B) * units, 0);
+            int64_t count = 0;
+            for (unsigned number = 0; number < 8 * each + 1000; ++number) {
+                const Unit u = unit_of(number, units, B);
+                if (u.utterance >= B) continue;
+                if (u.unit >= units) fail("no such unit", 0, B, units, 0, 0);
+                if (number >= 8 * each) fail("behind the grid", 0, B, units, 0, 0);
+                if (seen[static_cast<size_t>(u.utterance) * units + u.unit]++) fail("twice", 0, B, units, 0, 0);
+                ++count;
+            }
+            if (count != static_cast<int64_t>(B) * units) fail("nobody's", 0, B, units, 0, 0);
+            if (8ll * each > count + 7) fail("idle workgroups", 0, B, units, 0, 0);
+        }
     std::puts("ok");
 }
 '''
