@@ -519,7 +519,8 @@ __global__ __launch_bounds__(1024) void ctc_block_norm_weights_kernel(const floa
 {
     __shared__ double s_sum[16][16];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const int col = blockIdx.x * 16 + lane % 16;
+    // (each die has neighbouring columns, so that it has a line of memory's both halves)
+    const int col = static_cast<int>(blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8) * 16 + lane % 16;
     double sum = 0.0;
     if (col < 2 * H)
 #pragma unroll 16
@@ -583,7 +584,7 @@ int launch_block_norm_backward(const BlockNormBackArgs& p, bool bf16, float* dwe
     const int groups = block_norm_groups(p.rows, p.H);
     const int err = bf16 ? launch_backward_of<bf16_t>(p, static_cast<unsigned>(groups), s) : launch_backward_of<float>(p, static_cast<unsigned>(groups), s);
     if (err || !p.partials) return err;
-    return launch(ctc_block_norm_weights_kernel, dim3(blocks(2 * static_cast<int64_t>(p.H), 16)), 1024, s, p.partials, groups, p.H, p.weight_after,
+    return launch(ctc_block_norm_weights_kernel, dim3(blocks(2 * static_cast<int64_t>(p.H), 8 * 16) * 8), 1024, s, p.partials, groups, p.H, p.weight_after,
                   p.scale, dweight_after, dscale, dweight_before);
 }
 
