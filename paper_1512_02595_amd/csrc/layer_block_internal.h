@@ -185,13 +185,16 @@ struct LinearI4Args {
 
 // Rows and symbols to a workgroup, by what leaves the compute units work: every row that a tile has beyond the first sixteen takes its symbols' weights along.
 // (100 x 4096 by 3000, 188 tiles of 64 by 32: 64 by 16 11.8 us, 64 by 32 12.6; 128 x 2048 by 6000, 376: 12.2 and 11.5; 256 x 1000 by 12000: 26 and 18.5.)
-enum class I4Tile { k16x16, k16x16Deep, k32x16, k64x16, k64x32 };
+// Where there are 64 by 128 enough, its wavefronts have all columns each and nothing is added up (512 x 2048 by 6144 bf16, 384 tiles: 20.1 us, 32 by 64 20.2;
+// 1024 29.5 and 35.6; 384 x 4096 by 6144, 288: 28 and 23).
+enum class I4Tile { k16x16, k16x16Deep, k32x16, k64x16, k32x64, k64x128 };
 inline I4Tile i4_tile(int rows, int pitch, int A)
 {
     const auto tiles = [&](int m, int n) { return (static_cast<int64_t>(rows) + m - 1) / m * ((A + n - 1) / n); };
     if (rows <= 16) return tiles(16, 16) < 256 && pitch >= 1024 ? I4Tile::k16x16Deep : I4Tile::k16x16;
     if (rows <= 32) return I4Tile::k32x16;
-    return tiles(64, 32) < 256 ? I4Tile::k64x16 : I4Tile::k64x32;
+    if (tiles(64, 32) < 256) return I4Tile::k64x16;
+    return tiles(64, 128) < 384 ? I4Tile::k32x64 : I4Tile::k64x128;
 }
 
 int launch_quantize_i4(const void* weights, int A, int H, int group, bool bf16, uint8_t* weight_q, float* weight_scales, void* stream);

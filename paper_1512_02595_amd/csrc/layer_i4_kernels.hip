@@ -225,10 +225,26 @@ __device__ __forceinline__ void in_order()
 typedef int int4v __attribute__((ext_vector_type(4)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 
+// A tile's 128 columns to sixteen rows' sums with sixteen symbols.
+template <bool BY_64> __device__ __forceinline__ void add_columns(int4v low, int4v high, int4v w_low, int4v w_high, float by, float by_high, float4v& sum)
+{
+    int4v a = __builtin_amdgcn_mfma_i32_16x16x64_i8(low, w_low, int4v{}, 0, 0, 0);
+    if constexpr (BY_64) {
+        const int4v b = __builtin_amdgcn_mfma_i32_16x16x64_i8(high, w_high, int4v{}, 0, 0, 0);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sum[k] = fmaf(static_cast<float>(b[k]), by_high, fmaf(static_cast<float>(a[k]), by, sum[k]));
+    } else {
+        a = __builtin_amdgcn_mfma_i32_16x16x64_i8(high, w_high, a, 0, 0, 0);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sum[k] = fmaf(static_cast<float>(a[k]), by, sum[k]);
+    }
+}
+
 // RT by ST tiles of 16 rows by 16 symbols to a workgroup, each of whose wavefronts takes every WAVES-th 128 columns of all of them, straight from memory
 // into the matrix cores, the next ones asked for before these are multiplied; their sums are added in LDS.  A weight's four bits become the upper half
 // of a byte, sixteen times their value: that takes one `and` (and a shift for the lower half) for four weights, and a sixteenth comes into the row's scale.
-// (64 rows by 32 symbols: three wavefronts to a SIMD, by 64 symbols two; 256 x 2048 by 6144 bf16 13.7 us a pass, 16.8.)
+// (32 rows by 64 symbols: three wavefronts to a SIMD, as 64 by 32, whose rows are twice as many to turn over: 256 x 2048 by 6144 bf16 11.0 us on the GPU and 11.8;
+// 64 by 64 has two: 16.8 us a pass, 64 by 32 13.7.)
 // v_mfma_i32_16x16x64_i8: lane l gives bytes 16 (l / 16) .. of row l % 16 of either operand, and holds rows 4 (l / 16) .. + 3 of column
 // l % 16 of the result.
 template <typename T, int RT, int ST, int WAVES, bool BY_64>
@@ -323,17 +339,7 @@ __global__ __launch_bounds__(WAVES * kWave, RT * ST >= 8 ? 3 : 1) void ctc_linea
             const int4v w_low = here.w[s] << 4 & static_cast<int>(0xf0f0f0f0u), w_high = here.w[s] & static_cast<int>(0xf0f0f0f0u);
 #pragma unroll
             for (int i = 0; i < RT; ++i) {
-                int4v a = __builtin_amdgcn_mfma_i32_16x16x64_i8(low[i], w_low, int4v{}, 0, 0, 0);
-                if constexpr (BY_64) {
-                    const int4v b = __builtin_amdgcn_mfma_i32_16x16x64_i8(high[i], w_high, int4v{}, 0, 0, 0);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        sum[i][s][k] = fmaf(static_cast<float>(b[k]), here.by_high[s], fmaf(static_cast<float>(a[k]), here.by[s], sum[i][s][k]));
-                } else {
-                    a = __builtin_amdgcn_mfma_i32_16x16x64_i8(high[i], w_high, a, 0, 0, 0);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) sum[i][s][k] = fmaf(static_cast<float>(a[k]), here.by[s], sum[i][s][k]);
-                }
+                add_columns<BY_64>(low[i], high[i], w_low, w_high, here.by[s], BY_64 ? here.by_high[s] : 0.0f, sum[i][s]);
             }
         }
     }
@@ -356,11 +362,111 @@ __global__ __launch_bounds__(WAVES * kWave, RT * ST >= 8 ? 3 : 1) void ctc_linea
     }
 }
 
+// Many rows and symbols: a workgroup's wavefronts share RT tiles of rows, brought once for all of them through LDS, and have ST tiles of symbols each and all
+// columns, so that nothing is added up at the end.  Two buffers by turns: who writes one again has passed the barrier that its readers came to when they were done.
+// Bound by the vector units, which have two operations for each sum of 64 (128) columns beside the matrix cores' 16 (32) cycles for 256 of them, and by LDS:
+// 2048 x 4096 by 12000 in groups of 128 bf16 162 us, 1.2 PO/s.  (Asked for two or four steps ahead, 1024 x 2048 by 6144 28.2 and 29.4 us in place of 26.7; two
+// tiles of symbols a wavefront 159 there, but 2048 x 2048 by 2000 in groups of 64 24.9 in place of 22.7.)
+template <typename T, int RT, int ST, int WAVES, bool BY_64>
+__global__ __launch_bounds__(WAVES * kWave) void ctc_linear_i4_rows_kernel(LinearI4Args p)
+{
+    constexpr int kRows = 16 * RT, kThreads = WAVES * kWave, kLoads = RT * 128 / kThreads, kColumns = 16 * ST * WAVES;
+    __shared__ int4v s_quads[2][kRows * 8];
+    __shared__ int s_row[kRows];
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const unsigned across = static_cast<unsigned>((p.A + kColumns - 1) / kColumns), group = static_cast<unsigned>(group_number());
+    const int64_t m0 = static_cast<int64_t>(group / across) * kRows;
+    const int n0 = (static_cast<int>(group % across) * WAVES + wave) * ST;         // in tiles of 16 symbols
+    if (m0 >= listed(p.frames, p.rows)) return;
+    const int tiles = p.pitch / kTileColumns, last_tile = (p.A + 15) / 16 - 1;
+    const uint8_t* w[ST];
+    const float* scale[ST];
+#pragma unroll
+    for (int s = 0; s < ST; ++s) {
+        const int64_t tile = n0 + s < last_tile ? n0 + s : last_tile;
+        w[s] = p.weight_q + tile * tiles * kTileBytes + 16 * lane;
+        scale[s] = p.weight_scales + tile * p.groups * 16 + lane % 16;
+    }
+    struct Columns {
+        int4v q[kLoads], w[ST];
+        float by[ST], by_high[ST];
+    } here, next;
+    const int8_t* q[kLoads];
+    int to_lds[kLoads];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+        const int row = static_cast<int>(threadIdx.x) / 8 + i * (kThreads / 8), piece = threadIdx.x % 8;
+        const int r = row_at(p.frames, p.rows, m0 + row);
+        if (piece == 0) s_row[row] = r;
+        q[i] = p.q + static_cast<int64_t>(r < 0 ? 0 : r) * p.pitch + 16 * piece;          // (what row 0 gives instead is not written)
+        to_lds[i] = row * 8 + (piece ^ row % 8);
+    }
+    const auto bring = [&](int t, Columns& to) {
+        const int g = BY_64 ? 2 * t : t * kTileColumns / p.group;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) __builtin_memcpy(&to.q[i], __builtin_assume_aligned(q[i] + t * kTileColumns, 16), 16);
+#pragma unroll
+        for (int s = 0; s < ST; ++s) {
+            __builtin_memcpy(&to.w[s], __builtin_assume_aligned(w[s] + static_cast<int64_t>(t) * kTileBytes, 16), 16);
+            to.by[s] = scale[s][static_cast<int64_t>(g) * 16];
+            if constexpr (BY_64) to.by_high[s] = scale[s][static_cast<int64_t>(g + 1 < p.groups ? g + 1 : g) * 16];
+        }
+    };
+    bring(0, next);
+    float4v sum[RT][ST];
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int s = 0; s < ST; ++s) sum[i][s] = float4v{};
+    const int from_low = lane % 16 * 8 + (lane / 16 ^ lane % 8), from_high = lane % 16 * 8 + ((lane / 16 + 4) ^ lane % 8);
+    for (int t = 0; t < tiles; ++t) {
+        here = next;
+        int4v* const rows = s_quads[t % 2];
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) rows[to_lds[i]] = here.q[i];
+        __syncthreads();
+        if (t + 1 < tiles) bring(t + 1, next);
+        __builtin_amdgcn_sched_barrier(0);
+        int4v low[RT], high[RT];
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            low[i] = rows[from_low + i * 128];
+            high[i] = rows[from_high + i * 128];
+        }
+#pragma unroll
+        for (int s = 0; s < ST; ++s) {
+            const int4v w_low = here.w[s] << 4 & static_cast<int>(0xf0f0f0f0u), w_high = here.w[s] & static_cast<int>(0xf0f0f0f0u);
+#pragma unroll
+            for (int i = 0; i < RT; ++i) add_columns<BY_64>(low[i], high[i], w_low, w_high, here.by[s], BY_64 ? here.by_high[s] : 0.0f, sum[i][s]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int r = s_row[16 * i + 4 * (lane / 16) + k];
+            if (r < 0) continue;
+            const float by = p.scales[r] * 0.0625f;
+#pragma unroll
+            for (int s = 0; s < ST; ++s) {
+                const int64_t a = static_cast<int64_t>(n0 + s) * 16 + lane % 16;
+                if (a < p.A) static_cast<T*>(p.logits)[static_cast<int64_t>(r) * p.A + a] = narrow<T>(fmaf(sum[i][s][k], by, p.bias ? p.bias[a] : 0.0f));
+            }
+        }
+}
+
 template <typename T, int RT, int ST, int WAVES> int launch_i4_tile(const LinearI4Args& p, hipStream_t s)
 {
     const dim3 grid = spread(blocks(p.rows, 16 * RT) * blocks(p.A, 16 * ST));
     return p.group == 64 ? launch(ctc_linear_i4_kernel<T, RT, ST, WAVES, true>, grid, WAVES * kWave, s, p)
                          : launch(ctc_linear_i4_kernel<T, RT, ST, WAVES, false>, grid, WAVES * kWave, s, p);
+}
+
+template <typename T, int RT, int ST, int WAVES> int launch_i4_rows(const LinearI4Args& p, hipStream_t s)
+{
+    const dim3 grid = spread(blocks(p.rows, 16 * RT) * blocks(p.A, 16 * ST * WAVES));
+    return p.group == 64 ? launch(ctc_linear_i4_rows_kernel<T, RT, ST, WAVES, true>, grid, WAVES * kWave, s, p)
+                         : launch(ctc_linear_i4_rows_kernel<T, RT, ST, WAVES, false>, grid, WAVES * kWave, s, p);
 }
 
 template <typename T> int launch_linear_of(const LinearI4Args& p, hipStream_t s)
@@ -370,7 +476,8 @@ template <typename T> int launch_linear_of(const LinearI4Args& p, hipStream_t s)
     case I4Tile::k16x16Deep: return launch_i4_tile<T, 1, 1, 16>(p, s);
     case I4Tile::k32x16: return launch_i4_tile<T, 2, 1, 8>(p, s);
     case I4Tile::k64x16: return launch_i4_tile<T, 4, 1, 8>(p, s);
-    default: return launch_i4_tile<T, 4, 2, 4>(p, s);
+    case I4Tile::k32x64: return launch_i4_tile<T, 2, 4, 4>(p, s);
+    default: return launch_i4_rows<T, 4, 1, 8>(p, s);
     }
 }
 
