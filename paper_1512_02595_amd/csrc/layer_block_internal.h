@@ -184,16 +184,23 @@ struct LinearI4Args {
 };
 
 // Rows and symbols to a workgroup, by what leaves the compute units work: every row that a tile has beyond the first sixteen takes its symbols' weights along.
-// (100 x 4096 by 3000, 188 tiles of 64 by 32: 64 by 16 11.8 us, 64 by 32 12.6; 128 x 2048 by 6000, 376: 12.2 and 11.5; 256 x 1000 by 12000: 26 and 18.5.)
-// Where there are 64 by 128 enough, its wavefronts have all columns each and nothing is added up (512 x 2048 by 6144 bf16, 384 tiles: 20.1 us, 32 by 64 20.2;
-// 1024 29.5 and 35.6; 384 x 4096 by 6144, 288: 28 and 23).
-enum class I4Tile { k16x16, k16x16Deep, k32x16, k64x16, k32x64, k64x128 };
+// On the GPU, bf16, us (rows x columns by symbols):
+//   16 by 16, by so many wavefronts      4 x 2048 by 2000: four 3.1, eight 2.8, sixteen 3.0; 1 x 8192 by 3500: four 7.8, eight 5.2, sixteen 4.5
+//   16 by 16 (four) or 16 by 32 (eight)  1 x 2048 by 6144 3.1 and 3.3, 16 rows 4.4 and 3.6; 1 x 4096 by 5000 3.9 and 3.8, 16 rows 6.3 and 4.8
+//   32 by 16, 32 by 32 or 64 by 16       48 x 2048 by 2000 (250 tiles of 32 by 16) 3.5, 4.3 and 4.8; 128 x 4096 by 3500 (876) 11.0, 8.6 and 10.5
+//   32 by 32 or 32 by 64                 128 x 2048 by 6144 (384 tiles of 64 by 32) 7.4 and 8.0; 96 x 2048 by 9000 (564) 9.4 and 8.9
+//   32 by 64 or 64 by 128, whose wavefronts have all columns each, so that nothing is added up
+//                                        512 x 2048 by 6144 (384 tiles of 64 by 128) 20.2 and 20.1, 1024 rows 35.6 and 29.5; 384 x 4096 by 6144 (288) 23 and 28
+enum class I4Tile { k16x16, k16x16By8, k16x16By16, k16x32, k32x16, k32x32, k32x64, k64x128 };
 inline I4Tile i4_tile(int rows, int pitch, int A)
 {
     const auto tiles = [&](int m, int n) { return (static_cast<int64_t>(rows) + m - 1) / m * ((A + n - 1) / n); };
-    if (rows <= 16) return tiles(16, 16) < 256 && pitch >= 1024 ? I4Tile::k16x16Deep : I4Tile::k16x16;
-    if (rows <= 32) return I4Tile::k32x16;
-    if (tiles(64, 32) < 256) return I4Tile::k64x16;
+    if (rows <= 16) {
+        if (tiles(16, 16) < 256) return pitch < 8192 ? I4Tile::k16x16By8 : I4Tile::k16x16By16;
+        return rows <= 4 && pitch < 4096 ? I4Tile::k16x16 : I4Tile::k16x32;
+    }
+    if (rows <= 32 || tiles(32, 16) < 400) return I4Tile::k32x16;
+    if (tiles(64, 32) < 400) return I4Tile::k32x32;
     return tiles(64, 128) < 384 ? I4Tile::k32x64 : I4Tile::k64x128;
 }
 

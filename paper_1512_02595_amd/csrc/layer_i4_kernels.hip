@@ -473,9 +473,11 @@ template <typename T> int launch_linear_of(const LinearI4Args& p, hipStream_t s)
 {
     switch (i4_tile(p.rows, p.pitch, p.A)) {
     case I4Tile::k16x16: return launch_i4_tile<T, 1, 1, 4>(p, s);
-    case I4Tile::k16x16Deep: return launch_i4_tile<T, 1, 1, 16>(p, s);
+    case I4Tile::k16x16By8: return launch_i4_tile<T, 1, 1, 8>(p, s);
+    case I4Tile::k16x16By16: return launch_i4_tile<T, 1, 1, 16>(p, s);
+    case I4Tile::k16x32: return launch_i4_tile<T, 1, 2, 8>(p, s);
     case I4Tile::k32x16: return launch_i4_tile<T, 2, 1, 8>(p, s);
-    case I4Tile::k64x16: return launch_i4_tile<T, 4, 1, 8>(p, s);
+    case I4Tile::k32x32: return launch_i4_tile<T, 2, 2, 8>(p, s);
     case I4Tile::k32x64: return launch_i4_tile<T, 2, 4, 4>(p, s);
     default: return launch_i4_rows<T, 4, 1, 8>(p, s);
     }

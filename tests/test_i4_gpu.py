@@ -149,6 +149,6 @@ def test_product_of_many_listed_rows(dtype, kind):
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows, A, H, group", [(1, 6000, 2048, 128), (1, 29, 16384, 64), (3, 6000, 700, 64), (64, 2100, 1024, 128), (500, 29, 640, 64),
                                                (257, 1025, 1999, 128), (1000, 4000, 130, 64), (2, 70000, 64, 64), (6300, 500, 130, 64), (2000, 1600, 1000, 128), (1600, 2000, 333, 384),
-                                               (65, 25000, 64, 64)])
+                                               (65, 25000, 64, 64), (12, 5000, 300, 64), (1, 4500, 4200, 128), (500, 2000, 640, 64)])
 def test_product_of_many(rows, A, H, group, dtype):
     product(rows, A, H, group, dtype, "all")
