@@ -11,6 +11,7 @@
  *              ctc_block_norm              norm after a block, gate, scale, residual, norm before the next
  *   backward   ctc_recurrence_backward     gradient of gates, candidates and initial states
  *              ctc_block_norm_backward     gradient of its inputs and of its weights
+ *              ctc_clear_frames            zeros behind the utterances' ends
  *   streaming  ctc_quantize_weights_i4     weights to 4 bits with a scale per group of columns
  *              ctc_dequantize_weights_i4   and back
  *              ctc_linear_i4               activations from rows in 8 bits and weights in 4
@@ -142,6 +143,17 @@ ctc_status_t ctc_block_norm_backward(const void *dnormed, const void *dsum, cons
                                      ctc_dtype_t dtype, void *dx, void *dgate, void *dresidual, float *dweight_after,
                                      float *dscale, float *dweight_before, void *workspace, size_t workspace_bytes,
                                      hipStream_t stream);
+
+/*
+ * Zeros behind the utterances' ends: in rows t * B + b with t >= input_lengths[b], which the calls above leave as they were, for a
+ * product that goes over all rows.  Other rows are neither read nor written.
+ *
+ *   x              (device) [T*B rows, pitch] of type dtype: `width` columns of a row are set to 0
+ *   pitch          elements from one row to the next, >= width; width >= 1
+ *   input_lengths  (device) [B] int32; below 0 counts as 0, above T as T
+ */
+ctc_status_t ctc_clear_frames(void *x, int pitch, const int32_t *input_lengths, int T, int B, int width, ctc_dtype_t dtype,
+                              hipStream_t stream);
 
 /*
  * Weights in 4 bits.  A row's columns [i group, (i + 1) group) share a scale; with m the largest |value| of these, each is

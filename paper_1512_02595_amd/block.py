@@ -12,10 +12,10 @@ import ctypes
 from . import ctc, layer
 
 EXPORTS = ("ctc_recurrence_workspace_size", "ctc_recurrence", "ctc_recurrence_backward", "ctc_block_norm",
-           "ctc_block_norm_workspace_size", "ctc_block_norm_backward", "ctc_weights_i4_sizes", "ctc_quantize_weights_i4",
-           "ctc_dequantize_weights_i4", "ctc_linear_i4")
-_CALLS = ("recurrence", "recurrence_backward", "block_norm", "block_norm_backward", "quantize_weights_i4", "dequantize_weights_i4",
-          "linear_i4")
+           "ctc_block_norm_workspace_size", "ctc_block_norm_backward", "ctc_clear_frames", "ctc_weights_i4_sizes",
+           "ctc_quantize_weights_i4", "ctc_dequantize_weights_i4", "ctc_linear_i4")
+_CALLS = ("recurrence", "recurrence_backward", "block_norm", "block_norm_backward", "clear_frames", "quantize_weights_i4",
+          "dequantize_weights_i4", "linear_i4")
 
 _lib = None
 _native = None                # the module `_block_binding`, once load() has given it the library's addresses
@@ -154,6 +154,17 @@ def block_norm_backward(dnormed_ptr, dsum_ptr, x_ptr, gate_ptr, gate_pitch, sum_
                                                     dweight_before_ptr, workspace_ptr, workspace_bytes, stream)
     if st:
         layer._check(st, "ctc_block_norm_backward")
+
+
+def clear_frames_status(x_ptr, pitch, input_lengths_ptr, T, B, width, dtype, stream=0) -> int:
+    return _module().clear_frames(x_ptr, pitch, input_lengths_ptr, T, B, width, dtype, stream)
+
+
+def clear_frames(x_ptr, pitch, input_lengths_ptr, T, B, width, dtype, stream=0) -> None:
+    """Zeros behind the utterances' ends."""
+    st = (_native or _module()).clear_frames(x_ptr, pitch, input_lengths_ptr, T, B, width, dtype, stream)
+    if st:
+        layer._check(st, "ctc_clear_frames")
 
 
 def quantize_weights_i4_status(weights_ptr, A, H, group, dtype, weight_q_ptr, weight_scales_ptr, stream=0) -> int:

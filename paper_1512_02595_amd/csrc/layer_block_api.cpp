@@ -172,6 +172,15 @@ ctc_status_t ctc_block_norm_backward(const void* dnormed, const void* dsum, cons
     return launched(launch_block_norm_backward(p, dtype == CTC_DTYPE_BF16, dweight_after, dscale, dweight_before, stream));
 }
 
+ctc_status_t ctc_clear_frames(void* x, int pitch, const int32_t* input_lengths, int T, int B, int width, ctc_dtype_t dtype, hipStream_t stream)
+{
+    if (!known(dtype) || T < 1 || B < 1 || width < 1 || pitch < width) return CTC_STATUS_INVALID_VALUE;
+    if (B > kMaxUtterances || static_cast<int64_t>(T) * B > kMaxRows || pitch > kMaxPitch) return CTC_STATUS_UNSUPPORTED;
+    const size_t e = element(dtype);
+    if (!buffers_in_order({{x, pitched(T * B, pitch, width, e), true, true, e}, {input_lengths, matrix(B, 1, 4), false}})) return CTC_STATUS_INVALID_VALUE;
+    return launched(launch_clear_frames(x, pitch, input_lengths, T, B, width, dtype == CTC_DTYPE_BF16, stream));
+}
+
 ctc_status_t ctc_weights_i4_sizes(int A, int H, int group, size_t* weight_bytes_out, size_t* scale_bytes_out)
 {
     if (!weight_bytes_out || !scale_bytes_out) return CTC_STATUS_INVALID_VALUE;

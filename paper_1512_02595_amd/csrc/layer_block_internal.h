@@ -162,6 +162,8 @@ int launch_block_norm(const BlockNormArgs& p, bool bf16, void* stream);
 int launch_block_norm_backward(const BlockNormBackArgs& p, bool bf16, float* dweight_after, float* dscale, float* dweight_before,
                                void* stream);
 
+int launch_clear_frames(void* x, int pitch, const int32_t* lengths, int T, int B, int width, bool bf16, void* stream);
+
 // ---- weights in 4 bits ----
 
 constexpr int kTileRows = 16, kTileColumns = 128, kTileBytes = 1024;

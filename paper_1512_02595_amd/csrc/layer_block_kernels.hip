@@ -541,6 +541,29 @@ __global__ __launch_bounds__(1024) void ctc_block_norm_weights_kernel(const floa
     if (dscale) dscale[k] = static_cast<float>(weight_after ? sum * static_cast<double>(weight_after[k]) : sum);
 }
 
+// Zeros in an utterance's rows behind its end, so many of them to a workgroup, kept in the caches for the product that reads them (20800 of 48000 rows of 6144
+// bf16 44 us, past the caches 58; with four rows 44, with one 46, and the 64 wide 7 and 20 in place of 4).  Bound by the bytes.
+constexpr int kClearedAtOnce = 16;
+template <typename T> __global__ __launch_bounds__(256) void ctc_clear_frames_kernel(T* x, int64_t pitch, const int32_t* lengths, int frames, int B, int width)
+{
+    constexpr int kE = Vector<T>::kElements;
+    const int64_t at = group_number(), begin = at / B * kClearedAtOnce;
+    const int b = static_cast<int>(at % B);
+    if (begin >= frames) return;
+    const int64_t first = begin > lengths[b] ? begin : lengths[b], last = begin + kClearedAtOnce < frames ? begin + kClearedAtOnce : frames;
+    if (first >= last) return;
+    const unsigned vectors = static_cast<unsigned>((width + kE - 1) / kE), all = static_cast<unsigned>(last - first) * vectors;
+    for (unsigned i = threadIdx.x; i < all; i += 256) {
+        const int col = static_cast<int>(i % vectors) * kE;
+        T* const row = x + ((first + i / vectors) * B + b) * pitch;
+        const Vector<T> zeros{};
+        if (width < kE)
+            store_vector(row, col, width, zeros);
+        else                                        // (a row's last vector begins sooner, where it is not whole)
+            __builtin_memcpy(row + (col + kE <= width ? col : width - kE), &zeros, 16);
+    }
+}
+
 // Rows of up to 512 go to teams of as few lanes as hold them, wider ones to as many wavefronts.
 template <typename T> int launch_norm_of(const BlockNormArgs& p, hipStream_t s)
 {
@@ -571,6 +594,14 @@ template <typename T> int launch_backward_of(const BlockNormBackArgs& p, unsigne
 }
 
 }  // namespace
+
+int launch_clear_frames(void* x, int pitch, const int32_t* lengths, int T, int B, int width, bool bf16, void* stream)
+{
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const dim3 grid = spread(blocks(T, kClearedAtOnce) * static_cast<unsigned>(B));
+    return bf16 ? launch(ctc_clear_frames_kernel<bf16_t>, grid, 256, s, static_cast<bf16_t*>(x), static_cast<int64_t>(pitch), lengths, T, B, width)
+                : launch(ctc_clear_frames_kernel<float>, grid, 256, s, static_cast<float*>(x), static_cast<int64_t>(pitch), lengths, T, B, width);
+}
 
 int launch_block_norm(const BlockNormArgs& p, bool bf16, void* stream)
 {

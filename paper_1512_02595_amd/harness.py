@@ -355,10 +355,9 @@ class RecurrentBlock(_Block):
         dn, ds = (self._given(t, self.T, self.B, H) for t in (dnormed, dsum))
         df, first = (self._given(t, self.B, H, dtype=torch.float32) for t in (dfinal, initial))
         assert not {dn, ds} & {self.dresidual.data_ptr(), self.dstates.data_ptr()}
-        with self._on(stream):
-            # (The library leaves rows behind an utterance's end as they were, which may be the last minibatch's.  Which they are only the GPU knows.)
-            self.dprojections.zero_()
-            self.dresidual.zero_()
+        # (The other calls leave rows behind an utterance's end as they were, which may be the last minibatch's.)
+        for t, width in ((self.dprojections, 3 * H), (self.dresidual, H)):
+            block.clear_frames(t.data_ptr(), width, self.lengths.data_ptr(), self.T, self.B, width, self.dtype, s)
         block.block_norm_backward(dn, ds, self.states.data_ptr(), self._columns(projections, 2), 3 * H, self.sum.data_ptr(),
                                   self.weight_after.data_ptr(), self.scale.data_ptr(), self.weight_before.data_ptr(), self.eps,
                                   self.frames.data_ptr(), self.rows, H, self.dtype, self.dstates.data_ptr(), self._columns(self.dprojections, 2),

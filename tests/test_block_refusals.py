@@ -34,6 +34,7 @@ CALLS = {
                                 rows=200, H=100, dtype=F32, dx=address(9), dgate=address(10), dresidual=address(11),
                                 dweight_after=address(12), dscale=address(13), dweight_before=address(14), workspace=address(15),
                                 workspace_bytes=1 << 29),
+    "clear_frames": dict(x=address(0), pitch=100, input_lengths=address(1), T=500, B=4, width=80, dtype=F32),
     "quantize_weights_i4": dict(weights=address(0), A=29, H=300, group=128, dtype=F32, weight_q=address(1), weight_scales=address(2)),
     "dequantize_weights_i4": dict(weight_q=address(0), weight_scales=address(1), A=29, H=300, group=128, dtype=F32, out=address(2)),
     "linear_i4": dict(q=address(0), scales=address(1), weight_q=address(2), weight_scales=address(3), group=128, bias=address(4),
@@ -48,7 +49,7 @@ MAY_BE_NULL = {"recurrence": {"input_lengths", "initial", "final"},
 OUTPUTS = {"recurrence": {"states", "final", "workspace"}, "recurrence_backward": {"dinputs", "dinitial", "workspace"},
            "block_norm": {"sum", "normed"},
            "block_norm_backward": {"dx", "dgate", "dresidual", "dweight_after", "dscale", "dweight_before", "workspace"},
-           "quantize_weights_i4": {"weight_q", "weight_scales"}, "dequantize_weights_i4": {"out"}, "linear_i4": {"logits"}}
+           "clear_frames": {"x"}, "quantize_weights_i4": {"weight_q", "weight_scales"}, "dequantize_weights_i4": {"out"}, "linear_i4": {"logits"}}
 # outputs that may lie where an input does
 MAY_BE = {("recurrence", "final"): {"initial"}, ("recurrence_backward", "dinitial"): {"dfinal"},
           ("block_norm", "sum"): {"x", "residual"}, ("block_norm", "normed"): {"x", "residual"},
@@ -135,6 +136,15 @@ def test_sizes_and_types(name):
         assert status(name, A=(1 << 20) + 1) == UNSUPPORTED
     if "rows" in CALLS[name]:
         assert status(name, rows=(1 << 30) + 1) == UNSUPPORTED
+
+
+def test_columns_that_are_cleared():
+    for bad in (0, -1, 101):
+        assert status("clear_frames", width=bad) == INVALID
+    for bad in (0, -1, 79):
+        assert status("clear_frames", pitch=bad) == INVALID
+    assert status("clear_frames", pitch=(1 << 20) + 1) == UNSUPPORTED
+    assert status("clear_frames", pitch=(1 << 20) + 1, width=(1 << 20) + 1) == UNSUPPORTED
 
 
 def test_buffers_that_are_needed_together():
