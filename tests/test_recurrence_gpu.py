@@ -24,6 +24,9 @@ def lengths_of(kind, T, B, rng):
     n[rng.random(B) < 0.15] = 0
     if kind == "none":
         n[:] = 0
+    elif kind in ("equal", "up", "down", "powers"):
+        n = {"equal": np.full(B, T - 1), "up": np.linspace(0, T, B).astype(np.int32), "down": np.linspace(T + 3, -3, B).astype(np.int32),
+             "powers": np.minimum(1 << rng.integers(0, T.bit_length() + 1, B), T + 1)}[kind].astype(np.int32)
     elif B > 3:
         n[0], n[1], n[2] = T, -5, T + 7
     return torch.from_numpy(n).cuda(), [min(max(int(v), 0), T) for v in n]
@@ -141,6 +144,19 @@ def test_states(T, B, H, more, forward, dtype, kind):
 def test_gradient(T, B, H, more, forward, dtype, kind):
     say("recurrence back", T, B, H, more, forward, dtype, kind)
     c = Call(T, B, H, dtype, kind, 2 * H + more, forward, carried=kind != "all" or T % 2 == 1, slow=T > 200)
+    c.backward_call()
+    c.check_backward()
+
+
+@pytest.mark.parametrize("kind", ["equal", "up", "down", "powers"])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T, B, H", [(65, 64, 2), (128, 65, 64), (129, 191, 5), (255, 7, 130), (256, 200, 3), (300, 129, 1), (511, 16, 1030)])
+def test_utterances_in_every_order(T, B, H, dtype, kind):
+    """Long utterances are begun first: lengths that are all the same, in order, against it, and powers of two."""
+    say("orders", T, B, H, dtype, kind)
+    c = Call(T, B, H, dtype, kind, None, H // 2)
+    c.forward_call()
+    c.check_forward()
     c.backward_call()
     c.check_backward()
 
