@@ -524,14 +524,21 @@ __global__ __launch_bounds__(1024) void ctc_block_norm_weights_kernel(const floa
                                                                       float* __restrict__ dweight_after, float* __restrict__ dscale,
                                                                       float* __restrict__ dweight_before)
 {
+    constexpr int kAtOnce = 8;
     __shared__ double s_sum[16][16];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     // (each die has neighbouring columns, so that it has a line of memory's both halves)
     const int col = static_cast<int>(blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8) * 16 + lane % 16;
     double sum = 0.0;
+    // (eight at a time, all of them asked for at once: the last one again in place of those behind the end)
     if (col < 2 * H)
-#pragma unroll 16
-        for (int p = wave * 4 + lane / 16; p < count; p += 64) sum += static_cast<double>(partials[static_cast<int64_t>(p) * 2 * H + col]);
+        for (int p = wave * 4 + lane / 16; p < count; p += 64 * kAtOnce) {
+            float v[kAtOnce];
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) v[j] = partials[static_cast<int64_t>(p + 64 * j < count ? p + 64 * j : count - 1) * 2 * H + col];
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) sum += p + 64 * j < count ? static_cast<double>(v[j]) : 0.0;
+        }
     sum += __shfl_xor(sum, 16, kWave);
     sum += __shfl_xor(sum, 32, kWave);
     if (lane < 16) s_sum[wave][lane] = sum;
