@@ -412,109 +412,120 @@ __global__ __launch_bounds__(MANY ? kMostWaves * kWave : 256, 4) void ctc_block_
     }
 }
 
-// Rows of more than 8192, whose tensors a compute unit's registers do not hold beside the sums: a workgroup to a row, which reads it twice from memory and once more from the
-// caches, and adds to its own partial sums where they lie.
-template <typename T> __global__ __launch_bounds__(1024) void ctc_block_norm_backward_wide_kernel(BlockNormBackArgs p)
+// Rows of more than 8192: sixteen elements a thread, whose registers do not hold the row's tensors beside the sums: the partial sums are in LDS (a thread's columns
+// are its own), and all but x and the gradient at it are read a second time, from the caches, when the row's first sums are there.  Bound by waits, one workgroup a
+// compute unit: 6000 x 9000 bf16 387 us, fp32 463, 3000 x 16384 253 and 352 (partial sums in memory and x read three times: 872, 818, 725 and 719).
+template <typename T> __global__ __launch_bounds__(kMostWaves * kWave) void ctc_block_norm_backward_wide_kernel(BlockNormBackArgs p)
 {
-    constexpr int kE = Vector<T>::kElements, kStep = 1024 * kE;
+    constexpr int E = 16, kE = Vector<T>::kElements, kVectors = E / kE;
     __shared__ double s_first[3][kMostWaves], s_second[1][kMostWaves];
+    __shared__ __attribute__((aligned(16))) float s_dw[2][kMaxWidth];
     const Team<kWave, true> team;
     const int n = listed(p.frames, p.rows);
     const double share = 1.0 / p.H, eps = static_cast<double>(p.eps);
-    float* const sums_out = p.partials ? p.partials + static_cast<int64_t>(blockIdx.x) * 2 * p.H : nullptr;
-    if (sums_out)
-        for (int col = threadIdx.x * kE; col < p.H; col += kStep)
-            for (int k = 0; k < kE && col + k < p.H; ++k) sums_out[col + k] = sums_out[p.H + col + k] = 0.0f;
-    for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
+    const int stride = team.threads * kE;
+#pragma unroll
+    for (int v = 0; v < kVectors; ++v)
+#pragma unroll
+        for (int k = 0; k < kE; ++k) s_dw[0][(v * team.threads + team.thread) * kE + k] = s_dw[1][(v * team.threads + team.thread) * kE + k] = 0.0f;
+    for (int64_t i = team.first; i < n; i += team.teams) {
         const int r = row_of(p.frames, p.rows, static_cast<int>(i));
         if (r < 0) continue;
         const int64_t row = static_cast<int64_t>(r) * p.H;
-        const T* const at_x = static_cast<const T*>(p.x) + row;
-        const T* const at_z = static_cast<const T*>(p.sum) + row;
-        const T* const at_dy = static_cast<const T*>(p.dnormed) + row;
+        int mine = team.thread * kE;
+        asm("" : "+v"(mine));                                           // (worked out again for each row, where it would fill registers)
+        Vector<T> x[kVectors];
         double sums[3] = {};
-        for (int col = threadIdx.x * kE; col < p.H; col += kStep) {
-            const Vector<T> x = load_vector(at_x, col, p.H);
+#pragma unroll
+        for (int v = 0; v < kVectors; ++v) {
+            const int col = v * stride + mine;
+            x[v] = load_vector(static_cast<const T*>(p.x) + row, col, p.H);
             Vector<T> z{}, dy{};
             if (p.dnormed) {
-                z = load_vector(at_z, col, p.H);
-                dy = load_vector(at_dy, col, p.H);
+                z = load_vector(static_cast<const T*>(p.sum) + row, col, p.H);
+                dy = load_vector(static_cast<const T*>(p.dnormed) + row, col, p.H);
             }
 #pragma unroll
-            for (int v = 0; v < kE; v += 4) {
-                const Vector<float> w = weights_at(p.weight_before, col + v, p.H);
+            for (int u = 0; u < kE; u += 4) {
+                const Vector<float> w = weights_at(p.weight_before, col + u, p.H);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const double a = static_cast<double>(widen(x.v[v + j])), b = static_cast<double>(widen(z.v[v + j]));
+                    const double a = static_cast<double>(widen(x[v].v[u + j])), b = static_cast<double>(widen(z.v[u + j]));
                     sums[0] += a * a;
                     sums[1] += b * b;
-                    sums[2] += static_cast<double>(widen(dy.v[v + j]) * w.v[j]) * b;
+                    sums[2] += static_cast<double>(widen(dy.v[u + j]) * w.v[j]) * b;
                 }
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
         team.sum(sums, sums, s_first);
         const double r1 = rsqrt(fma(sums[0], share, eps)), r2 = rsqrt(fma(sums[1], share, eps));
         const float f1 = static_cast<float>(r1), f2 = static_cast<float>(r2), c2 = static_cast<float>(sums[2] * share * r2 * r2);
+        forget(x);
+        asm("" : "+v"(mine));
         double along[1] = {};
-        float c1 = 0.0f;
-        // Twice: for the sum along x and what needs no such sum but the partial sums, then for what is written, which may be in the inputs' place.
-#pragma unroll 1
-        for (int pass = 0; pass < 2; ++pass) {
-            for (int col = threadIdx.x * kE; col < p.H; col += kStep) {
-                const Vector<T> x = load_vector(at_x, col, p.H);
-                Vector<T> g{}, z{}, dy{}, dz{};
-                if (p.gate) g = load_vector(static_cast<const T*>(p.gate) + r * p.gate_pitch, col, p.H);
-                if (p.dnormed) {
-                    z = load_vector(at_z, col, p.H);
-                    dy = load_vector(at_dy, col, p.H);
-                }
-                if (p.dsum) dz = load_vector(static_cast<const T*>(p.dsum) + row, col, p.H);
-                Vector<T> dx;
+        float e[E];
+        // What is written may be in the inputs' place: a thread reads its columns, and no other's, before it writes them.
 #pragma unroll
-                for (int v = 0; v < kE; v += 4) {
-                    const Vector<float> wa = weights_at(p.weight_after, col + v, p.H), ws = weights_at(p.scale, col + v, p.H);
-                    const Vector<float> wb = weights_at(p.weight_before, col + v, p.H);
-                    Vector<float> more[2] = {};
-                    if (sums_out && !pass) {
-                        more[0] = load_vector(sums_out, col + v, p.H);
-                        more[1] = load_vector(sums_out + p.H, col + v, p.H);
-                    }
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float dyk = widen(dy.v[v + j]), zk = widen(z.v[v + j]), xk = widen(x.v[v + j]), after = wa.v[j] * ws.v[j];
-                        const float d = (dyk * wb.v[j] - zk * c2) * f2 + widen(dz.v[v + j]);
-                        float a = 1.0f;
-                        const float normed = xk * f1;
-                        if (p.gate) {
-                            const float gate = widen(g.v[v + j]);
-                            const Gate s = gate_of<sizeof(T) == 4>(gate);
-                            a = gate * s.z;
-                            g.v[v + j] = narrow<T>(d * after * normed * (s.z + a * s.stays));
-                        }
-                        const float e = d * a * after;
-                        along[0] += pass ? 0.0 : static_cast<double>(e) * static_cast<double>(xk);
-                        more[0].v[j] += dyk * (zk * f2);
-                        more[1].v[j] += d * a * normed;
-                        dx.v[v + j] = narrow<T>((e - xk * c1) * f1);
-                        dz.v[v + j] = narrow<T>(d);
-                    }
-                    if (sums_out && !pass) {
-                        for (int j = 0; j < 4 && col + v + j < p.H; ++j) {
-                            sums_out[col + v + j] = more[0].v[j];
-                            sums_out[p.H + col + v + j] = more[1].v[j];
-                        }
-                    }
-                }
-                if (!pass) continue;
-                store_vector(static_cast<T*>(p.dx) + row, col, p.H, dx);
-                if (p.gate) store_vector(static_cast<T*>(p.dgate) + r * p.gate_pitch, col, p.H, g);
-                if (p.dresidual) store_vector(static_cast<T*>(p.dresidual) + row, col, p.H, dz);
+        for (int v = 0; v < kVectors; ++v) {
+            const int col = v * stride + mine;
+            Vector<T> g{}, z{}, dy{}, dz{};
+            if (p.gate) g = load_vector(static_cast<const T*>(p.gate) + r * p.gate_pitch, col, p.H);
+            if (p.dnormed) {
+                z = load_vector(static_cast<const T*>(p.sum) + row, col, p.H);
+                dy = load_vector(static_cast<const T*>(p.dnormed) + row, col, p.H);
             }
-            if (pass) break;
-            team.sum(along, along, s_second);
-            c1 = static_cast<float>(along[0] * share * r1 * r1);
+            if (p.dsum) dz = load_vector(static_cast<const T*>(p.dsum) + row, col, p.H);
+#pragma unroll
+            for (int u = 0; u < kE; u += 4) {
+                const Vector<float> wa = weights_at(p.weight_after, col + u, p.H), ws = weights_at(p.scale, col + u, p.H);
+                const Vector<float> wb = weights_at(p.weight_before, col + u, p.H);
+                Vector<float> before = load_whole(&s_dw[0][col + u]), q = load_whole(&s_dw[1][col + u]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float dyk = widen(dy.v[u + j]), zk = widen(z.v[u + j]), xk = widen(x[v].v[u + j]), after = wa.v[j] * ws.v[j];
+                    const float d = (dyk * wb.v[j] - zk * c2) * f2 + widen(dz.v[u + j]), normed = xk * f1;
+                    dz.v[u + j] = narrow<T>(d);
+                    float a = 1.0f;
+                    if (p.gate) {
+                        const float gate = widen(g.v[u + j]);
+                        const Gate s = gate_of<sizeof(T) == 4>(gate);
+                        a = gate * s.z;
+                        g.v[u + j] = narrow<T>(d * after * normed * (s.z + a * s.stays));
+                    }
+                    before.v[j] += dyk * (zk * f2);
+                    q.v[j] += d * a * normed;
+                    const float here = d * a * after;
+                    e[v * kE + u + j] = here;
+                    along[0] += static_cast<double>(here) * static_cast<double>(xk);
+                }
+                __builtin_memcpy(&s_dw[0][col + u], &before, 16);
+                __builtin_memcpy(&s_dw[1][col + u], &q, 16);
+                __builtin_amdgcn_sched_barrier(0);                      // (registers)
+            }
+            if (p.gate) store_vector(static_cast<T*>(p.dgate) + r * p.gate_pitch, col, p.H, g);
+            if (p.dresidual) store_vector(static_cast<T*>(p.dresidual) + row, col, p.H, dz);
+        }
+        forget(x);
+        team.sum(along, along, s_second);
+        const float c1 = static_cast<float>(along[0] * share * r1 * r1);
+#pragma unroll
+        for (int v = 0; v < kVectors; ++v) {
+#pragma unroll
+            for (int j = 0; j < kE; ++j) x[v].v[j] = narrow<T>((e[v * kE + j] - widen(x[v].v[j]) * c1) * f1);
+            store_vector(static_cast<T*>(p.dx) + row, v * stride + mine, p.H, x[v]);
         }
     }
+    if (!p.partials) return;
+    float* const out = p.partials + static_cast<int64_t>(blockIdx.x) * 2 * p.H;
+#pragma unroll
+    for (int v = 0; v < kVectors; ++v)
+#pragma unroll
+        for (int u = 0; u < kE; u += 4) {
+            const int col = (v * team.threads + team.thread) * kE + u;
+            store_vector(out, col, p.H, load_whole(&s_dw[0][col]));
+            store_vector(out + p.H, col, p.H, load_whole(&s_dw[1][col]));
+        }
 }
 
 // The weights' gradients from the workgroups' sums, added in fp64: of the two sums a column has, one is dweight_before, of the other the two weights
@@ -604,7 +615,7 @@ template <typename T> int launch_backward_of(const BlockNormBackArgs& p, unsigne
     case 32: return launch(ctc_block_norm_backward_kernel<T, 32, false>, grid, 256, s, p);
     case 64: return launch(ctc_block_norm_backward_kernel<T, 64, false>, grid, 256, s, p);
     }
-    return team.elements == 8 ? launch(ctc_block_norm_backward_kernel<T, 64, true>, grid, team.lanes, s, p) : launch(ctc_block_norm_backward_wide_kernel<T>, grid, 1024, s, p);
+    return team.elements == 8 ? launch(ctc_block_norm_backward_kernel<T, 64, true>, grid, team.lanes, s, p) : launch(ctc_block_norm_backward_wide_kernel<T>, grid, team.lanes, s, p);
 }
 
 }  // namespace

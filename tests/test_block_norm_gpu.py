@@ -113,7 +113,7 @@ def test_forward_rows(rows, H, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("H", [64, 700, 1999, 5001])
+@pytest.mark.parametrize("H", [64, 700, 1999, 5001, 9001])
 def test_forward_absent_and_shared_buffers(H, dtype):
     for kind in LISTS:
         for gate, residual, weights in ((False, True, True), (True, False, True), (True, True, False), (False, False, False)):
@@ -177,7 +177,7 @@ def test_backward_rows(rows, H, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("H", [64, 700, 1999, 5001])
+@pytest.mark.parametrize("H", [64, 700, 1999, 5001, 9001])
 def test_backward_absent_and_shared_buffers(H, dtype):
     for kind in LISTS:
         for gate, weights in ((False, True), (True, False), (False, False)):
