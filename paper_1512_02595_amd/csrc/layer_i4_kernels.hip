@@ -169,7 +169,9 @@ __global__ __launch_bounds__(256) void ctc_quantize_weights_i4_wide_kernel(const
     if (j == 0) weight_scales[(row_tile * groups + unit) * 16 + r] = scale_of(most);
 }
 
-template <typename T>
+// PAST the caches, but for rows that begin anywhere, of whose 64 bytes several wavefronts write a part (20000 x 2047 fp32 59 us past the caches, so 30, bf16 40 and 19;
+// 24000 x 4096 fp32 63, kept in them 76).
+template <typename T, bool PAST>
 __global__ __launch_bounds__(256) void ctc_dequantize_weights_i4_kernel(const uint8_t* __restrict__ weight_q, const float* __restrict__ weight_scales,
                                                                         int A, int H, int group, int groups, int tiles, T* __restrict__ out)
 {
@@ -203,7 +205,10 @@ __global__ __launch_bounds__(256) void ctc_dequantize_weights_i4_kernel(const ui
         }
         const auto four = [&](const T (&v)[4], int c) {
             if (c + 4 <= H) {
-                store_past<sizeof(v)>(row + c, v);
+                if constexpr (PAST)
+                    store_past<sizeof(v)>(row + c, v);
+                else
+                    __builtin_memcpy(row + c, v, sizeof(v));
                 return;
             }
 #pragma unroll
@@ -506,8 +511,11 @@ int launch_dequantize_i4(const uint8_t* weight_q, const float* weight_scales, in
     hipStream_t s = static_cast<hipStream_t>(stream);
     const int tiles = pitch_of(H) / kTileColumns, groups = groups_of(H, group);
     const dim3 grid = spread(blocks(A, 16) * blocks(tiles, kTilesAtOnce));
-    if (bf16) return launch(ctc_dequantize_weights_i4_kernel<bf16_t>, grid, 256, s, weight_q, weight_scales, A, H, group, groups, tiles, static_cast<bf16_t*>(out));
-    return launch(ctc_dequantize_weights_i4_kernel<float>, grid, 256, s, weight_q, weight_scales, A, H, group, groups, tiles, static_cast<float*>(out));
+    const auto go = [&](auto* to, auto* past, auto* kept) {
+        return launch(H * sizeof(*to) % 64 == 0 ? past : kept, grid, 256, s, weight_q, weight_scales, A, H, group, groups, tiles, to);
+    };
+    if (bf16) return go(static_cast<bf16_t*>(out), ctc_dequantize_weights_i4_kernel<bf16_t, true>, ctc_dequantize_weights_i4_kernel<bf16_t, false>);
+    return go(static_cast<float*>(out), ctc_dequantize_weights_i4_kernel<float, true>, ctc_dequantize_weights_i4_kernel<float, false>);
 }
 
 int launch_linear_i4(const LinearI4Args& p, bool bf16, void* stream)
