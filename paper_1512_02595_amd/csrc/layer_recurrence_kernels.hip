@@ -36,9 +36,9 @@ template <typename T, int V> __device__ __forceinline__ Some<T, V> load_some(con
     __builtin_memcpy(&r, row + at, sizeof(r));
     return r;
 }
-template <typename T, int V> __device__ __forceinline__ void store_some(char* row, uint32_t at, const Some<T, V>& r)
+template <typename T, int V, bool PAST> __device__ __forceinline__ void store_some(char* row, uint32_t at, const Some<T, V>& r)
 {
-    if constexpr (sizeof(r) % 4 == 0)
+    if constexpr (PAST && sizeof(r) % 4 == 0)
         store_past<sizeof(r)>(row + at, &r);
     else
         __builtin_memcpy(row + at, &r, sizeof(r));
@@ -206,8 +206,8 @@ template <int V> __device__ __forceinline__ void leave_map(const RecurrenceArgs&
     }
 }
 
-// Rounds of WAVES runs of RUN frames.  BACK: the gradient, whose steps are an utterance's in the other order.
-template <typename T, int V, int RUN, int WAVES, Part PART, bool BACK>
+// Rounds of WAVES runs of RUN frames.  BACK: the gradient, whose steps are an utterance's in the other order.  PAST: what is written goes past the caches.
+template <typename T, int V, int RUN, int WAVES, Part PART, bool BACK, bool PAST>
 __global__ __launch_bounds__(WAVES * kWave) void ctc_recurrence_kernel(RecurrenceArgs p)
 {
     __shared__ Map s_map[WAVES > 1 ? 2 : 1][WAVES][V][kWave];
@@ -368,8 +368,8 @@ __global__ __launch_bounds__(WAVES * kWave) void ctc_recurrence_kernel(Recurrenc
             }
         char* to = static_cast<char*>(p.out) + row * (BACK ? row_bytes : state_bytes);
         const auto write = [&](int i) {
-            store_some<T, V>(to, at_gate, g[i]);
-            if constexpr (BACK) store_some<T, V>(to, at_candidate, c[i]);
+            store_some<T, V, PAST>(to, at_gate, g[i]);
+            if constexpr (BACK) store_some<T, V, PAST>(to, at_candidate, c[i]);
             to += BACK ? hop : hop_states;
         };
         if (!at.mine) {
@@ -392,12 +392,12 @@ __global__ __launch_bounds__(WAVES * kWave) void ctc_recurrence_kernel(Recurrenc
     }
 }
 
-template <typename T, int V, int RUN, int WAVES, Part PART, bool BACK> int launch_part(RecurrenceArgs p, int64_t tiles, hipStream_t s)
+template <typename T, int V, int RUN, int WAVES, Part PART, bool BACK, bool PAST = true> int launch_part(RecurrenceArgs p, int64_t tiles, hipStream_t s)
 {
     if (PART == Part::kSummary) --p.stretches;                  // (nobody asks for the last one's)
     // (at most 257 tiles by 65535 utterances: stretches come where places are few)
     const dim3 grid = spread(8 * units_of_a_die(static_cast<unsigned>(tiles * p.stretches), static_cast<unsigned>(p.B)));
-    return launch(ctc_recurrence_kernel<T, V, RUN, WAVES, PART, BACK>, grid, WAVES * kWave, s, p);
+    return launch(ctc_recurrence_kernel<T, V, RUN, WAVES, PART, BACK, PAST>, grid, WAVES * kWave, s, p);
 }
 
 template <typename T, int V, bool BACK> int launch_channels(RecurrenceArgs p, hipStream_t s)
@@ -411,6 +411,14 @@ template <typename T, int V, bool BACK> int launch_channels(RecurrenceArgs p, hi
     if (p.T <= 4) return launch_part<T, V, 4, 1, Part::kWhole, BACK>(p, tiles, s);
     if (plan.waves == 1) return launch_part<T, V, kFrames, 1, Part::kWhole, BACK>(p, tiles, s);
     if (plan.waves == 4) return launch_part<T, V, kFrames, 4, Part::kWhole, BACK>(p, tiles, s);
+    if constexpr (BACK && V == 2) {
+        // Of each 64 bytes at a tile's end two workgroups write a part, where rows begin anywhere: kept in the caches, 64 x 300 x 1999 bf16 128 us -> 110, fp32 213
+        // -> 198, 60 x 600 x 1500 172 -> 150 and 312 -> 298, 40 x 1000 x 515 fp32 114 -> 111.  But where the six tensors are not much more than the 256 MB cache holds,
+        // 200 x 100 x 333 fp32 35 and 43, 100 x 200 x 700 ragged 49 and 56, 40 x 1000 x 515 bf16 ragged 64 and 74.
+        const bool large = 6.0 * p.T * p.B * p.H * sizeof(T) > 384.0 * (1 << 20);
+        if (plan.stretches == 1 && large && p.pitch * sizeof(T) % 64 != 0)
+            return launch_part<T, V, kFrames, kRecurrenceWaves, Part::kWhole, BACK, false>(p, tiles, s);
+    }
     if (plan.stretches == 1) return launch_part<T, V, kFrames, kRecurrenceWaves, Part::kWhole, BACK>(p, tiles, s);
     const int err = launch_part<T, V, kFrames, kRecurrenceWaves, Part::kSummary, BACK>(p, tiles, s);
     return err ? err : launch_part<T, V, kFrames, kRecurrenceWaves, Part::kStretch, BACK>(p, tiles, s);

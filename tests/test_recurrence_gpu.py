@@ -161,6 +161,15 @@ def test_utterances_in_every_order(T, B, H, dtype, kind):
     c.check_backward()
 
 
+@pytest.mark.parametrize("T, B, H, dtype", [(150, 130, 901, F32), (200, 190, 901, BF16)])
+def test_gradient_of_more_than_the_caches_hold(T, B, H, dtype):
+    """Rows that begin anywhere, of 400 MB: what is written stays in the caches."""
+    say("large", T, B, H, dtype)
+    c = Call(T, B, H, dtype, "some", 2 * H + 1, 300)
+    c.backward_call()
+    c.check_backward()
+
+
 # ---- what may be done with the calls ----------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", TYPES)
